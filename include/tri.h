@@ -89,10 +89,15 @@ typedef enum tri_op {
   TRI_OP_RMSNORM = 1, TRI_OP_RES_RMSNORM = 2, TRI_OP_ROPE_QK = 3,
   TRI_OP_SWIGLU = 4, TRI_OP_CHAIN = 5, TRI_OP_QK_NORM_ROPE = 6,
   TRI_OP_CHAIN_LAYERS = 7,  /* selection records of tri_decode_chain_layers */
-  TRI_OP_SILU = 8, TRI_OP_ADD = 9, TRI_OP_MASKED_FILL = 10, TRI_OP_EMBEDDING = 11
+  TRI_OP_SILU = 8, TRI_OP_ADD = 9, TRI_OP_MASKED_FILL = 10, TRI_OP_EMBEDDING = 11,
+  TRI_OP_KV_SLOTS = 12, TRI_OP_KV_WRITE = 13, TRI_OP_PAGED_ATTENTION = 14
 } tri_op;
 
 enum { TRI_MAX_LAYERS = 1024 };   /* layers per tri_decode_chain_layers call */
+
+/* The paged KV cache: requests per call, slots per page, and workgroups that
+ * share the keys of one tile of queries, at most. */
+enum { TRI_MAX_REQUESTS = 4096, TRI_MAX_PAGE = 65536, TRI_MAX_KV_SPLITS = 64 };
 
 enum {
   TRI_CACHE_AUTO_INSTALL = 1u,   /* on a miss: install, then launch */
@@ -253,6 +258,58 @@ typedef struct tri_chain_args {
   /* optional RoPE variant (NULL: plain rotate-half over hd, int32 positions) */
   const tri_rope_ext *rope_ext;
 } tri_chain_args;
+
+/* A paged KV cache of one layer: n_pages pages of `page` slots, a slot the nk
+ * heads of hd elements of one token's K (and V). Strides in elements: from page
+ * to page (ps), slot to slot (ss) and head to head (hs); the hd elements of a
+ * head are contiguous. Any order of the three that does not overlap: slots of
+ * packed heads [n_pages, page, nk, hd], a page's slots head by head
+ * [n_pages, nk, page, hd], or views of larger tensors. */
+typedef struct tri_kv_cache {
+  void *k, *v;
+  int64_t k_ps, k_ss, k_hs;
+  int64_t v_ps, v_ss, v_hs;
+  int32_t n_pages, page, nk, hd;
+} tri_kv_cache;
+
+/* Arguments of tri_kv_slots. */
+typedef struct tri_kv_slots_args {
+  int64_t T;                 /* rows of slots and pos                          */
+  int32_t R;                 /* requests, 1..TRI_MAX_REQUESTS                  */
+  int32_t page;              /* slots per page                                 */
+  const int32_t *kv_len;     /* [R] tokens each request holds                  */
+  const int32_t *new_len;    /* [R] tokens each request adds                   */
+  int32_t *table;            /* [R, cols] block table, updated                 */
+  int64_t table_rs;
+  int32_t cols;
+  int32_t n_free;            /* entries of free_pages                          */
+  const int32_t *free_pages; /* [n_free] stack of free pages                   */
+  const int32_t *free_count; /* [1] pages on the stack                         */
+  int64_t *slots;            /* [T]                                            */
+  int32_t *pos;              /* [T]                                            */
+  int32_t *q_start;          /* [R + 1]                                        */
+  int32_t *kv_len_out;       /* [R]                                            */
+  int32_t *free_out;         /* [2]                                            */
+} tri_kv_slots_args;
+
+/* Arguments of tri_paged_attention. */
+typedef struct tri_attention_args {
+  int32_t dtype;             /* tri_dtype of q, out and the cache              */
+  int32_t nq;                /* query heads, a multiple of kv.nk               */
+  int64_t T;                 /* rows of q and out                              */
+  int32_t R;                 /* requests, 1..TRI_MAX_REQUESTS                  */
+  int32_t cols;              /* columns of the block table                     */
+  const void *q;   int64_t q_ts;
+  void *out;       int64_t o_ts;
+  const int32_t *table; int64_t table_rs;   /* [R, cols] block table           */
+  const int32_t *kv_len;     /* [R] tokens in the cache, the new ones included */
+  const int32_t *q_start;    /* [R + 1] first row of each request              */
+  float scale;
+  int32_t window;            /* keys a query sees, 0: all up to its own        */
+  int64_t max_kv;            /* a bound on kv_len the host knows, 0: none      */
+  void *workspace; int64_t workspace_bytes;
+  tri_kv_cache kv;
+} tri_attention_args;
 
 /* ---- cache ---------------------------------------------------------------- */
 
@@ -463,6 +520,76 @@ tri_status tri_masked_fill(tri_cache *cache, tri_dtype dtype, const void *x, int
 tri_status tri_embedding(tri_cache *cache, tri_dtype dtype, const void *table, int64_t t_rs,
                          int64_t n_rows, const void *ids, int32_t ids_int64,
                          void *out, int64_t o_rs, int64_t T, int64_t H, void *stream);
+
+/* ---- the paged KV cache of a serving step (not in the paper: what stands
+ * between the RoPE and the output projection of a decode step; vLLM-style
+ * pages). A step of R requests calls tri_kv_slots once, then for each layer
+ * tri_kv_write after the RoPE and tri_paged_attention. Same cache of versions,
+ * same guards (op, dtype, head layout, token bucket, 16-byte alignment;
+ * attention also its form and whether it splits the keys).
+ * Lengths, tables and slots are device data that the host never reads: a value
+ * out of range is handled as stated, and never reaches memory outside the
+ * operands. Launches carry their kernel arguments (no resident blocks), take
+ * the precompiled kernels under TRI_CACHE_JIT, and have one candidate plan. ---- */
+
+/* Pages, block table, slots and positions of a step, from request lengths.
+ * Request r holds c = clamp(kv_len[r], 0, cols * page) tokens in the first
+ * ceil(c / page) pages of its table row and adds n = max(new_len[r], 0):
+ *   q_start[r + 1] = q_start[r] + n (q_start[0] = 0), kv_len_out[r] = c + n,
+ *     both held at 2^31 - 1;
+ *   new pages: ceil((c + n) / page), at most cols, less those held. They come
+ *     off the top of the stack free_pages[0 .. free_count), request by request
+ *     and in table order; where the stack is empty the entry becomes -1. No
+ *     other entry of the table changes;
+ *   row q_start[r] + i < T: pos = c + i, slots = table entry of pos / page
+ *     times page plus pos % page, -1 without a page (none left, a negative
+ *     entry, beyond the table); rows from q_start[R] on: slots -1, pos 0;
+ *   free_out = {pages left on the stack, pages that were missing}: the count of
+ *     the next call's stack (free_count is clamped to [0, n_free]).
+ * The outputs must not overlap each other or an input (kv_len, free_count and
+ * free_pages are read while they are written); the table row stride is at
+ * least cols. cols * page must be below 2^31, page 1..TRI_MAX_PAGE. All
+ * pointers 4-byte aligned, slots 8. */
+tri_status tri_kv_slots(tri_cache *cache, const tri_kv_slots_args *args, void *stream);
+
+/* Store k, v [T, nk, hd] (heads packed) into their slots:
+ * K[slots[t] / page][slots[t] % page] = k[t], V likewise. A slot outside
+ * [0, n_pages * page) is skipped. The slots of one call must be distinct: of
+ * two rows with one slot either may remain, vector by vector. k and v must not
+ * overlap the cache. hd 1..512, nk 1..4096. */
+tri_status tri_kv_write(tri_cache *cache, tri_dtype dtype, const void *k, int64_t k_ts,
+                        const void *v, int64_t v_ts, const int64_t *slots, int64_t T,
+                        const tri_kv_cache *kv, void *stream);
+
+/* Causal attention of the new tokens over the paged cache. The rows
+ * q_start[r] .. q_start[r + 1] of q [T, nq, hd] (heads packed) are the last
+ * n = q_start[r + 1] - q_start[r] of request r's kv_len[r] tokens: row i of
+ * them stands at p = kv_len[r] - n + i and sees the keys j with
+ * 0 <= j <= p, j > p - window when window > 0, whose table entry is in
+ * [0, n_pages). Query head h takes K head h / (nq / nk):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,
+ * in float32 with one rounding at the end (bf16: the weights, at most 1, are
+ * rounded to bf16 before they meet V). Keys that are not seen contribute
+ * nothing, whatever their slots hold (NaN and infinities included); a row that
+ * sees no key, or whose scores are all -inf, is zero. Rows of out before
+ * q_start[0] and from q_start[R] on are left as they were. kv_len is clamped
+ * to [0, cols * page], q_start to [0, T] and must not decrease (rows that two
+ * requests claim hold either's result). out may alias q exactly.
+ * The keys of a tile of queries may be split over several workgroups that
+ * leave partial results in `workspace` (16-byte aligned device memory of the
+ * caller, its contents undefined before and after; two calls that may run at
+ * once need one each); a second launch joins them. The call splits no further
+ * than workspace_bytes allows: with NULL or 0 it does not split.
+ * tri_paged_attention_workspace gives what the call would use. max_kv only
+ * steers the split; a wrong one costs time, not correctness.
+ * hd 1..512; nq 1..4096; T * nq below 2^31; cols * page below 2^31; scale
+ * finite; window, max_kv >= 0. */
+tri_status tri_paged_attention(tri_cache *cache, const tri_attention_args *args, void *stream);
+
+/* Bytes of workspace that tri_paged_attention would use for these arguments
+ * (its workspace fields are ignored, pointers are not read); 0 when it does
+ * not split or the arguments are not valid. */
+int64_t tri_paged_attention_workspace(const tri_attention_args *args);
 
 /* For callers that cannot allocate device memory (code under HIP graph
  * capture, tight serving loops, harnesses that forbid allocation):

@@ -205,6 +205,44 @@ def _vector(t: torch.Tensor, name: str, n: int, dtype, dev: int) -> None:
     _on(t, name, dev)
 
 
+def _kv_view(t: torch.Tensor, name: str, n: int, page: int, nk: int, hd: int) -> tuple:
+    """Page, slot and head strides (elements) of a cache [n_pages, page, nk, hd]
+    whose heads are contiguous; dimensions of one report what a packed cache has."""
+    st = t.stride()
+    if hd > 1 and st[3] != 1:
+        raise ValueError(f"{name}: inner stride must be 1")
+    hs = st[2] if nk > 1 else hd
+    ss = st[1] if page > 1 else max(hd, nk * hs)
+    return st[0] if n > 1 else page * max(ss, nk * hs), ss, hs
+
+
+def _kv_cache(k: torch.Tensor, v: torch.Tensor, dtype, dev: int) -> L.KvCache:
+    """The tri_kv_cache of k and v [n_pages, page, nk, hd]."""
+    n, page, nk, hd = _dims(k, "k_cache", 4, dev)
+    _like(v, "v_cache", k.shape, dtype, dev)
+    _like(k, "k_cache", k.shape, dtype, dev)
+    return L.KvCache(k.data_ptr(), v.data_ptr(), *_kv_view(k, "k_cache", n, page, nk, hd),
+                     *_kv_view(v, "v_cache", n, page, nk, hd), n, page, nk, hd)
+
+
+def _int32(t: torch.Tensor, name: str, n: int, dev: int) -> int:
+    """The address of n (at least n where n is negative) contiguous int32."""
+    if (t.dim() != 1 or t.dtype != torch.int32 or (t.shape[0] > 1 and t.stride(0) != 1)
+            or (t.shape[0] != n if n >= 0 else t.shape[0] < -n)):
+        raise ValueError(f"{name}: expected a contiguous int32 tensor of "
+                         f"{n if n >= 0 else f'at least {-n}'}, got {tuple(t.shape)} {t.dtype}")
+    _on(t, name, dev)
+    return t.data_ptr()
+
+
+def _table(t: torch.Tensor, name: str, dev: int) -> tuple:
+    """Rows, columns and row stride of a block table [R, cols]."""
+    R, cols = _dims(t, name, 2, dev)
+    if t.dtype != torch.int32:
+        raise ValueError(f"{name}: expected int32, got {t.dtype}")
+    return R, cols, _rows(t, name, cols)
+
+
 class Graph:
     """A captured decode step (tri_graph); destroy before its cache."""
 
@@ -242,9 +280,12 @@ class Prepared:
     must not. A MISS installs and calls again, as the ordinary method does;
     an error raises TriError."""
 
-    __slots__ = ("_cache", "_what", "_fn", "_raw", "_args", "_cargs", "_max_misses", "result")
+    __slots__ = ("_cache", "_what", "_fn", "_raw", "_args", "_cargs", "_max_misses", "result",
+                 "_keep")
 
-    def __init__(self, cache: "SpecCache", what: str, fn, args, max_misses: int, result):
+    def __init__(self, cache: "SpecCache", what: str, fn, args, max_misses: int, result,
+                 keep=None):
+        self._keep = keep                      # the tensors behind the addresses
         self._cache = cache
         self._what = what
         self._fn = fn
@@ -364,7 +405,8 @@ class SpecCache:
         if len(rec) != 1:
             raise ValueError(f"prepare: {op!r} does not make exactly one entry call")
         what, fn, cargs, max_misses = rec[0]
-        return Prepared(self, what, fn, cargs[:-1], max_misses, result)
+        return Prepared(self, what, fn, cargs[:-1], max_misses, result,
+                        (args, kwargs))
 
     def install_last_miss(self) -> Selection:
         sel = Selection()
@@ -584,6 +626,88 @@ class SpecCache:
                    table.data_ptr(), _rows(table, "table", H), n_rows, ids.data_ptr(),
                    int(ids.dtype == torch.int64), o.data_ptr(), _rows(o, "out", H), T, H,
                    _stream_ptr(stream, self._dev))
+        return o
+
+    # ---- the paged KV cache --------------------------------------------------------
+    def kv_slots(self, kv_len, new_len, block_table, free_pages, free_count, page: int, T: int,
+                 slots=None, pos=None, q_start=None, kv_len_out=None, free_out=None, stream=None):
+        """Pages, block table, slots and positions of a step (tri_kv_slots).
+
+        Request r holds kv_len[r] tokens and adds new_len[r] (int32 [R]). New pages of `page`
+        slots come off the top of the stack free_pages[:free_count[0]] (int32) into block_table
+        (int32 [R, cols], updated in place; -1 where the stack is empty). Returns slots
+        (int64 [T], -1 without a page and past the last request), pos (int32 [T]), q_start
+        (int32 [R + 1]), kv_len_out (int32 [R]) and free_out (int32 [2]: pages left, pages
+        missing; the next step's free_count)."""
+        dev = self._dev
+        R, cols, rs = _table(block_table, "block_table", dev)
+        T = int(T)
+        kv, nw = _int32(kv_len, "kv_len", R, dev), _int32(new_len, "new_len", R, dev)
+        fp = _int32(free_pages, "free_pages", free_pages.numel(), dev)
+        fc = _int32(free_count, "free_count", -1, dev)
+
+        def new(t, n, dtype=torch.int32):
+            return torch.empty(n, dtype=dtype, device=block_table.device) if t is None else t
+
+        slots, pos = new(slots, T, torch.int64), new(pos, T)
+        q_start, kv_len_out, free_out = new(q_start, R + 1), new(kv_len_out, R), new(free_out, 2)
+        _vector(slots, "slots", T, torch.int64, dev)
+        a = L.KvSlotsArgs(T, R, page, kv, nw, block_table.data_ptr(), rs, cols,
+                          free_pages.shape[0], fp, fc, slots.data_ptr(),
+                          _int32(pos, "pos", T, dev), _int32(q_start, "q_start", R + 1, dev),
+                          _int32(kv_len_out, "kv_len_out", R, dev),
+                          _int32(free_out, "free_out", 2, dev))
+        self._call("tri_kv_slots", _dll.tri_kv_slots, C.byref(a), _stream_ptr(stream, dev))
+        return slots, pos, q_start, kv_len_out, free_out
+
+    def kv_write(self, k, v, slots, k_cache, v_cache, stream=None):
+        """Store k and v [T, nk, hd] in the slots (int64 [T]) of a paged cache
+        [n_pages, page, nk, hd] (any strides with contiguous heads); slots
+        out of range are skipped (tri_kv_write)."""
+        dev = self._dev
+        T, nk, hd = _dims(k, "k", 3, dev)
+        _like(v, "v", k.shape, k.dtype, dev)
+        _vector(slots, "slots", T, torch.int64, dev)
+        kv = _kv_cache(k_cache, v_cache, k.dtype, dev)
+        if (kv.nk, kv.hd) != (nk, hd):
+            raise ValueError(f"k_cache: expected heads ({nk}, {hd}), got ({kv.nk}, {kv.hd})")
+        self._call("tri_kv_write", _dll.tri_kv_write, dtype_code(k.dtype), k.data_ptr(),
+                   _tokens(k, "k", nk, hd), v.data_ptr(), _tokens(v, "v", nk, hd),
+                   slots.data_ptr(), T, C.byref(kv), _stream_ptr(stream, dev))
+        return k_cache, v_cache
+
+    def paged_attention(self, q, k_cache, v_cache, block_table, kv_len, q_start,
+                        scale: Optional[float] = None, window: int = 0, max_kv: int = 0,
+                        out=None, stream=None) -> torch.Tensor:
+        """Causal attention of q [T, nq, hd] over a paged cache [n_pages, page,
+        nk, hd] (tri_paged_attention): rows q_start[r]:q_start[r + 1] are the
+        last of request r's kv_len[r] tokens. scale defaults to hd ** -0.5;
+        window > 0 limits a row to its last `window` keys; max_kv, a bound on
+        kv_len that the host knows (0: the table's width), steers how the
+        work is split. Rows of no request keep what `out` held (an output made
+        here is not initialised)."""
+        dev = self._dev
+        T, nq, hd = _dims(q, "q", 3, dev)
+        o = torch.empty((T, nq, hd), dtype=q.dtype, device=q.device) if out is None else out
+        _like(o, "out", q.shape, q.dtype, dev)
+        R, cols, rs = _table(block_table, "block_table", dev)
+        kv = _kv_cache(k_cache, v_cache, q.dtype, dev)
+        if kv.hd != hd:
+            raise ValueError(f"k_cache: expected heads of {hd}, got {kv.hd}")
+        a = L.AttentionArgs(dtype_code(q.dtype), nq, T, R, cols, q.data_ptr(),
+                            _tokens(q, "q", nq, hd), o.data_ptr(), _tokens(o, "out", nq, hd),
+                            block_table.data_ptr(), rs, _int32(kv_len, "kv_len", R, dev),
+                            _int32(q_start, "q_start", R + 1, dev),
+                            hd ** -0.5 if scale is None else scale, window, max_kv, None, 0, kv)
+        need = _dll.tri_paged_attention_workspace(C.byref(a))
+        if need:
+            # on the call's stream: the allocator may hand the block on once
+            # the work queued there so far is done
+            with torch.cuda.stream(stream):
+                a._workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            a.workspace, a.workspace_bytes = a._workspace.data_ptr(), need
+        self._call("tri_paged_attention", _dll.tri_paged_attention, C.byref(a),
+                   _stream_ptr(stream, dev))
         return o
 
     def chain_args(self, x, residual, w, q, k, pos, gate, up, eps=1e-6, base=10000.0,

@@ -19,6 +19,8 @@ F32, BF16 = 0, 1
 OP_RMSNORM, OP_RES_RMSNORM, OP_ROPE_QK, OP_SWIGLU, OP_CHAIN, OP_QK_NORM_ROPE = 1, 2, 3, 4, 5, 6
 OP_CHAIN_LAYERS = 7
 OP_SILU, OP_ADD, OP_MASKED_FILL, OP_EMBEDDING = 8, 9, 10, 11
+OP_KV_SLOTS, OP_KV_WRITE, OP_PAGED_ATTENTION = 12, 13, 14
+MAX_REQUESTS, MAX_PAGE, MAX_KV_SPLITS = 4096, 65536, 64
 MAX_LAYERS = 1024
 AUTO_INSTALL = 1
 JIT = 2
@@ -100,6 +102,38 @@ class ChainArgs(C.Structure):
                 ("rope_ext", C.POINTER(RopeExt))]
 
 
+class KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_ps", C.c_int64), ("k_ss", C.c_int64), ("k_hs", C.c_int64),
+                ("v_ps", C.c_int64), ("v_ss", C.c_int64), ("v_hs", C.c_int64),
+                ("n_pages", C.c_int32), ("page", C.c_int32), ("nk", C.c_int32),
+                ("hd", C.c_int32)]
+
+
+class KvSlotsArgs(C.Structure):
+    _fields_ = [("T", C.c_int64), ("R", C.c_int32), ("page", C.c_int32),
+                ("kv_len", C.c_void_p), ("new_len", C.c_void_p),
+                ("table", C.c_void_p), ("table_rs", C.c_int64),
+                ("cols", C.c_int32), ("n_free", C.c_int32),
+                ("free_pages", C.c_void_p), ("free_count", C.c_void_p),
+                ("slots", C.c_void_p), ("pos", C.c_void_p), ("q_start", C.c_void_p),
+                ("kv_len_out", C.c_void_p), ("free_out", C.c_void_p)]
+
+
+class AttentionArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("nq", C.c_int32), ("T", C.c_int64),
+                ("R", C.c_int32), ("cols", C.c_int32),
+                ("q", C.c_void_p), ("q_ts", C.c_int64),
+                ("out", C.c_void_p), ("o_ts", C.c_int64),
+                ("table", C.c_void_p), ("table_rs", C.c_int64),
+                ("kv_len", C.c_void_p), ("q_start", C.c_void_p),
+                ("scale", C.c_float), ("window", C.c_int32), ("max_kv", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
+                ("kv", KvCache)]
+
+
+assert C.sizeof(KvCache) == 80 and C.sizeof(KvSlotsArgs) == 112
+assert C.sizeof(AttentionArgs) == 200
 assert C.sizeof(Selection) == 120 and C.sizeof(ChainArgs) == 240 and C.sizeof(RopeExt) == 48
 assert C.sizeof(VersionInfo) == 144 and C.sizeof(ResidentInfo) == 16
 
@@ -126,6 +160,11 @@ SIGNATURES = {
                                   _P]),
     "tri_embedding": (C.c_int, [_P, C.c_int, _P, _I64, _I64, _P, _I32, _P, _I64, _I64, _I64,
                                 _P]),
+    "tri_kv_slots": (C.c_int, [_P, C.POINTER(KvSlotsArgs), _P]),
+    "tri_kv_write": (C.c_int, [_P, C.c_int, _P, _I64, _P, _I64, _P, _I64, C.POINTER(KvCache),
+                               _P]),
+    "tri_paged_attention": (C.c_int, [_P, C.POINTER(AttentionArgs), _P]),
+    "tri_paged_attention_workspace": (_I64, [C.POINTER(AttentionArgs)]),
     "tri_decode_chain": (C.c_int, [_P, C.POINTER(ChainArgs), _P]),
     "tri_decode_chain_layers": (C.c_int, [_P, C.POINTER(ChainArgs), _U32, _P]),
     "tri_graph_build_layers": (C.c_int, [_P, C.POINTER(ChainArgs), _U32, C.POINTER(C.c_void_p)]),

@@ -239,8 +239,9 @@ tri_status install_key(tri_cache *c, const Key &k, int32_t candidate, bool gener
   }
 
   // A compiled specialization fixes the key's shape fields, so a version
-  // with a range of row lengths runs the precompiled kernels.
-  if ((c->flags & TRI_CACHE_JIT) && v.guard.h_lo == 0) {
+  // with a range of row lengths runs the precompiled kernels; so do the paged
+  // ops, whose kernels already have the head size at compile time.
+  if ((c->flags & TRI_CACHE_JIT) && v.guard.h_lo == 0 && !is_paged_op(op)) {
     // Compile one specialization per launch of the plan (Sec. 3.5 growth),
     // or load it from the code directory.
     v.jit = 2;
@@ -402,6 +403,9 @@ tri_status tri_spec_install_last_miss(tri_cache *c, tri_selection *out) {
   if (out) {
     const int32_t i = scan_versions(c, c->miss_key);
     if (i >= 0) fill_selection(c->versions[i], i, c->miss_T, out, &c->miss_key);
+    // the paged ops' launches depend on more than the key and T
+    if (is_paged_op(key_op(c->miss_key)))
+      for (int j = 0; j < out->n_launches; ++j) out->launch[j].grid_x = c->miss_grid[j];
   }
   return TRI_OK;
 }

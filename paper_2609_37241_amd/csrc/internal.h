@@ -22,6 +22,8 @@ enum Variant : int32_t {
   CH_FUSED = 50, CH_SEQ = 51,
   ELT_SCALAR = 60, ELT_FLAT = 61, ELT_FLAT_U2 = 62, ELT_ROWS = 63,
   EMB_SCALAR = 70, EMB_VEC = 71,
+  KV_SLOTS = 80, KVW_ANY = 82, KVW_VEC = 83,
+  PA_ANY = 90, PA_JOIN = 93,
   EMPTY = 99,
 };
 
@@ -50,12 +52,17 @@ constexpr uint32_t kMaxCapacity = 4096;
 constexpr unsigned kAlign = 1, kContig = 2;   // per-role guard flag bits
 constexpr unsigned kChainQkNorm = 0x40;        // chain key flag: QK-RMSNorm before RoPE
 
+// The paged KV cache.
+constexpr int32_t kAttnHdMax = 512;        // head sizes of kv_write and attention
+constexpr int64_t kPosLimit = int64_t(1) << 31;   // positions and rows * heads are below this
+
 // ---- key --------------------------------------------------------------------------
 // k0: op | dtype << 8 | bucket << 16 | flags << 24 | RoPE base bits << 32
 // k1: H | I << 32
 // k2: hd | nq << 16 | nk << 32
 // k3: rotary dim | variant bits << 16 | scaling << 24 | original_max_pos << 32
 // k4: factor bits | low_freq_factor bits << 32;  k5: high_freq_factor bits
+// Attention: k3 = form << 16 | split << 24 (AttnForm; 1: keys split and joined).
 // Fields an op does not use are zero.
 struct Key {
   uint64_t k0, k1, k2, k3, k4, k5;
@@ -155,6 +162,34 @@ inline uint32_t rope_geometry_bits(int32_t slices, int32_t tokens) {
 // Element-wise ops (silu, add, masked_fill) over [T, W] and embedding rows.
 Role elt_role(uint32_t dtype, int64_t W, unsigned flags, uint32_t bucket, int64_t T);
 Role emb_role(uint32_t dtype, int64_t H, unsigned flags, int64_t T);
+
+// ---- the paged KV cache ----
+inline bool is_paged_op(uint32_t op) { return op >= TRI_OP_KV_SLOTS && op <= TRI_OP_PAGED_ATTENTION; }
+// How attention computes: any alignment and head size, a wavefront per row.
+enum AttnForm : uint32_t { kAttnAny = 0 };
+inline uint32_t key_attn_form(const Key &k) { return uint32_t((k.k3 >> 16) & 0xFF); }
+inline bool key_attn_split(const Key &k) { return (k.k3 >> 24) & 1; }
+// Form, splits and launch geometry of an attention call.
+struct AttnPlan {
+  uint32_t form;
+  int32_t splits;
+  int32_t tiles;         // tiles of queries per K head (matrix forms)
+  uint32_t grid[2];      // the attention launch, and the join's when splits > 1
+};
+// `aligned`: every address and stride of q, out and the cache is a multiple of
+// 16 bytes. kv_max: the most keys a row can see. workspace: bytes available.
+AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
+                   bool aligned, int64_t kv_max, uint64_t workspace);
+// Bytes a call of T rows with `splits` needs: per row and split hd sums, a
+// maximum and a sum, in float32.
+inline uint64_t attn_workspace(int64_t T, int32_t nq, int32_t hd, int32_t splits) {
+  return splits > 1 ? uint64_t(T) * uint64_t(nq) * uint64_t(splits) * uint64_t(hd + 2) * 4 : 0;
+}
+// Whether the matrix forms serve a head size at 16-byte alignment.
+uint32_t kv_slots_grid(int64_t T, int32_t R);
+uint32_t kv_write_grid(int64_t T, uint32_t row_items);
+// n / d by multiplication (kernargs.h).
+FastDiv fast_div_of(uint32_t d);
 
 // A version's plan: which kernels it launches, fixed at install.
 struct Plan {
@@ -306,7 +341,7 @@ struct Version {
   uint64_t hits;
 };
 
-constexpr int kOps = 12;   // op ids 1..11
+constexpr int kOps = 15;   // op ids 1..14
 
 // Memo of first matches: a direct-mapped table of keys and the version
 // Algorithm 1's scan selected for them. First match depends only on the key
@@ -331,6 +366,7 @@ struct tri_cache {
   bool has_miss;
   tri::Key miss_key;
   int64_t miss_T;
+  uint32_t miss_grid[2];         // paged ops: the launches of the missed call
   tri_stats stats;
   tri_selection last;
   void *empty_fn;

@@ -143,6 +143,68 @@ struct ChainArgs {
   uint32_t rope_blocks;
 };
 
+// ---- the paged KV cache ----
+// n / d for n < 2^31 and 1 <= d < 2^31 as (n * mul) >> 32 >> shift: with
+// shift = ceil(log2 d) - 1 and mul = floor(2^(32 + shift) / d) + 1 the product
+// exceeds n / d by less than n / 2^(32 + shift) < 1 / d (0 stands for d = 1).
+struct FastDiv {
+  uint32_t mul, shift;
+};
+
+// Where the heads of a paged K or V lie: elements from page to page, slot to
+// slot and head to head.
+struct PagedView {
+  void *p;
+  int64_t ps, ss, hs;
+};
+
+// Pages, block table, slots and positions of a step (KV_SLOTS).
+struct KvSlotsArgs {
+  const int32_t *kv_len, *new_len;
+  int32_t *table;
+  const int32_t *free_pages, *free_count;
+  int64_t *slots;
+  int32_t *pos, *q_start, *kv_len_out, *free_out;
+  int64_t T, table_rs;
+  int32_t R, page, cols, n_free;
+  FastDiv div;            // by page
+};
+
+// New K and V rows into their slots (KVW_*).
+struct KvWriteArgs {
+  const void *k, *v;
+  const int64_t *slots;
+  PagedView ck, cv;
+  int64_t k_ts, v_ts, T;
+  int64_t n_slots;        // n_pages * page
+  int32_t page, nk, hd;
+  FastDiv div;            // by page
+  FastDiv row_div;        // by the work-items that a row takes
+  uint32_t row_items;
+};
+
+// Attention over pages (PA_*). With splits > 1 a workgroup leaves, for each of
+// its rows (t * nq + head), hd float32 sums at part[(row * splits + s) * hd]
+// and (maximum, sum) at ml[row * splits + s]; PA_JOIN adds them up.
+struct PagedArgs {
+  const void *q;
+  void *out;
+  PagedView k, v;
+  const int32_t *table, *kv_len, *q_start;
+  float *part;
+  float *ml;             // pairs
+  int64_t q_ts, o_ts, table_rs;
+  int32_t T, R, cols, n_pages;
+  int32_t page, nq, nk, hd;
+  int32_t g;              // query heads per K head
+  int32_t splits;
+  int32_t tiles;          // tiles of queries per K head
+  int32_t window;
+  float scale;            // times log2 e: the weights are powers of two
+  FastDiv div;            // by page
+  FastDiv g_div;          // by g
+};
+
 // An argument block held in device memory for launches without kernel
 // arguments: the kernel's argument struct (zero beyond its size), the
 // launch's workgroup count and a tag that marks the slot as written
@@ -185,6 +247,12 @@ static_assert(sizeof(EltArgs) == 88 && __builtin_offsetof(EltArgs, value) == 80,
 static_assert(sizeof(EmbArgs) == 72 && __builtin_offsetof(EmbArgs, ids64) == 64, "EmbArgs layout");
 static_assert(sizeof(ChainArgs) == 288 && __builtin_offsetof(ChainArgs, rn_blocks) == 280,
               "ChainArgs layout");
+static_assert(sizeof(KvSlotsArgs) == 120 && __builtin_offsetof(KvSlotsArgs, div) == 112,
+              "KvSlotsArgs layout");
+static_assert(sizeof(KvWriteArgs) == 152 && __builtin_offsetof(KvWriteArgs, row_items) == 148,
+              "KvWriteArgs layout");
+static_assert(sizeof(PagedArgs) == 216 && __builtin_offsetof(PagedArgs, div) == 196,
+              "PagedArgs layout");
 static_assert(sizeof(ResidentBlock) == 320 && __builtin_offsetof(ResidentBlock, grid) == 288 &&
                   __builtin_offsetof(ResidentBlock, tag) == 292,
               "ResidentBlock layout");

@@ -1,0 +1,64 @@
+// Device-side building blocks of the paged KV cache's kernels: division by a
+// launch constant, the request that a row belongs to, the slot of a key, and
+// what the attention forms share.
+#pragma once
+#include "device.h"
+
+namespace tri {
+namespace dev {
+
+__device__ inline uint32_t fast_div(uint32_t n, FastDiv d) {
+  return d.mul ? __umulhi(n, d.mul) >> d.shift : n;
+}
+
+__device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kNegInf = -__builtin_inff();
+
+// The keys that the rows of one request see. Lengths and starts are device
+// data and may hold anything: clamped so that every row lies in [0, T) and
+// every key in the table.
+struct Request {
+  int32_t q0, q1;   // rows
+  int32_t kv;       // tokens in the cache
+};
+
+__device__ inline int32_t clamp_i32(int32_t v, int32_t lo, int32_t hi) {
+  return v < lo ? lo : v > hi ? hi : v;
+}
+
+__device__ inline Request request_of(const PagedArgs &a, int32_t r) {
+  Request q;
+  q.q0 = clamp_i32(a.q_start[r], 0, a.T);
+  q.q1 = clamp_i32(a.q_start[r + 1], 0, a.T);
+  q.kv = clamp_i32(a.kv_len[r], 0, a.cols * a.page);
+  return q;
+}
+
+// First key that the row at position p (>= 0) sees.
+__device__ inline int32_t first_key(int32_t p, int32_t window) {
+  return window > 0 && p >= window ? p - window + 1 : 0;
+}
+
+// Elements from the start of K (or V) to a key's slot, or -1 where its page is
+// not in the pool. `key` must be below cols * page.
+__device__ inline int64_t slot_offset(const int32_t *row, uint32_t key, const PagedArgs &a,
+                                      const PagedView &c) {
+  const uint32_t col = fast_div(key, a.div);
+  const int32_t id = row[col];
+  if (uint32_t(id) >= uint32_t(a.n_pages)) return -1;
+  return int64_t(id) * c.ps + int64_t(key - col * uint32_t(a.page)) * c.ss;
+}
+
+// The keys [lo, hi) of a tile cut into `splits` runs of whole 64s: run s.
+__device__ inline void split_keys(int32_t lo, int32_t hi, int32_t splits, int32_t s, int32_t *b,
+                                  int32_t *e) {
+  const int32_t n = hi > lo ? hi - lo : 0;
+  const int64_t run = (int64_t(n) + int64_t(splits) * 64 - 1) / (int64_t(splits) * 64) * 64;
+  const int64_t first = lo + s * run, last = first + run;
+  *b = first < hi ? int32_t(first) : hi;
+  *e = last < hi ? int32_t(last) : hi;
+}
+
+}  // namespace dev
+}  // namespace tri

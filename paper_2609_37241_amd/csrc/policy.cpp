@@ -210,6 +210,41 @@ Role emb_role(uint32_t dtype, int64_t H, unsigned flags, int64_t T) {
           slot_grid(dtype, T, H, kEmbSlots)};
 }
 
+// ---- the paged KV cache ----
+FastDiv fast_div_of(uint32_t d) {
+  if (d <= 1) return {0, 0};
+  const uint32_t l = uint32_t(32 - __builtin_clz(d - 1));   // ceil(log2 d)
+  return {uint32_t((uint64_t(1) << (31 + l)) / d + 1), l - 1};
+}
+
+uint32_t kv_slots_grid(int64_t T, int32_t R) {
+  const int64_t rows = T > R ? T : int64_t(R);
+  const int64_t g = cdiv(rows, 4 * int64_t(kBlock));
+  return uint32_t(g > 256 ? 256 : g);
+}
+
+uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
+  return clamp_grid(cdiv(T * int64_t(row_items), kBlock));
+}
+
+AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
+                   bool aligned, int64_t kv_max, uint64_t workspace) {
+  (void)dtype, (void)R, (void)nk, (void)aligned;
+  AttnPlan p{};
+  p.form = kAttnAny;
+  p.splits = 1;
+  const int64_t rows = T * nq;
+  // 2048 wavefronts, runs of at least 256 keys
+  const int64_t want = cdiv(2048, rows), most = cdiv(kv_max, 256);
+  int64_t s = want < most ? want : most;
+  if (s > TRI_MAX_KV_SPLITS) s = TRI_MAX_KV_SPLITS;
+  while (s > 1 && attn_workspace(T, nq, hd, int32_t(s)) > workspace) --s;
+  p.splits = s < 1 ? 1 : int32_t(s);
+  p.grid[0] = clamp_grid(cdiv(rows * p.splits, 4));
+  p.grid[1] = clamp_grid(cdiv(rows, 4));
+  return p;
+}
+
 // Workgroups of a role variant for T tokens (I is the row width: the norm
 // row H, the SwiGLU width, the row width of an element-wise op, or the
 // embedding row width).
@@ -258,12 +293,28 @@ int32_t fused_sub(int32_t rn, int32_t rope, int32_t sw) {
 
 }  // namespace
 
+// Keys of the paged ops: the head layout (none for the bookkeeping, no query
+// heads for the store); attention's form and splits in word 3.
+static bool paged_key_valid(const Key &k) {
+  const uint32_t op = key_op(k), hd = key_hd(k), nq = key_nq(k), nk = key_nk(k);
+  if (key_flags(k) & kContig || k.k0 >> 32 || k.k1 || k.k4 || k.k5 || k.k2 >> 48) return false;
+  if (op == TRI_OP_KV_SLOTS)
+    return key_dtype(k) == 0 && key_flags(k) == 0 && k.k2 == 0 && k.k3 == 0;
+  if (hd < 1 || int32_t(hd) > kAttnHdMax || nk < 1 || int32_t(nk) > kHeadsMax) return false;
+  if (op == TRI_OP_KV_WRITE) return nq == 0 && k.k3 == 0;
+  const uint32_t form = key_attn_form(k);
+  if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
+  if (k.k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
+  return form == kAttnAny;
+}
+
 // A key the entry points could have produced (used to check imported keys):
 // the same limits as argument validation, unused fields zero.
 bool key_valid(const Key &k) {
   const uint32_t op = key_op(k), dt = key_dtype(k), fl = key_flags(k);
   const bool short_op = op >= TRI_OP_SILU && op <= TRI_OP_EMBEDDING;
-  if ((op < TRI_OP_RMSNORM || op > TRI_OP_QK_NORM_ROPE) && !short_op) return false;
+  if ((op < TRI_OP_RMSNORM || op > TRI_OP_QK_NORM_ROPE) && !short_op && !is_paged_op(op))
+    return false;
   if (dt != TRI_F32 && dt != TRI_BF16) return false;
   if (key_bucket(k) > 22) return false;
   const bool chain = op == TRI_OP_CHAIN;
@@ -275,6 +326,7 @@ bool key_valid(const Key &k) {
     const uint64_t k3_ok = op == TRI_OP_EMBEDDING ? (uint64_t(1) << 16) : 0;
     return (k.k0 >> 32) == 0 && k.k2 == 0 && (k.k3 & ~k3_ok) == 0 && k.k4 == 0 && k.k5 == 0;
   }
+  if (is_paged_op(op)) return paged_key_valid(k);
   const bool norm = op == TRI_OP_RMSNORM || op == TRI_OP_RES_RMSNORM || chain;
   const bool sw = op == TRI_OP_SWIGLU || chain;
   const bool rope = op == TRI_OP_ROPE_QK || op == TRI_OP_QK_NORM_ROPE || chain;
@@ -354,6 +406,20 @@ Plan plan_for_key(const Key &k) {
       p.ksub[0] = int32_t(key_rope_bits(k) & 1);   // int64 ids
       return p;
     }
+    case TRI_OP_KV_SLOTS:
+      p.variant = p.kvariant[0] = KV_SLOTS;
+      p.n_launches = 1;
+      return p;
+    case TRI_OP_KV_WRITE:
+      p.variant = p.kvariant[0] =
+          (fl & kAlign) && key_hd(k) % vec_elems(dt) == 0 ? KVW_VEC : KVW_ANY;
+      p.n_launches = 1;
+      return p;
+    case TRI_OP_PAGED_ATTENTION:
+      p.variant = p.kvariant[0] = PA_ANY;
+      p.n_launches = 1;
+      if (key_attn_split(k)) p.kvariant[p.n_launches++] = PA_JOIN;
+      return p;
     case TRI_OP_SWIGLU: {
       const Role r = sw_role(dt, key_I(k), fl, call_bytes(k) > kStreamBytes, 1);
       p.variant = r.variant;
