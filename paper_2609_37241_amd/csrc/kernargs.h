@@ -200,7 +200,8 @@ struct PagedArgs {
   int32_t splits;
   int32_t tiles;          // tiles of queries per K head
   int32_t window;
-  float scale;            // times log2 e: the weights are powers of two
+  float scale;            // |scale| log2 e, above 0: the weights are powers of two
+  uint32_t flip;          // 1: scale is negative, the queries change sign
   FastDiv div;            // by page
   FastDiv g_div;          // by g
 };
@@ -251,7 +252,7 @@ static_assert(sizeof(KvSlotsArgs) == 120 && __builtin_offsetof(KvSlotsArgs, div)
               "KvSlotsArgs layout");
 static_assert(sizeof(KvWriteArgs) == 152 && __builtin_offsetof(KvWriteArgs, row_items) == 148,
               "KvWriteArgs layout");
-static_assert(sizeof(PagedArgs) == 216 && __builtin_offsetof(PagedArgs, div) == 196,
+static_assert(sizeof(PagedArgs) == 216 && __builtin_offsetof(PagedArgs, div) == 200,
               "PagedArgs layout");
 static_assert(sizeof(ResidentBlock) == 320 && __builtin_offsetof(ResidentBlock, grid) == 288 &&
                   __builtin_offsetof(ResidentBlock, tag) == 292,

@@ -1,0 +1,775 @@
+// Attention over pages on the matrix cores (PA_ROWS, PA_TILE): rows of 16-byte
+// aligned heads of up to 256 elements, held in HDP of them (64, 128 or 256).
+//
+// Both forms compute the transposed products, S^T = K Q^T and O^T = V^T P^T: a
+// lane then holds scores of one query only, so the softmax needs no exchange
+// but the maximum over the lanes that share the query, and the scores are the
+// second product's operand where they lie. A matrix instruction sums over
+// keys in any order as long as both operands have the same one, so the keys
+// are taken in the order in which the first product leaves them:
+//   16x16 (S^T: lane l holds query l % 16, keys 4 (l / 16) + i, i < 4), and
+//   32x32 (query l % 32, keys 8 b + 4 (l / 32) + i, b < 4).
+// V is needed with the keys along a lane's elements: bf16 rows in LDS are read
+// by the transposing read (16 lanes exchange 4 rows of 16 elements), float32
+// ones element by element.
+//
+// The weights are 2^(c x - m) with x = q.k, c = |scale| log2 e > 0 (a negative
+// scale changes q's sign) and m the running maximum of c x, in one fused
+// operation: c x is not rounded by itself, and an error in m is common to all
+// of a row's weights. Sums and products accumulate in float32. In bf16 the
+// weights are rounded to bf16 (at most half a step, 2^-8, of each; the sum
+// they are divided by takes them unrounded): the matrix instruction takes both
+// operands in one type, and V's exponents do not fit float16.
+#pragma once
+#include "paged.h"
+
+namespace tri {
+namespace dev {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// 4 rows of 16 bf16 elements, row l / 4 read by lane l of 16 (4 elements
+// each): lane l gets element l of the four rows.
+__device__ inline u32x2 lds_transpose(const void *p) {
+  typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+  return __builtin_bit_cast(
+      u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)p));
+}
+
+// x or -x: with `flip` the sign bits of a vector's elements change, so that
+// the scale is positive and the largest product has the largest score.
+template <int DT>
+__device__ inline void flip_sign(u32x4 &v, uint32_t flip) {
+  const uint32_t bits = flip ? (DT == kF32 ? 0x80000000u : 0x80008000u) : 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] ^= bits;
+}
+
+// Over the lanes l, l ^ 16, l ^ 32, l ^ 48 (or l, l ^ 32), the same in all.
+__device__ inline float max_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float sum_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ inline float max_16_32(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return max_32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float sum_16_32(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return sum_32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// Clears the infinities and NaN of a vector; whether there were any.
+template <int DT>
+__device__ inline bool clear_not_finite(u32x4 &v) {
+  u32x4 keep;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT == kF32) {
+      keep[i] = (v[i] & 0x7F800000u) == 0x7F800000u ? 0u : ~0u;
+    } else {
+      keep[i] = ((v[i] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) |
+                ((v[i] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+    }
+  }
+  const bool bad = (keep[0] & keep[1] & keep[2] & keep[3]) != ~0u;
+  v &= keep;
+  return bad;
+}
+
+// V may hold infinities or NaN at a key that some rows of a tile see and others
+// must not (a later token of the same chunk, an earlier one than the window):
+// a product over all keys would make NaN of their weight of 0. So in the steps
+// whose keys the rows see differently such elements go to LDS as zeros, and
+// where there are any, the lanes whose query sees their key add them from
+// memory: v is the key's V, e the first of four elements, w the query's weight.
+template <int DT>
+__device__ inline void add_not_finite(const char *v, int32_t e, int32_t hd, float w, bool mine,
+                                      float *o) {
+  if (e >= hd) return;
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = Elt<DT>::ld(v, e + i);
+    if (mine && !(fabsf(y[i]) < __builtin_inff())) o[i] = fmaf(w, y[i], o[i]);
+  }
+}
+
+// The tile of queries that a workgroup computes: M rows of request r's n * g
+// rows of one K head (row i: token i / g, head i % g). Tiles are numbered
+// through the requests without knowing their lengths on the host: those of r
+// start at floor(q_start[r] g / M) + r, which leaves each request room for
+// ceil(n g / M) and the whole fewer than floor(T g / M) + R + 1.
+struct Tile {
+  int32_t r;        // request, -1: nothing to do
+  int32_t row0, rows;
+  Request rq;
+  int32_t p0, p1;   // positions of the first and the last row
+};
+
+template <int M>
+__device__ inline Tile find_tile(const PagedArgs &a, int32_t tile) {
+  const int lane = threadIdx.x & 63;
+  Tile t;
+  t.r = -1;
+  for (int32_t b = 0; b < a.R; b += 64) {
+    const int32_t x = b + lane;
+    const int64_t first =
+        x < a.R ? int64_t(clamp_i32(a.q_start[x], 0, a.T)) * a.g / M + x : int64_t(1) << 40;
+    t.r += __popcll(__ballot(first <= tile));
+  }
+  t.r = __builtin_amdgcn_readfirstlane(t.r);
+  if (t.r < 0) return t;
+  t.rq = request_of(a, t.r);
+  const int64_t all = int64_t(t.rq.q1 - t.rq.q0) * a.g;
+  const int64_t at = (tile - (int64_t(t.rq.q0) * a.g / M + t.r)) * M;
+  if (at < 0 || at >= all) {
+    t.r = -1;
+    return t;
+  }
+  t.row0 = int32_t(at);
+  t.rows = int32_t(all - at < M ? all - at : M);
+  const int32_t base = t.rq.kv - (t.rq.q1 - t.rq.q0);
+  t.p0 = base + int32_t(fast_div(uint32_t(t.row0), a.g_div));
+  t.p1 = base + int32_t(fast_div(uint32_t(t.row0 + t.rows - 1), a.g_div));
+  return t;
+}
+
+// Token (row of q and out) and query head of row i of a tile of K head kh.
+__device__ inline void row_of(const PagedArgs &a, const Tile &t, int32_t i, int32_t kh,
+                              int32_t *token, int32_t *head) {
+  const uint32_t x = uint32_t(t.row0 + i), tok = fast_div(x, a.g_div);
+  *token = t.rq.q0 + int32_t(tok);
+  *head = kh * a.g + int32_t(x - tok * uint32_t(a.g));
+}
+
+// Four neighbouring elements of the result (or of the partial sums).
+template <int DT>
+__device__ inline void store4(const PagedArgs &a, int32_t token, int32_t head, int32_t d,
+                              const float *v) {
+  char *o = static_cast<char *>(a.out) +
+            (int64_t(token) * a.o_ts + int64_t(head) * a.hd + d) * Elt<DT>::ES;
+  if constexpr (DT == kF32)
+    *reinterpret_cast<u32x4 *>(o) = Elt<kF32>::pack(v);
+  else
+    *reinterpret_cast<u32x2 *>(o) =
+        u32x2{Elt<kBF16>::pack2(v[0], v[1]), Elt<kBF16>::pack2(v[2], v[3])};
+}
+
+// ---- PA_ROWS ------------------------------------------------------------------------------------
+// Few rows per request (decode): a tile is 16 rows, and the four wavefronts
+// share out its keys, KB at a time each with its own softmax, joined in LDS at
+// the end. HBM-bound: K goes from memory into the registers of the first
+// product, V through the wavefront's own part of LDS (no barrier) into the
+// second's, and both loads of the next keys are in flight while these are
+// computed; the pages of the keys after those are looked up meanwhile.
+template <int DT, int HDP>
+struct RowsShape {
+  static constexpr int ES = Elt<DT>::ES;
+  static constexpr int KB = DT == kF32 ? 16 : 32;         // keys of a step
+  static constexpr int MB = KB / 16;
+  static constexpr int NS = HDP * ES / 64;                // 16-byte vectors of a lane and key
+  // bytes of a row of V in LDS: 16 rows of the transposing read (of a column
+  // of float32) fall on different banks
+  static constexpr int VS = HDP * ES + (DT == kF32 ? 16 : 32);
+  static constexpr int ND = HDP / 16;
+  static constexpr int OS = HDP + 4;                      // floats of a row of O in LDS
+  static constexpr int WAVE_LDS = KB * VS > 16 * OS * 4 ? KB * VS : 16 * OS * 4;
+};
+
+template <int DT, int HDP>
+__device__ void body_pa_rows(const PagedArgs &a) {
+  typedef RowsShape<DT, HDP> S;
+  constexpr int ES = S::ES, KB = S::KB, MB = S::MB, NS = S::NS, ND = S::ND;
+  __shared__ __attribute__((aligned(16))) char lds[4 * S::WAVE_LDS];
+  __shared__ float wave_m[4][16], wave_l[4][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n = lane & 15, quarter = lane >> 4;
+  const uint32_t kh = blockIdx.x % uint32_t(a.nk), rest = blockIdx.x / uint32_t(a.nk);
+  const int32_t split = int32_t(rest % uint32_t(a.splits));
+  const Tile t = find_tile<16>(a, int32_t(rest / uint32_t(a.splits)));
+  if (t.r < 0) return;
+  const int32_t lo = t.p0 < 0 ? 0 : first_key(t.p0, a.window), hi = t.p1 + 1;
+  int32_t b, e;
+  split_keys(lo, hi, a.splits, split, &b, &e);
+  // what the lane's query sees; rows behind the tile's last do as that one
+  int32_t token, head;
+  row_of(a, t, n < t.rows ? n : t.rows - 1, int32_t(kh), &token, &head);
+  const int32_t my_p = t.rq.kv - (t.rq.q1 - token);
+  const int32_t my_lo = my_p < 0 ? 0 : first_key(my_p, a.window), my_hi = my_p + 1;
+  // keys that all rows see
+  const int32_t all_lo = t.p1 < 0 ? 0 : first_key(t.p1, a.window), all_hi = t.p0 + 1;
+
+  const int hdb = a.hd * ES;
+  u32x4 q[NS];
+  {
+    const char *p = static_cast<const char *>(a.q) +
+                    (int64_t(token) * a.q_ts + int64_t(head) * a.hd) * ES + quarter * 16;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      q[s] = u32x4{0, 0, 0, 0};
+      if (quarter * 16 + 64 * s < hdb) q[s] = *reinterpret_cast<const u32x4 *>(p + 64 * s);
+      flip_sign<DT>(q[s], a.flip);
+    }
+  }
+  const int32_t *table = a.table + int64_t(t.r) * a.table_rs;
+  const char *kp = static_cast<const char *>(a.k.p) + int64_t(kh) * a.k.hs * ES;
+  const char *vp = static_cast<const char *>(a.v.p) + int64_t(kh) * a.v.hs * ES;
+  char *vl = lds + wave * S::WAVE_LDS;
+
+  f32x4 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) o[i] = f32x4{0, 0, 0, 0};
+  float m = kNegInf, l = 0.0f;
+
+  // the page of key k0 + 16 j + n (0 beyond the end: a page of the pool)
+  int32_t page[MB];
+  const auto look_up = [&](int32_t k0) {
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+      const int32_t key = k0 + 16 * j + n;
+      page[j] = table[fast_div(uint32_t(key < e ? key : e - 1), a.div)];
+    }
+  };
+  // rows of K and V of those keys, and which of them are there
+  const char *kr[MB], *vr[MB];
+  bool there[MB];
+  const auto rows_of = [&](int32_t k0) {
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+      const int32_t key = k0 + 16 * j + n;
+      const uint32_t k1 = uint32_t(key < e ? key : e - 1);
+      there[j] = key < e && uint32_t(page[j]) < uint32_t(a.n_pages);
+      const int64_t id = there[j] ? page[j] : 0;
+      const int64_t in = k1 - fast_div(k1, a.div) * uint32_t(a.page);
+      kr[j] = kp + (id * a.k.ps + in * a.k.ss) * ES + quarter * 16;
+      vr[j] = vp + (id * a.v.ps + in * a.v.ss) * ES + quarter * 16;
+    }
+  };
+  u32x4 k[MB][NS], v[MB][NS];
+  const auto load = [&](u32x4(&x)[MB][NS], const char *const(&r)[MB]) {
+#pragma unroll
+    for (int j = 0; j < MB; ++j)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        // a head shorter than HDP ends inside: its rest is zero
+        x[j][s] = u32x4{0, 0, 0, 0};
+        if (quarter * 16 + 64 * s < hdb) x[j][s] = *reinterpret_cast<const u32x4 *>(r[j] + 64 * s);
+      }
+  };
+
+  const auto sees = [&](int32_t key) { return key >= my_lo && key < my_hi; };
+  int32_t k0 = b + wave * KB;
+  if (k0 < e) {
+    look_up(k0);
+    rows_of(k0);
+    load(k, kr);
+    load(v, vr);
+    if (k0 + 4 * KB < e) look_up(k0 + 4 * KB);
+  }
+  for (; k0 < e; k0 += 4 * KB) {
+    const bool more = k0 + 4 * KB < e;
+    // S^T
+    f32x4 st[MB];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+      st[j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        if constexpr (DT == kF32) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            st[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[j][s][i]),
+                                                         __uint_as_float(q[s][i]), st[j], 0, 0, 0);
+        } else {
+          st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[j][s]),
+                                                          __builtin_bit_cast(bf16x8, q[s]), st[j],
+                                                          0, 0, 0);
+        }
+      }
+    }
+    // V to LDS; rows that are not there are zero, so that no weight of 0 meets
+    // a NaN
+    uint32_t seen = 0;   // bit i: key k0 + i is there
+#pragma unroll
+    for (int j = 0; j < MB; ++j) seen |= uint32_t(__ballot(there[j]) & 0xFFFF) << (16 * j);
+    const int32_t k1 = k0 + KB < e ? k0 + KB : e;
+    const bool mixed = k0 < all_lo || k1 > all_hi;   // some row sees not all of them
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < MB; ++j)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        if (!there[j]) v[j][s] = u32x4{0, 0, 0, 0};
+        if (mixed) odd |= clear_not_finite<DT>(v[j][s]);
+        *reinterpret_cast<u32x4 *>(vl + (16 * j + n) * S::VS + quarter * 16 + 64 * s) = v[j][s];
+      }
+    if (more) {
+      rows_of(k0 + 4 * KB);
+      load(k, kr);
+      load(v, vr);
+      if (k0 + 8 * KB < e) look_up(k0 + 8 * KB);
+    }
+    // softmax: the lane's keys are k0 + 16 j + 4 quarter + i
+    const bool partial = mixed || seen != (KB == 32 ? 0xFFFFFFFFu : 0xFFFFu);
+    float top = kNegInf;
+#pragma unroll
+    for (int j = 0; j < MB; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (partial) {
+          const int32_t x = 16 * j + 4 * quarter + i;
+          if (!((seen >> x) & 1) || !sees(k0 + x)) st[j][i] = kNegInf;
+        }
+        top = fmaxf(top, st[j][i]);
+      }
+    top = max_16_32(top);
+    const float mn = fmaxf(m, top == kNegInf ? kNegInf : top * a.scale);
+    const float ms = mn == kNegInf ? 0.0f : mn;
+    const float alpha = exp2_hw(m - ms);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int j = 0; j < MB; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        st[j][i] = exp2_hw(fmaf(st[j][i], a.scale, -ms));
+        l += st[j][i];
+      }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] *= alpha;
+    if (mixed && __ballot(odd)) {
+#pragma unroll 1
+      for (int x = 0; x < KB; ++x) {
+        if (!((seen >> x) & 1)) continue;
+        // lane n + 16 (x / 4 % 4) has the query's weight of key x
+        float w = 0.0f;
+#pragma unroll
+        for (int j = 0; j < MB; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (x / 16 == j && x % 4 == i) w = st[j][i];
+        w = __shfl(Elt<DT>::round(w), n + 16 * ((x / 4) % 4));
+        const char *y = vp + slot_offset(table, uint32_t(k0 + x), a, a.v) * ES;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
+          add_not_finite<DT>(y, 16 * d + 4 * quarter, a.hd, w, sees(k0 + x), z);
+          o[d] = f32x4{z[0], z[1], z[2], z[3]};
+        }
+      }
+    }
+    u32x4 p = {0, 0, 0, 0};
+    if constexpr (DT == kBF16) {
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        p[2 * j] = Elt<kBF16>::pack2(st[j][0], st[j][1]);
+        p[2 * j + 1] = Elt<kBF16>::pack2(st[j][2], st[j][3]);
+      }
+    }
+    // O^T
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      if constexpr (DT == kF32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float y =
+              *reinterpret_cast<const float *>(vl + (4 * quarter + i) * S::VS + (16 * d + n) * 4);
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(y, st[0][i], o[d], 0, 0, 0);
+        }
+      } else {
+        const char *x = vl + (4 * quarter + (n >> 2)) * S::VS + (16 * d + 4 * (n & 3)) * 2;
+        const u32x2 y0 = lds_transpose(x), y1 = lds_transpose(x + 16 * S::VS);
+        const u32x4 y = {y0[0], y0[1], y1[0], y1[1]};
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y),
+                                                       __builtin_bit_cast(bf16x8, p), o[d], 0, 0, 0);
+      }
+    }
+  }
+
+  // join the wavefronts
+  l = sum_16_32(l);
+  if (quarter == 0) {
+    wave_m[wave][n] = m;
+    wave_l[wave][n] = l;
+  }
+  float *ol = reinterpret_cast<float *>(vl);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+    *reinterpret_cast<f32x4 *>(ol + n * S::OS + 16 * d + 4 * quarter) = o[d];
+  __syncthreads();
+  const int row = threadIdx.x >> 4, part = threadIdx.x & 15;
+  if (row >= t.rows) return;
+  float top = kNegInf;
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    if (wave_l[w][row] != 0.0f) top = fmaxf(top, wave_m[w][row]);
+  const float ts = top == kNegInf ? 0.0f : top;
+  float f[4], sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = 0.0f;
+    if (wave_l[w][row] != 0.0f) {
+      f[w] = exp2_hw(wave_m[w][row] - ts);
+      sum += f[w] * wave_l[w][row];
+    }
+  }
+  row_of(a, t, row, int32_t(kh), &token, &head);
+  const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int c = 0; c < HDP / 64; ++c) {
+    const int d = 64 * c + 4 * part;
+    if (d >= a.hd) break;
+    f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (wave_l[w][row] == 0.0f) continue;
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(
+          reinterpret_cast<const float *>(lds + w * S::WAVE_LDS) + row * S::OS + d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], x[i], acc[i]);
+    }
+    if (a.splits > 1) {
+      *reinterpret_cast<f32x4 *>(a.part + at * a.hd + d) = acc;
+    } else {
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = acc[i] * inv;
+      store4<DT>(a, token, head, d, y);
+    }
+  }
+  if (a.splits > 1 && part == 0) {
+    a.ml[2 * at] = top;
+    a.ml[2 * at + 1] = sum;
+  }
+}
+
+// ---- PA_TILE ------------------------------------------------------------------------------------
+// Many rows per request (chunks of a prompt): a tile is 128 rows, 32 of them a
+// wavefront's, against KB keys at a time whose K and V the workgroup stages in
+// LDS. MFMA-bound in principle; the 32 exponentials a lane takes per 32 matrix
+// instructions and the 32 KiB of LDS that a wavefront reads for them each cost
+// about as much, so two workgroups a compute unit fill each other's gaps. The
+// next keys' loads are in flight during the products, and go to the other half
+// of LDS between them (one barrier a step).
+//
+// The running maximum is the softmax's reference only; it is raised, and what
+// was summed rescaled, when a score passes it by more than 2^8 (a branch that
+// the first step takes and few others): weights up to 256 lose nothing in
+// float32 or bf16.
+template <int DT, int HDP>
+struct TileShape {
+  static constexpr int ES = Elt<DT>::ES;
+  static constexpr int KB = DT == kF32 || HDP > 128 ? 32 : 64;
+  static constexpr int NB = KB / 32;
+  static constexpr int NQ = HDP * ES / 32;                // 16-byte vectors of a lane's query
+  static constexpr int ND = HDP / 32;
+  // bytes of a row in LDS. K: 8 rows of 16 bytes on different banks. V: the
+  // transposing read's 4 rows of 64 bytes, or (float32) 32 elements of rows 4
+  // apart
+  static constexpr int KS = HDP * ES + 16;
+  static constexpr int VS = HDP * ES + (DT == kF32 ? 32 : 64);
+  static constexpr int BUF = KB * (KS + VS);
+  static constexpr int NBUF = BUF <= 40 * 1024 ? 2 : 1;
+  static constexpr int CH = HDP * ES / 16;                // vectors of a row
+  static constexpr int RP = 256 / CH;                     // rows that a pass stages
+  static constexpr int NP = KB / RP;
+};
+
+template <int DT, int HDP>
+__device__ void body_pa_tile(const PagedArgs &a) {
+  typedef TileShape<DT, HDP> S;
+  constexpr int ES = S::ES, KB = S::KB, NB = S::NB, NQ = S::NQ, ND = S::ND, NP = S::NP;
+  __shared__ __attribute__((aligned(16))) char lds[S::NBUF * S::BUF];
+  __shared__ int32_t odd_at[2];   // 1 + first key of a step whose V has infinities or NaN
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = lane & 31, half = lane >> 5;
+  const uint32_t kh = blockIdx.x % uint32_t(a.nk), rest = blockIdx.x / uint32_t(a.nk);
+  const int32_t split = int32_t(rest % uint32_t(a.splits));
+  // the last tiles, which see the most keys, first
+  const Tile t = find_tile<128>(a, a.tiles - 1 - int32_t(rest / uint32_t(a.splits)));
+  if (t.r < 0) return;
+  if (tid < 2) odd_at[tid] = 0;
+  const int32_t lo = t.p0 < 0 ? 0 : first_key(t.p0, a.window), hi = t.p1 + 1;
+  int32_t b, e;
+  split_keys(lo, hi, a.splits, split, &b, &e);
+  const int32_t all_lo = t.p1 < 0 ? 0 : first_key(t.p1, a.window), all_hi = t.p0 + 1;
+  // the lane's row (behind the last: as the last) and what it sees; what all
+  // rows, and any row, of the wavefront see
+  const int32_t row = 32 * wave + n;
+  int32_t token, head;
+  row_of(a, t, row < t.rows ? row : t.rows - 1, int32_t(kh), &token, &head);
+  const int32_t base = t.rq.kv - t.rq.q1;
+  const int32_t my_p = base + token;
+  const int32_t my_lo = my_p < 0 ? 0 : first_key(my_p, a.window), my_hi = my_p + 1;
+  const int32_t w0 = __builtin_amdgcn_readlane(my_p, 0), w1 = __builtin_amdgcn_readlane(my_p, 31);
+  const int32_t w_lo = w0 < 0 ? 0 : first_key(w0, a.window), w_hi = w1 + 1;
+  const int32_t w_all_lo = w1 < 0 ? 0 : first_key(w1, a.window), w_all_hi = w0 + 1;
+  const bool idle = 32 * wave >= t.rows;
+  const auto sees = [&](int32_t key) { return key >= my_lo && key < my_hi; };
+
+  const int hdb = a.hd * ES;
+  u32x4 q[NQ];
+  {
+    const char *p = static_cast<const char *>(a.q) +
+                    (int64_t(token) * a.q_ts + int64_t(head) * a.hd) * ES + half * 16;
+#pragma unroll
+    for (int s = 0; s < NQ; ++s) {
+      q[s] = u32x4{0, 0, 0, 0};
+      if (half * 16 + 32 * s < hdb) q[s] = *reinterpret_cast<const u32x4 *>(p + 32 * s);
+      flip_sign<DT>(q[s], a.flip);
+    }
+  }
+  const int32_t *table = a.table + int64_t(t.r) * a.table_rs;
+  const char *kp = static_cast<const char *>(a.k.p) + int64_t(kh) * a.k.hs * ES;
+  const char *vp = static_cast<const char *>(a.v.p) + int64_t(kh) * a.v.hs * ES;
+
+  f32x16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+  float m = kNegInf, l = 0.0f;
+
+  // staging: this work-item's vector of rows srow + RP i
+  const int srow = tid / S::CH, sbyte = (tid % S::CH) * 16;
+  const bool inside = sbyte < hdb;
+  // the page of key k0 + lane % KB (beyond the end: the last key's)
+  const auto look_up = [&](int32_t k0) {
+    const int32_t key = k0 + (lane & (KB - 1));
+    return table[fast_div(uint32_t(key < e ? key : e - 1), a.div)];
+  };
+  u32x4 sk[NP], sv[NP];
+  uint64_t seen = 0;     // bit i: key k0 + i of the staged step is there
+  const auto load = [&](int32_t k0, int32_t page) {
+    seen = __ballot(k0 + (lane & (KB - 1)) < e && uint32_t(page) < uint32_t(a.n_pages));
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int r = srow + S::RP * i;
+      const int32_t pid = __shfl(page, r);
+      const uint32_t key = uint32_t(k0 + r < e ? k0 + r : e - 1);
+      const int64_t id = (seen >> r) & 1 ? pid : 0;
+      const int64_t in = key - fast_div(key, a.div) * uint32_t(a.page);
+      sk[i] = u32x4{0, 0, 0, 0};
+      sv[i] = u32x4{0, 0, 0, 0};
+      if (inside) {
+        sk[i] = *reinterpret_cast<const u32x4 *>(kp + (id * a.k.ps + in * a.k.ss) * ES + sbyte);
+        sv[i] = *reinterpret_cast<const u32x4 *>(vp + (id * a.v.ps + in * a.v.ss) * ES + sbyte);
+      }
+    }
+  };
+  // rows of V that are not there are zero, so that no weight of 0 meets a NaN
+  const auto store = [&](int32_t k0, int buf) {
+    char *kl = lds + buf * S::BUF, *vl = kl + KB * S::KS;
+    const int32_t k1 = k0 + KB < e ? k0 + KB : e;
+    const bool mixed = k0 < all_lo || k1 > all_hi;
+    const bool some = seen != ~uint64_t(0);   // (32 keys: their bits twice)
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int r = srow + S::RP * i;
+      if (some && !((seen >> r) & 1)) sv[i] = u32x4{0, 0, 0, 0};
+      if (mixed) odd |= clear_not_finite<DT>(sv[i]);
+      *reinterpret_cast<u32x4 *>(kl + r * S::KS + sbyte) = sk[i];
+      *reinterpret_cast<u32x4 *>(vl + r * S::VS + sbyte) = sv[i];
+    }
+    if (mixed && odd) odd_at[buf] = k0 + 1;
+  };
+
+  uint64_t there = 0;    // `seen` of the step being computed
+  int32_t page = 0;
+  if (b < e) {
+    load(b, look_up(b));
+    __syncthreads();     // odd_at is clear
+    store(b, 0);
+    there = seen;
+    if (b + KB < e) {
+      page = look_up(b + KB);
+      load(b + KB, page);
+      if (b + 2 * KB < e) page = look_up(b + 2 * KB);
+    }
+    __syncthreads();
+  }
+  int buf = 0;
+  for (int32_t k0 = b; k0 < e; k0 += KB) {
+    const char *kl = lds + buf * S::BUF, *vl = kl + KB * S::KS;
+    const bool work = !idle && k0 < w_hi && k0 + KB > w_lo;
+    f32x16 st[NB];
+    if (work) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[j][i] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < NQ; ++s) {
+          const u32x4 k = *reinterpret_cast<const u32x4 *>(kl + (32 * j + n) * S::KS + half * 16 +
+                                                           32 * s);
+          if constexpr (DT == kF32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              st[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[i]),
+                                                           __uint_as_float(q[s][i]), st[j], 0, 0, 0);
+          } else {
+            st[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
+                                                            __builtin_bit_cast(bf16x8, q[s]), st[j],
+                                                            0, 0, 0);
+          }
+        }
+      }
+    }
+    const uint64_t now = there;
+    if constexpr (S::NBUF == 2) {
+      if (k0 + KB < e) {
+        store(k0 + KB, buf ^ 1);
+        there = seen;
+        if (k0 + 2 * KB < e) {
+          load(k0 + 2 * KB, page);
+          if (k0 + 3 * KB < e) page = look_up(k0 + 3 * KB);
+        }
+      }
+    }
+    if (work) {
+      // the lane's keys are k0 + 32 j + 8 (i / 4) + 4 half + i % 4
+      const int32_t k1 = k0 + KB < e ? k0 + KB : e;
+      const bool mixed = k0 < w_all_lo || k1 > w_all_hi;
+      if (mixed || now != ~uint64_t(0)) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int32_t x = 32 * j + 8 * (i / 4) + 4 * half + i % 4;
+            if (!((now >> x) & 1) || !sees(k0 + x)) st[j][i] = kNegInf;
+          }
+      }
+      float top = kNegInf;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, st[j][i]);
+      top = max_32(top);
+      top = top == kNegInf ? kNegInf : top * a.scale;
+      if (__ballot(top > m + 8.0f)) {
+        const float mn = fmaxf(m, top);
+        const float alpha = exp2_hw(m - (mn == kNegInf ? 0.0f : mn));
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= alpha;
+      }
+      const float ms = m == kNegInf ? 0.0f : m;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          st[j][i] = exp2_hw(fmaf(st[j][i], a.scale, -ms));
+          l += st[j][i];
+        }
+      if (odd_at[buf] == k0 + 1) {
+#pragma unroll 1
+        for (int x = 0; x < KB; ++x) {
+          if (!((now >> x) & 1)) continue;
+          // lane n + 32 (x / 4 % 2) has the query's weight of key x
+          float w = 0.0f;
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (x / 32 == j && (x % 32) / 8 == i / 4 && x % 4 == i % 4) w = st[j][i];
+          w = __shfl(Elt<DT>::round(w), n + 32 * ((x / 4) % 2));
+          const char *y = vp + slot_offset(table, uint32_t(k0 + x), a, a.v) * ES;
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float z[4];
+#pragma unroll
+              for (int c = 0; c < 4; ++c) z[c] = o[d][4 * i + c];
+              add_not_finite<DT>(y, 32 * d + 8 * i + 4 * half, a.hd, w, sees(k0 + x), z);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) o[d][4 * i + c] = z[c];
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+      }
+      if constexpr (DT == kF32) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            const float y = *reinterpret_cast<const float *>(
+                vl + (8 * (i / 4) + 4 * half + i % 4) * S::VS + (32 * d + n) * 4);
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(y, st[0][i], o[d], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int s = 0; s < KB / 16; ++s) {
+          // keys 16 s + 4 half + (0..3 and 8..11)
+          u32x4 p;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            p[i] = Elt<kBF16>::pack2(st[s / 2][8 * (s % 2) + 2 * i], st[s / 2][8 * (s % 2) + 2 * i + 1]);
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            const char *x = vl + (16 * s + 4 * half + ((lane & 15) >> 2)) * S::VS +
+                            (32 * d + (lane & 16) + 4 * (lane & 3)) * 2;
+            const u32x2 y0 = lds_transpose(x), y1 = lds_transpose(x + 8 * S::VS);
+            const u32x4 y = {y0[0], y0[1], y1[0], y1[1]};
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y),
+                                                           __builtin_bit_cast(bf16x8, p), o[d], 0, 0,
+                                                           0);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    if constexpr (S::NBUF == 2) {
+      buf ^= 1;
+    } else if (k0 + KB < e) {
+      store(k0 + KB, 0);
+      there = seen;
+      if (k0 + 2 * KB < e) {
+        load(k0 + 2 * KB, page);
+        if (k0 + 3 * KB < e) page = look_up(k0 + 3 * KB);
+      }
+      __syncthreads();
+    }
+  }
+
+  if (row >= t.rows) return;
+  l = sum_32(l);
+  const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e0 = 32 * d + 8 * i + 4 * half;
+      if (e0 >= a.hd) continue;
+      float y[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) y[x] = a.splits > 1 ? o[d][4 * i + x] : o[d][4 * i + x] * inv;
+      if (a.splits > 1)
+        *reinterpret_cast<u32x4 *>(a.part + at * a.hd + e0) = Elt<kF32>::pack(y);
+      else
+        store4<DT>(a, token, head, e0, y);
+    }
+  if (a.splits > 1 && half == 0) {
+    a.ml[2 * at] = m;
+    a.ml[2 * at + 1] = l;
+  }
+}
+
+}  // namespace dev
+}  // namespace tri

@@ -1,0 +1,35 @@
+// Attention over pages on the matrix cores, float32.
+#include "../internal.h"
+#include "attn.h"
+
+namespace tri {
+using namespace dev;
+
+template <int HDP>
+__global__ __launch_bounds__(256, HDP == 256 ? 1 : 2) void k_pa_rows_f32(PagedArgs a) {
+  body_pa_rows<kF32, HDP>(a);
+}
+
+template <int HDP>
+__global__ __launch_bounds__(256, HDP == 256 ? 1 : 2) void k_pa_tile_f32(PagedArgs a) {
+  body_pa_tile<kF32, HDP>(a);
+}
+
+// hdp: the head size rounded up to 64, 128 or 256.
+const void *attn_kernel_f32(int32_t variant, int32_t hdp) {
+  const void *rows[3] = {reinterpret_cast<const void *>(&k_pa_rows_f32<64>),
+                         reinterpret_cast<const void *>(&k_pa_rows_f32<128>),
+                         reinterpret_cast<const void *>(&k_pa_rows_f32<256>)};
+  const void *tile[3] = {reinterpret_cast<const void *>(&k_pa_tile_f32<64>),
+                         reinterpret_cast<const void *>(&k_pa_tile_f32<128>),
+                         reinterpret_cast<const void *>(&k_pa_tile_f32<256>)};
+  if (hdp != 64 && hdp != 128 && hdp != 256) return nullptr;
+  const int i = hdp == 64 ? 0 : hdp == 128 ? 1 : 2;
+  switch (variant) {
+    case PA_ROWS: return rows[i];
+    case PA_TILE: return tile[i];
+    default: return nullptr;
+  }
+}
+
+}  // namespace tri

@@ -242,15 +242,16 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
       if (ko >= 0) {
         float dot = 0.0f;
         for (int d = 0; d < a.hd; ++d) dot = fmaf(qs[wave][d], Elt<DT>::ld(kp + ko * ES, d), dot);
-        sc = dot * a.scale;
+        sc = a.flip ? -dot : dot;
       }
       const uint64_t seen = __ballot(ko >= 0);
       float top = sc;
 #pragma unroll
       for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-      const float mn = fmaxf(m, top), ms = mn == kNegInf ? 0.0f : mn;
+      const float mn = fmaxf(m, top == kNegInf ? kNegInf : top * a.scale);
+      const float ms = mn == kNegInf ? 0.0f : mn;
       const float alpha = exp2_hw(m - ms);
-      const float w = ko >= 0 ? exp2_hw(sc - ms) : 0.0f;
+      const float w = ko >= 0 ? exp2_hw(fmaf(sc, a.scale, -ms)) : 0.0f;
       float sum = w;
 #pragma unroll
       for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
@@ -332,9 +333,14 @@ const void *sym(F *f) {
 }
 }  // namespace
 
-const void *paged_kernel(int32_t variant, uint32_t dtype, int32_t) {
+const void *attn_kernel_bf16(int32_t variant, int32_t hdp);
+const void *attn_kernel_f32(int32_t variant, int32_t hdp);
+
+const void *paged_kernel(int32_t variant, uint32_t dtype, int32_t sub) {
   const bool f32 = dtype == TRI_F32;
   switch (variant) {
+    case PA_ROWS:
+    case PA_TILE: return f32 ? attn_kernel_f32(variant, sub) : attn_kernel_bf16(variant, sub);
     case KV_SLOTS: return sym(&k_kv_slots);
     case KVW_ANY: return f32 ? sym(&k_kv_write<kF32, false>) : sym(&k_kv_write<kBF16, false>);
     case KVW_VEC: return f32 ? sym(&k_kv_write<kF32, true>) : sym(&k_kv_write<kBF16, true>);

@@ -231,14 +231,18 @@ tri_status tri_paged_attention(tri_cache *c, const tri_attention_args *p, void *
   k.k3 = (uint64_t(plan.form) << 16) | (uint64_t(plan.splits > 1) << 24);
   float *part = static_cast<float *>(a.workspace);
   const int32_t g = a.nq / a.kv.nk;
-  // log2 e: the weights are 2^(scale log2 e q.k - maximum)
+  // the weights are 2^(c q.k - maximum), c = |scale| log2 e; for 0 a c so small
+  // that all weights are 1 (a masked score stays -inf)
+  float c2 = float(fabs(double(a.scale)) * 1.4426950408889634);
+  if (!(c2 >= 1e-36f)) c2 = 1e-36f;
+  if (!(c2 <= 3e38f)) c2 = 3e38f;
   const PagedArgs args{a.q, a.out, {a.kv.k, a.kv.k_ps, a.kv.k_ss, a.kv.k_hs},
                        {a.kv.v, a.kv.v_ps, a.kv.v_ss, a.kv.v_hs}, a.table, a.kv_len, a.q_start,
                        plan.splits > 1 ? part : nullptr,
                        plan.splits > 1 ? part + a.T * a.nq * plan.splits * a.kv.hd : nullptr,
                        a.q_ts, a.o_ts, a.table_rs, int32_t(a.T), a.R, a.cols, a.kv.n_pages,
                        a.kv.page, a.nq, a.kv.nk, a.kv.hd, g, plan.splits, plan.tiles, a.window,
-                       float(double(a.scale) * 1.4426950408889634), fast_div_of(uint32_t(a.kv.page)),
+                       c2, a.scale < 0.0f, fast_div_of(uint32_t(a.kv.page)),
                        fast_div_of(uint32_t(g))};
   return run_paged(c, op, k, a.T, plan.grid, plan.splits > 1 ? 2 : 1, &args, sizeof args, stream);
 }

@@ -229,18 +229,33 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
 
 AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                    bool aligned, int64_t kv_max, uint64_t workspace) {
-  (void)dtype, (void)R, (void)nk, (void)aligned;
   AttnPlan p{};
   p.form = kAttnAny;
-  p.splits = 1;
-  const int64_t rows = T * nq;
-  // 2048 wavefronts, runs of at least 256 keys
-  const int64_t want = cdiv(2048, rows), most = cdiv(kv_max, 256);
-  int64_t s = want < most ? want : most;
+  const int64_t rows = T * nq, g = nq / nk;
+  // workgroups (PA_ANY: of four wavefronts) before any split, those wanted,
+  // and the fewest keys a split is worth
+  int64_t have = cdiv(rows, 4), want = 512, run = 256;
+  int64_t tiles = 0;
+  if (aligned && hd % vec_elems(dtype) == 0 && hd <= kAttnMatrixHd) {
+    // rows of a request and K head, were the requests equal
+    p.form = cdiv(T, R) * g <= 16 ? kAttnRows : kAttnTile;
+    const int64_t m = p.form == kAttnRows ? 16 : 128;
+    tiles = T * g / m + R;
+    // a request has at least a tile, and no more requests than rows have any
+    const int64_t full = cdiv(T * g, m);
+    have = (full > (R < T ? R : T) ? full : (R < T ? R : T)) * nk;
+    want = p.form == kAttnRows ? 1024 : 512;
+    run = p.form == kAttnRows ? 256 : 512;
+  }
+  int64_t s = cdiv(want, have);
+  const int64_t most = cdiv(kv_max, run);
+  if (s > most) s = most;
   if (s > TRI_MAX_KV_SPLITS) s = TRI_MAX_KV_SPLITS;
   while (s > 1 && attn_workspace(T, nq, hd, int32_t(s)) > workspace) --s;
   p.splits = s < 1 ? 1 : int32_t(s);
-  p.grid[0] = clamp_grid(cdiv(rows * p.splits, 4));
+  p.tiles = int32_t(tiles);
+  p.grid[0] = p.form == kAttnAny ? clamp_grid(cdiv(rows * p.splits, 4))
+                                 : uint32_t(tiles * nk * p.splits);
   p.grid[1] = clamp_grid(cdiv(rows, 4));
   return p;
 }
@@ -305,7 +320,9 @@ static bool paged_key_valid(const Key &k) {
   const uint32_t form = key_attn_form(k);
   if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
   if (k.k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
-  return form == kAttnAny;
+  const bool matrix = (key_flags(k) & kAlign) && int32_t(hd) <= kAttnMatrixHd &&
+                      hd % uint32_t(vec_elems(key_dtype(k))) == 0;
+  return matrix ? form == kAttnRows || form == kAttnTile : form == kAttnAny;
 }
 
 // A key the entry points could have produced (used to check imported keys):
@@ -416,7 +433,10 @@ Plan plan_for_key(const Key &k) {
       p.n_launches = 1;
       return p;
     case TRI_OP_PAGED_ATTENTION:
-      p.variant = p.kvariant[0] = PA_ANY;
+      p.variant = p.kvariant[0] = key_attn_form(k) == kAttnRows   ? PA_ROWS
+                                  : key_attn_form(k) == kAttnTile ? PA_TILE
+                                                                  : PA_ANY;
+      if (p.variant != PA_ANY) p.ksub[0] = attn_hdp(int32_t(key_hd(k)));
       p.n_launches = 1;
       if (key_attn_split(k)) p.kvariant[p.n_launches++] = PA_JOIN;
       return p;
