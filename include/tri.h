@@ -43,7 +43,7 @@
  * - dtype: weights share the activations' dtype. Arithmetic is float32 with
  *   one rounding to the output dtype.
  * - T == 0 is a valid no-op: TRI_OK, nothing launched, no other argument
- *   inspected.
+ *   inspected (tri_kv_slots aside).
  * - Validation happens before any launch; a failed check returns a negative
  *   status and leaves the cache unchanged except its counters.
  * - One thread per cache. A cache is bound to the device current when it is
@@ -549,7 +549,8 @@ tri_status tri_embedding(tri_cache *cache, tri_dtype dtype, const void *table, i
  * The outputs must not overlap each other or an input (kv_len, free_count and
  * free_pages are read while they are written); the table row stride is at
  * least cols. cols * page must be below 2^31, page 1..TRI_MAX_PAGE. All
- * pointers 4-byte aligned, slots 8. */
+ * pointers 4-byte aligned, slots 8. T may be 0 (slots and pos are then not
+ * used): lengths and pages are done all the same. */
 tri_status tri_kv_slots(tri_cache *cache, const tri_kv_slots_args *args, void *stream);
 
 /* Store k, v [T, nk, hd] (heads packed) into their slots:

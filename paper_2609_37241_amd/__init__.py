@@ -52,7 +52,7 @@ class _PythonForm:
         return None
 
     rmsnorm = residual_rmsnorm = swiglu = silu = add = masked_fill = embedding = _decline
-    rope = chain = layers = close = _decline
+    rope = chain = layers = close = kv_slots = kv_write = paged_attention = _decline
 
 
 def _native_calls():
@@ -639,6 +639,11 @@ class SpecCache:
         (int64 [T], -1 without a page and past the last request), pos (int32 [T]), q_start
         (int32 [R + 1]), kv_len_out (int32 [R]) and free_out (int32 [2]: pages left, pages
         missing; the next step's free_count)."""
+        if self._rec is None:
+            r = self._fast.kv_slots(self, kv_len, new_len, block_table, free_pages, free_count,
+                                    page, T, slots, pos, q_start, kv_len_out, free_out, stream)
+            if r is not None:
+                return r
         dev = self._dev
         R, cols, rs = _table(block_table, "block_table", dev)
         T = int(T)
@@ -664,6 +669,10 @@ class SpecCache:
         """Store k and v [T, nk, hd] in the slots (int64 [T]) of a paged cache
         [n_pages, page, nk, hd] (any strides with contiguous heads); slots
         out of range are skipped (tri_kv_write)."""
+        if self._rec is None:
+            r = self._fast.kv_write(self, k, v, slots, k_cache, v_cache, stream)
+            if r is not None:
+                return r
         dev = self._dev
         T, nk, hd = _dims(k, "k", 3, dev)
         _like(v, "v", k.shape, k.dtype, dev)
@@ -686,6 +695,11 @@ class SpecCache:
         kv_len that the host knows (0: the table's width), steers how the
         work is split. Rows of no request keep what `out` held (an output made
         here is not initialised)."""
+        if self._rec is None:
+            r = self._fast.paged_attention(self, q, k_cache, v_cache, block_table, kv_len, q_start,
+                                           scale, window, max_kv, out, stream)
+            if r is not None:
+                return r
         dev = self._dev
         T, nq, hd = _dims(q, "q", 3, dev)
         o = torch.empty((T, nq, hd), dtype=q.dtype, device=q.device) if out is None else out

@@ -23,6 +23,8 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <vector>
 
 #include "tri.h"
@@ -413,6 +415,223 @@ PyObject *rope(Handle *h, PyObject *owner, PyObject *const *a) {
   return PyTuple_Pack(2, a[0], a[1]);
 }
 
+bool integer(PyObject *o, int64_t *v) {
+  if (!PyLong_CheckExact(o)) return false;
+  const long long x = PyLong_AsLongLong(o);
+  if (x == -1 && PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  *v = x;
+  return true;
+}
+
+// n contiguous integers (at least n with `more`) of type `st` on GPU `dev`.
+template <class T>
+bool integers(PyObject *o, int dev, at::ScalarType st, int64_t n, bool more, T **p) {
+  const at::Tensor *t = plain(o, dev);
+  if (!t || t->dim() != 1 || t->scalar_type() != st || (more ? t->size(0) < n : t->size(0) != n) ||
+      (t->size(0) > 1 && t->stride(0) != 1))
+    return false;
+  *p = static_cast<T *>(t->data_ptr());
+  return true;
+}
+
+// A block table [R, cols]: its size and row stride.
+bool block_table(PyObject *o, int dev, int32_t **p, int64_t *R, int64_t *cols, int64_t *rs,
+                 const at::Tensor **out) {
+  const at::Tensor *t = plain(o, dev);
+  if (!t || t->dim() != 2 || t->scalar_type() != at::kInt || t->size(0) > INT32_MAX ||
+      t->size(1) > INT32_MAX)
+    return false;
+  *R = t->size(0);
+  *cols = t->size(1);
+  *rs = rows(*t);
+  *p = static_cast<int32_t *>(t->data_ptr());
+  *out = t;
+  return *rs >= 0;
+}
+
+// The cache of k and v [n_pages, page, nk, hd] of `like`'s type; a dimension
+// of one reports what a packed cache has.
+bool kv_cache(PyObject *ko, PyObject *vo, int dev, const at::Tensor &like, tri_kv_cache *c) {
+  const at::Tensor *k = plain(ko, dev), *v = plain(vo, dev);
+  if (!k || !v || k->dim() != 4 || k->scalar_type() != like.scalar_type() || !same(*v, *k))
+    return false;
+  const int64_t n = k->size(0), page = k->size(1), nk = k->size(2), hd = k->size(3);
+  if (n > INT32_MAX || page > INT32_MAX || nk > INT32_MAX || hd > INT32_MAX) return false;
+  const auto view = [&](const at::Tensor &t, int64_t *ps, int64_t *ss, int64_t *hs) {
+    if (hd > 1 && t.stride(3) != 1) return false;
+    *hs = nk > 1 ? t.stride(2) : hd;
+    *ss = page > 1 ? t.stride(1) : std::max(hd, nk * *hs);
+    *ps = n > 1 ? t.stride(0) : page * std::max(*ss, nk * *hs);
+    return true;
+  };
+  c->k = k->data_ptr();
+  c->v = v->data_ptr();
+  c->n_pages = int32_t(n);
+  c->page = int32_t(page);
+  c->nk = int32_t(nk);
+  c->hd = int32_t(hd);
+  return view(*k, &c->k_ps, &c->k_ss, &c->k_hs) && view(*v, &c->v_ps, &c->v_ss, &c->v_hs);
+}
+
+// kv_slots(owner, kv_len, new_len, block_table, free_pages, free_count, page,
+// T, slots, pos, q_start, kv_len_out, free_out, stream)
+PyObject *kv_slots(Handle *h, PyObject *owner, PyObject *const *a) {
+  tri_kv_slots_args x{};
+  const at::Tensor *table;
+  int64_t R, cols, page;
+  void *s;
+  int32_t *kv, *more, *count, *stack = nullptr;
+  const at::Tensor *fp = plain(a[3], h->dev);
+  if (!block_table(a[2], h->dev, &x.table, &R, &cols, &x.table_rs, &table) ||
+      !integers(a[0], h->dev, at::kInt, R, false, &kv) ||
+      !integers(a[1], h->dev, at::kInt, R, false, &more) || !fp || fp->size(0) > INT32_MAX ||
+      !integers(a[3], h->dev, at::kInt, 0, true, &stack) ||
+      !integers(a[4], h->dev, at::kInt, 1, true, &count) || !integer(a[5], &page) ||
+      page > INT32_MAX || page < INT32_MIN || !integer(a[6], &x.T) || x.T < 0 ||
+      !stream_of(h, a[12], &s))
+    Py_RETURN_NONE;
+  x.R = int32_t(R);
+  x.cols = int32_t(cols);
+  x.page = int32_t(page);
+  x.n_free = int32_t(fp->size(0));
+  x.kv_len = kv;
+  x.new_len = more;
+  x.free_pages = stack;
+  x.free_count = count;
+  const int64_t n[5] = {x.T, x.T, R + 1, R, 2};
+  void *p[5];
+  for (int i = 0; i < 5; ++i) {
+    if (a[7 + i] == Py_None) continue;
+    int32_t *q;
+    if (i == 0 ? !integers(a[7], h->dev, at::kLong, n[0], false, &x.slots)
+               : !integers(a[7 + i], h->dev, at::kInt, n[i], false, &q))
+      Py_RETURN_NONE;
+    p[i] = i == 0 ? static_cast<void *>(x.slots) : q;
+  }
+  // those not given: the step's (slots, pos, q_start) share one allocation,
+  // what the next step takes (kv_len_out, free_out) another
+  at::Tensor made[5];
+  {
+    NoGil g;
+    for (int b = 0; b < 5; b = b ? 5 : 3) {
+      const int e = b ? 5 : 3;
+      int64_t at[5], bytes = 0;
+      for (int i = b; i < e; ++i) {
+        at[i] = bytes;
+        if (a[7 + i] == Py_None) bytes += (n[i] * (i ? 4 : 8) + 15) / 16 * 16;
+      }
+      if (!bytes) continue;
+      const at::Tensor all = at::empty({bytes}, table->options().dtype(at::kByte));
+      for (int i = b; i < e; ++i) {
+        if (a[7 + i] != Py_None) continue;
+        made[i] = at::detail::make_tensor<c10::TensorImpl>(
+            c10::Storage(all.storage()), all.key_set(),
+            c10::scalarTypeToTypeMeta(i ? at::kInt : at::kLong));
+        made[i].unsafeGetTensorImpl()->set_sizes_contiguous({n[i]});
+        made[i].unsafeGetTensorImpl()->set_storage_offset(at[i] / (i ? 4 : 8));
+        p[i] = static_cast<char *>(all.data_ptr()) + at[i];
+      }
+    }
+  }
+  x.slots = static_cast<int64_t *>(p[0]);
+  x.pos = static_cast<int32_t *>(p[1]);
+  x.q_start = static_cast<int32_t *>(p[2]);
+  x.kv_len_out = static_cast<int32_t *>(p[3]);
+  x.free_out = static_cast<int32_t *>(p[4]);
+  if (!issue(owner, "tri_kv_slots", [&] { return tri_kv_slots(h->cache, &x, s); })) return nullptr;
+  PyObject *r = PyTuple_New(5);
+  if (!r) return nullptr;
+  for (int i = 0; i < 5; ++i) {
+    PyObject *o = a[7 + i];
+    if (o == Py_None) {
+      o = THPVariable_Wrap(std::move(made[i]));
+      if (!o) {
+        Py_DECREF(r);
+        return nullptr;
+      }
+    } else {
+      Py_INCREF(o);
+    }
+    PyTuple_SET_ITEM(r, i, o);
+  }
+  return r;
+}
+
+// kv_write(owner, k, v, slots, k_cache, v_cache, stream)
+PyObject *kv_write(Handle *h, PyObject *owner, PyObject *const *a) {
+  const at::Tensor *k = plain(a[0], h->dev), *v = plain(a[1], h->dev);
+  tri_kv_cache c;
+  int64_t *slots;
+  void *s;
+  if (!k || !v || k->dim() != 3 || dtype_of(*k) < 0 || !same(*v, *k) ||
+      !integers(a[2], h->dev, at::kLong, k->size(0), false, &slots) ||
+      !kv_cache(a[3], a[4], h->dev, *k, &c) || c.nk != k->size(1) || c.hd != k->size(2) ||
+      !stream_of(h, a[5], &s))
+    Py_RETURN_NONE;
+  const int64_t T = k->size(0), ks = tokens(*k), vs = tokens(*v);
+  if (ks < 0 || vs < 0) Py_RETURN_NONE;
+  const tri_dtype dt = tri_dtype(dtype_of(*k));
+  const void *kp = k->data_ptr(), *vp = v->data_ptr();
+  if (!issue(owner, "tri_kv_write",
+             [&] { return tri_kv_write(h->cache, dt, kp, ks, vp, vs, slots, T, &c, s); }))
+    return nullptr;
+  return PyTuple_Pack(2, a[3], a[4]);
+}
+
+// paged_attention(owner, q, k_cache, v_cache, block_table, kv_len, q_start,
+// scale, window, max_kv, out, stream)
+PyObject *paged_attention(Handle *h, PyObject *owner, PyObject *const *a) {
+  const at::Tensor *q = plain(a[0], h->dev), *table;
+  tri_attention_args x{};
+  int64_t R, cols, window;
+  int32_t *tp, *kv, *starts;
+  void *s;
+  if (!q || q->dim() != 3 || dtype_of(*q) < 0 || q->size(1) > INT32_MAX ||
+      !kv_cache(a[1], a[2], h->dev, *q, &x.kv) || x.kv.hd != q->size(2) ||
+      !block_table(a[3], h->dev, &tp, &R, &cols, &x.table_rs, &table) ||
+      !integers(a[4], h->dev, at::kInt, R, false, &kv) ||
+      !integers(a[5], h->dev, at::kInt, R + 1, false, &starts) ||
+      !integer(a[7], &window) || window > INT32_MAX || window < INT32_MIN ||
+      !integer(a[8], &x.max_kv) || !stream_of(h, a[10], &s))
+    Py_RETURN_NONE;
+  if (a[6] == Py_None)
+    x.scale = float(1.0 / std::sqrt(double(q->size(2))));
+  else if (!number(a[6], &x.scale))
+    Py_RETURN_NONE;
+  Out y;
+  if (a[9] == Py_None && !q->is_contiguous()) Py_RETURN_NONE;
+  if (!y.take(a[9], *q, h->dev)) Py_RETURN_NONE;
+  x.dtype = dtype_of(*q);
+  x.nq = int32_t(q->size(1));
+  x.T = q->size(0);
+  x.R = int32_t(R);
+  x.cols = int32_t(cols);
+  x.q = q->data_ptr();
+  x.q_ts = tokens(*q);
+  x.out = y.t.data_ptr();
+  x.o_ts = tokens(y.t);
+  if (x.q_ts < 0 || x.o_ts < 0) Py_RETURN_NONE;
+  x.table = tp;
+  x.kv_len = kv;
+  x.q_start = starts;
+  x.window = int32_t(window);
+  at::Tensor work;
+  if (const int64_t need = tri_paged_attention_workspace(&x)) {
+    if (a[10] != Py_None) Py_RETURN_NONE;   // made on the call's stream there
+    NoGil g;
+    work = at::empty({need}, q->options().dtype(at::kByte));
+    x.workspace = work.data_ptr();
+    x.workspace_bytes = need;
+  }
+  if (!issue(owner, "tri_paged_attention",
+             [&] { return tri_paged_attention(h->cache, &x, s); }))
+    return nullptr;
+  return y.result();
+}
+
 // decode_chain_args(owner, args, stream)
 PyObject *chain(Handle *h, PyObject *owner, PyObject *const *a) {
   const void *p = structure(a[0], g_chain_args, sizeof(tri_chain_args));
@@ -463,6 +682,9 @@ PyMethodDef g_methods[] = {
     {"masked_fill", fn<masked_fill, 5>(), METH_FASTCALL, nullptr},
     {"embedding", fn<embedding, 4>(), METH_FASTCALL, nullptr},
     {"rope", fn<rope, 10>(), METH_FASTCALL, nullptr},
+    {"kv_slots", fn<kv_slots, 13>(), METH_FASTCALL, nullptr},
+    {"kv_write", fn<kv_write, 6>(), METH_FASTCALL, nullptr},
+    {"paged_attention", fn<paged_attention, 11>(), METH_FASTCALL, nullptr},
     {"chain", fn<chain, 2>(), METH_FASTCALL, nullptr},
     {"layers", fn<layers, 2>(), METH_FASTCALL, nullptr},
     {"close", close, METH_NOARGS, nullptr},

@@ -404,8 +404,10 @@ tri_status tri_spec_install_last_miss(tri_cache *c, tri_selection *out) {
     const int32_t i = scan_versions(c, c->miss_key);
     if (i >= 0) fill_selection(c->versions[i], i, c->miss_T, out, &c->miss_key);
     // the paged ops' launches depend on more than the key and T
-    if (is_paged_op(key_op(c->miss_key)))
+    if (is_paged_op(key_op(c->miss_key))) {
       for (int j = 0; j < out->n_launches; ++j) out->launch[j].grid_x = c->miss_grid[j];
+      out->launch[0].block_x = c->miss_block;
+    }
   }
   return TRI_OK;
 }

@@ -180,6 +180,7 @@ struct AttnPlan {
   int32_t splits;
   int32_t tiles;         // tiles of queries per K head (matrix forms)
   uint32_t grid[2];      // the attention launch, and the join's when splits > 1
+  uint32_t block;        // work-items of the first's workgroups
 };
 // `aligned`: every address and stride of q, out and the cache is a multiple of
 // 16 bytes. kv_max: the most keys a row can see. workspace: bytes available.
@@ -371,7 +372,7 @@ struct tri_cache {
   bool has_miss;
   tri::Key miss_key;
   int64_t miss_T;
-  uint32_t miss_grid[2];         // paged ops: the launches of the missed call
+  uint32_t miss_grid[2], miss_block;   // paged ops: the launches of the missed call
   tri_stats stats;
   tri_selection last;
   void *empty_fn;

@@ -186,6 +186,9 @@ struct KvWriteArgs {
 // Attention over pages (PA_*). With splits > 1 a workgroup leaves, for each of
 // its rows (t * nq + head), hd float32 sums at part[(row * splits + s) * hd]
 // and (maximum, sum) at ml[row * splits + s]; PA_JOIN adds them up.
+constexpr int32_t kJoinWave = 8;   // splits that a wavefront joins alone
+// Wavefronts of a PA_ROWS workgroup whose kernel holds heads of hdp elements.
+constexpr int rows_waves(int hdp) { return hdp > 128 ? 4 : 8; }
 struct PagedArgs {
   const void *q;
   void *out;
@@ -201,7 +204,8 @@ struct PagedArgs {
   int32_t tiles;          // tiles of queries per K head
   int32_t window;
   float scale;            // |scale| log2 e, above 0: the weights are powers of two
-  uint32_t flip;          // 1: scale is negative, the queries change sign
+  uint16_t flip;          // 1: scale is negative, the queries change sign
+  uint16_t stream;        // 1: K and V are read nontemporally (PA_ROWS)
   FastDiv div;            // by page
   FastDiv g_div;          // by g
 };

@@ -92,17 +92,17 @@ __device__ inline bool clear_not_finite(u32x4 &v) {
 // must not (a later token of the same chunk, an earlier one than the window):
 // a product over all keys would make NaN of their weight of 0. So in the steps
 // whose keys the rows see differently such elements go to LDS as zeros, and
-// where there are any, the lanes whose query sees their key add them from
-// memory: v is the key's V, e the first of four elements, w the query's weight.
+// where there were any, the lanes whose query sees their key add them to its
+// sums in the end, from memory. Weights are above 0 and have no say in what an
+// infinity or NaN makes of a sum; one that was in it already changes nothing.
+// v: the key's V; e: the first of four elements.
 template <int DT>
-__device__ inline void add_not_finite(const char *v, int32_t e, int32_t hd, float w, bool mine,
-                                      float *o) {
+__device__ inline void add_not_finite(const char *v, int32_t e, int32_t hd, float *o) {
   if (e >= hd) return;
-  float y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y[i] = Elt<DT>::ld(v, e + i);
-    if (mine && !(fabsf(y[i]) < __builtin_inff())) o[i] = fmaf(w, y[i], o[i]);
+    const float y = Elt<DT>::ld(v, e + i);
+    if (!(fabsf(y) < __builtin_inff())) o[i] += y;
   }
 }
 
@@ -120,18 +120,24 @@ struct Tile {
 
 template <int M>
 __device__ inline Tile find_tile(const PagedArgs &a, int32_t tile) {
-  const int lane = threadIdx.x & 63;
   Tile t;
-  t.r = -1;
-  for (int32_t b = 0; b < a.R; b += 64) {
-    const int32_t x = b + lane;
-    const int64_t first =
-        x < a.R ? int64_t(clamp_i32(a.q_start[x], 0, a.T)) * a.g / M + x : int64_t(1) << 40;
-    t.r += __popcll(__ballot(first <= tile));
+  const auto starts = [&](int32_t r, int32_t q0) {
+    return int64_t(clamp_i32(q0, 0, a.T)) * a.g / M + r <= tile;
+  };
+  if (a.R <= 64) {   // all in one round of loads
+    const int lane = threadIdx.x & 63, x = lane < a.R ? lane : 0;
+    const int32_t q0 = a.q_start[x], q1 = a.q_start[x + 1], kv = a.kv_len[x];
+    const uint64_t hit = __ballot(lane < a.R && starts(x, q0));
+    t.r = hit ? 63 - __builtin_clzll(hit) : -1;
+    if (t.r < 0) return t;
+    t.rq = clamped(a, __builtin_amdgcn_readlane(q0, t.r), __builtin_amdgcn_readlane(q1, t.r),
+                   __builtin_amdgcn_readlane(kv, t.r));
+  } else {
+    t.r = last_request(a.R, [&](int32_t x) { return starts(x, a.q_start[x]); });
+    t.r = __builtin_amdgcn_readfirstlane(t.r);
+    if (t.r < 0) return t;
+    t.rq = request_of(a, t.r);
   }
-  t.r = __builtin_amdgcn_readfirstlane(t.r);
-  if (t.r < 0) return t;
-  t.rq = request_of(a, t.r);
   const int64_t all = int64_t(t.rq.q1 - t.rq.q0) * a.g;
   const int64_t at = (tile - (int64_t(t.rq.q0) * a.g / M + t.r)) * M;
   if (at < 0 || at >= all) {
@@ -168,20 +174,29 @@ __device__ inline void store4(const PagedArgs &a, int32_t token, int32_t head, i
 }
 
 // ---- PA_ROWS ------------------------------------------------------------------------------------
-// Few rows per request (decode): a tile is 16 rows, and the four wavefronts
-// share out its keys, KB at a time each with its own softmax, joined in LDS at
-// the end. HBM-bound: K goes from memory into the registers of the first
-// product, V through the wavefront's own part of LDS (no barrier) into the
-// second's, and both loads of the next keys are in flight while these are
-// computed; the pages of the keys after those are looked up meanwhile.
+// Few rows per request (decode): a tile is 16 rows, and the wavefronts (eight,
+// or four of the widest heads, whose registers leave no room for more) share
+// out its keys, KB at a time each with its own softmax, joined in LDS at
+// the end. HBM-bound: K and V come in whole rows, a wavefront's loads covering
+// 1 KiB of them, and pass through a part of LDS that is the wavefront's own (no
+// barrier), first K, then V, on their way into the products. Each is in flight
+// until its step begins, and the pages of the step after are looked up
+// meanwhile. Read in the order of the first product's operand instead, 64
+// bytes of 16 rows a load, 1 GiB came at 6.35 TB/s, in whole rows at 6.95
+// (nontemporal; 6.1 and 6.2 without).
 template <int DT, int HDP>
 struct RowsShape {
   static constexpr int ES = Elt<DT>::ES;
+  static constexpr int NW = rows_waves(HDP);              // wavefronts
   static constexpr int KB = DT == kF32 ? 16 : 32;         // keys of a step
   static constexpr int MB = KB / 16;
-  static constexpr int NS = HDP * ES / 64;                // 16-byte vectors of a lane and key
-  // bytes of a row of V in LDS: 16 rows of the transposing read (of a column
-  // of float32) fall on different banks
+  static constexpr int NS = HDP * ES / 64;                // 16-byte vectors of a lane's query
+  static constexpr int CH = HDP * ES / 16;                // vectors of a row
+  static constexpr int RP = 64 / CH;                      // rows of a load
+  static constexpr int NP = KB / RP;
+  // bytes of a row in LDS: 8 rows of K on different banks; 16 rows of the
+  // transposing read of V (of a column of float32)
+  static constexpr int KS = HDP * ES + 16;
   static constexpr int VS = HDP * ES + (DT == kF32 ? 16 : 32);
   static constexpr int ND = HDP / 16;
   static constexpr int OS = HDP + 4;                      // floats of a row of O in LDS
@@ -191,9 +206,9 @@ struct RowsShape {
 template <int DT, int HDP>
 __device__ void body_pa_rows(const PagedArgs &a) {
   typedef RowsShape<DT, HDP> S;
-  constexpr int ES = S::ES, KB = S::KB, MB = S::MB, NS = S::NS, ND = S::ND;
-  __shared__ __attribute__((aligned(16))) char lds[4 * S::WAVE_LDS];
-  __shared__ float wave_m[4][16], wave_l[4][16];
+  constexpr int ES = S::ES, KB = S::KB, MB = S::MB, NS = S::NS, ND = S::ND, NW = S::NW;
+  __shared__ __attribute__((aligned(16))) char lds[NW * S::WAVE_LDS];
+  __shared__ float wave_m[NW][16], wave_l[NW][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int n = lane & 15, quarter = lane >> 4;
   const uint32_t kh = blockIdx.x % uint32_t(a.nk), rest = blockIdx.x / uint32_t(a.nk);
@@ -233,53 +248,66 @@ __device__ void body_pa_rows(const PagedArgs &a) {
   for (int i = 0; i < ND; ++i) o[i] = f32x4{0, 0, 0, 0};
   float m = kNegInf, l = 0.0f;
 
-  // the page of key k0 + 16 j + n (0 beyond the end: a page of the pool)
-  int32_t page[MB];
+  // the page of key k0 + lane % KB (beyond the end: the last key's)
   const auto look_up = [&](int32_t k0) {
-#pragma unroll
-    for (int j = 0; j < MB; ++j) {
-      const int32_t key = k0 + 16 * j + n;
-      page[j] = table[fast_div(uint32_t(key < e ? key : e - 1), a.div)];
-    }
+    const int32_t key = k0 + (lane & (KB - 1));
+    return table[fast_div(uint32_t(key < e ? key : e - 1), a.div)];
   };
-  // rows of K and V of those keys, and which of them are there
-  const char *kr[MB], *vr[MB];
-  bool there[MB];
-  const auto rows_of = [&](int32_t k0) {
-#pragma unroll
-    for (int j = 0; j < MB; ++j) {
-      const int32_t key = k0 + 16 * j + n;
-      const uint32_t k1 = uint32_t(key < e ? key : e - 1);
-      there[j] = key < e && uint32_t(page[j]) < uint32_t(a.n_pages);
-      const int64_t id = there[j] ? page[j] : 0;
-      const int64_t in = k1 - fast_div(k1, a.div) * uint32_t(a.page);
-      kr[j] = kp + (id * a.k.ps + in * a.k.ss) * ES + quarter * 16;
-      vr[j] = vp + (id * a.v.ps + in * a.v.ss) * ES + quarter * 16;
-    }
+  // where the lane's key lies (the pool's first page for one that is not
+  // there), handed to the lanes that load its row
+  const int srow = lane / S::CH, sbyte = (lane % S::CH) * 16;
+  const bool inside = sbyte < hdb, one_layout = a.k.ps == a.v.ps && a.k.ss == a.v.ss;
+  int64_t ko, vo;
+  uint64_t seen = 0;      // bit i: key k0 + i is there
+  const auto rows_of = [&](int32_t k0, int32_t page) {
+    const int32_t mine = k0 + (lane & (KB - 1));
+    const bool ok = mine < e && uint32_t(page) < uint32_t(a.n_pages);
+    seen = __ballot(ok);
+    const uint32_t key = uint32_t(mine < e ? mine : e - 1);
+    const int64_t id = ok ? page : 0;
+    const int64_t in = key - fast_div(key, a.div) * uint32_t(a.page);
+    ko = (id * a.k.ps + in * a.k.ss) * ES;
+    vo = ko;
+    if (!one_layout) vo = (id * a.v.ps + in * a.v.ss) * ES;
   };
-  u32x4 k[MB][NS], v[MB][NS];
-  const auto load = [&](u32x4(&x)[MB][NS], const char *const(&r)[MB]) {
+  u32x4 k[S::NP], v[S::NP];
 #pragma unroll
-    for (int j = 0; j < MB; ++j)
+  for (int i = 0; i < S::NP; ++i) k[i] = v[i] = u32x4{0, 0, 0, 0};
+  const auto load = [&](u32x4(&x)[S::NP], const char *p, int64_t at) {
+    int64_t r[S::NP];
 #pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        // a head shorter than HDP ends inside: its rest is zero
-        x[j][s] = u32x4{0, 0, 0, 0};
-        if (quarter * 16 + 64 * s < hdb) x[j][s] = *reinterpret_cast<const u32x4 *>(r[j] + 64 * s);
-      }
+    for (int i = 0; i < S::NP; ++i) r[i] = __shfl(at, srow + S::RP * i);
+    if (!inside) return;
+    if (a.stream) {
+#pragma unroll
+      for (int i = 0; i < S::NP; ++i)
+        x[i] = ld16<true>(reinterpret_cast<const u32x4 *>(p + r[i] + sbyte));
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::NP; ++i)
+        x[i] = ld16<false>(reinterpret_cast<const u32x4 *>(p + r[i] + sbyte));
+    }
   };
 
   const auto sees = [&](int32_t key) { return key >= my_lo && key < my_hi; };
-  int32_t k0 = b + wave * KB;
+  int32_t odd_b = 0, odd_e = 0;   // from the first to the last step with infinities or NaN
+  int32_t k0 = b + wave * KB, page = 0;
   if (k0 < e) {
-    look_up(k0);
-    rows_of(k0);
-    load(k, kr);
-    load(v, vr);
-    if (k0 + 4 * KB < e) look_up(k0 + 4 * KB);
+    rows_of(k0, look_up(k0));
+    load(k, kp, ko);
+    load(v, vp, vo);
+    if (k0 + NW * KB < e) page = look_up(k0 + NW * KB);
   }
-  for (; k0 < e; k0 += 4 * KB) {
-    const bool more = k0 + 4 * KB < e;
+  for (; k0 < e; k0 += NW * KB) {
+    const bool more = k0 + NW * KB < e;
+    const uint64_t there = seen;
+#pragma unroll
+    for (int i = 0; i < S::NP; ++i)
+      *reinterpret_cast<u32x4 *>(vl + (srow + S::RP * i) * S::KS + sbyte) = k[i];
+    if (more) {
+      rows_of(k0 + NW * KB, page);
+      load(k, kp, ko);
+    }
     // S^T
     f32x4 st[MB];
 #pragma unroll
@@ -287,42 +315,45 @@ __device__ void body_pa_rows(const PagedArgs &a) {
       st[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(vl + (16 * j + n) * S::KS + quarter * 16 +
+                                                         64 * s);
         if constexpr (DT == kF32) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            st[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[j][s][i]),
+            st[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[i]),
                                                          __uint_as_float(q[s][i]), st[j], 0, 0, 0);
         } else {
-          st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[j][s]),
+          st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
                                                           __builtin_bit_cast(bf16x8, q[s]), st[j],
                                                           0, 0, 0);
         }
       }
     }
-    // V to LDS; rows that are not there are zero, so that no weight of 0 meets
-    // a NaN
-    uint32_t seen = 0;   // bit i: key k0 + i is there
-#pragma unroll
-    for (int j = 0; j < MB; ++j) seen |= uint32_t(__ballot(there[j]) & 0xFFFF) << (16 * j);
+    // V in K's place; rows that are not there are zero, so that no weight of 0
+    // meets a NaN
     const int32_t k1 = k0 + KB < e ? k0 + KB : e;
     const bool mixed = k0 < all_lo || k1 > all_hi;   // some row sees not all of them
-    bool odd = false;
+    const bool partial = mixed || there != ~uint64_t(0);
+    if (partial) {
+      bool odd = false;
 #pragma unroll
-    for (int j = 0; j < MB; ++j)
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        if (!there[j]) v[j][s] = u32x4{0, 0, 0, 0};
-        if (mixed) odd |= clear_not_finite<DT>(v[j][s]);
-        *reinterpret_cast<u32x4 *>(vl + (16 * j + n) * S::VS + quarter * 16 + 64 * s) = v[j][s];
+      for (int i = 0; i < S::NP; ++i) {
+        if (!((there >> (srow + S::RP * i)) & 1)) v[i] = u32x4{0, 0, 0, 0};
+        if (mixed) odd |= clear_not_finite<DT>(v[i]);
       }
+      if (__ballot(odd)) {
+        if (odd_b == odd_e) odd_b = k0;
+        odd_e = k1;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < S::NP; ++i)
+      *reinterpret_cast<u32x4 *>(vl + (srow + S::RP * i) * S::VS + sbyte) = v[i];
     if (more) {
-      rows_of(k0 + 4 * KB);
-      load(k, kr);
-      load(v, vr);
-      if (k0 + 8 * KB < e) look_up(k0 + 8 * KB);
+      load(v, vp, vo);
+      if (k0 + 2 * NW * KB < e) page = look_up(k0 + 2 * NW * KB);
     }
     // softmax: the lane's keys are k0 + 16 j + 4 quarter + i
-    const bool partial = mixed || seen != (KB == 32 ? 0xFFFFFFFFu : 0xFFFFu);
     float top = kNegInf;
 #pragma unroll
     for (int j = 0; j < MB; ++j)
@@ -330,7 +361,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
       for (int i = 0; i < 4; ++i) {
         if (partial) {
           const int32_t x = 16 * j + 4 * quarter + i;
-          if (!((seen >> x) & 1) || !sees(k0 + x)) st[j][i] = kNegInf;
+          if (!((there >> x) & 1) || !sees(k0 + x)) st[j][i] = kNegInf;
         }
         top = fmaxf(top, st[j][i]);
       }
@@ -349,27 +380,6 @@ __device__ void body_pa_rows(const PagedArgs &a) {
       }
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[d] *= alpha;
-    if (mixed && __ballot(odd)) {
-#pragma unroll 1
-      for (int x = 0; x < KB; ++x) {
-        if (!((seen >> x) & 1)) continue;
-        // lane n + 16 (x / 4 % 4) has the query's weight of key x
-        float w = 0.0f;
-#pragma unroll
-        for (int j = 0; j < MB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (x / 16 == j && x % 4 == i) w = st[j][i];
-        w = __shfl(Elt<DT>::round(w), n + 16 * ((x / 4) % 4));
-        const char *y = vp + slot_offset(table, uint32_t(k0 + x), a, a.v) * ES;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
-          add_not_finite<DT>(y, 16 * d + 4 * quarter, a.hd, w, sees(k0 + x), z);
-          o[d] = f32x4{z[0], z[1], z[2], z[3]};
-        }
-      }
-    }
     u32x4 p = {0, 0, 0, 0};
     if constexpr (DT == kBF16) {
 #pragma unroll
@@ -398,6 +408,17 @@ __device__ void body_pa_rows(const PagedArgs &a) {
     }
   }
 
+  for (int32_t x = odd_b; x < odd_e; ++x) {
+    const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
+    if (at < 0 || !sees(x)) continue;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
+      add_not_finite<DT>(vp + at * ES, 16 * d + 4 * quarter, a.hd, z);
+      o[d] = f32x4{z[0], z[1], z[2], z[3]};
+    }
+  }
+
   // join the wavefronts
   l = sum_16_32(l);
   if (quarter == 0) {
@@ -409,16 +430,17 @@ __device__ void body_pa_rows(const PagedArgs &a) {
   for (int d = 0; d < ND; ++d)
     *reinterpret_cast<f32x4 *>(ol + n * S::OS + 16 * d + 4 * quarter) = o[d];
   __syncthreads();
-  const int row = threadIdx.x >> 4, part = threadIdx.x & 15;
+  constexpr int PR = NW * 4;   // work-items of a row
+  const int row = threadIdx.x / PR, part = threadIdx.x % PR;
   if (row >= t.rows) return;
   float top = kNegInf;
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
+  for (int w = 0; w < NW; ++w)
     if (wave_l[w][row] != 0.0f) top = fmaxf(top, wave_m[w][row]);
   const float ts = top == kNegInf ? 0.0f : top;
-  float f[4], sum = 0.0f;
+  float f[NW], sum = 0.0f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     f[w] = 0.0f;
     if (wave_l[w][row] != 0.0f) {
       f[w] = exp2_hw(wave_m[w][row] - ts);
@@ -429,12 +451,12 @@ __device__ void body_pa_rows(const PagedArgs &a) {
   const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-  for (int c = 0; c < HDP / 64; ++c) {
-    const int d = 64 * c + 4 * part;
+  for (int c = 0; c < (HDP + 4 * PR - 1) / (4 * PR); ++c) {
+    const int d = 4 * PR * c + 4 * part;
     if (d >= a.hd) break;
     f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       if (wave_l[w][row] == 0.0f) continue;
       const f32x4 x = *reinterpret_cast<const f32x4 *>(
           reinterpret_cast<const float *>(lds + w * S::WAVE_LDS) + row * S::OS + d);
@@ -488,12 +510,14 @@ struct TileShape {
   static constexpr int NP = KB / RP;
 };
 
+constexpr int kAhead = 4;   // products between an operand's read from LDS and its use
+
 template <int DT, int HDP>
 __device__ void body_pa_tile(const PagedArgs &a) {
   typedef TileShape<DT, HDP> S;
   constexpr int ES = S::ES, KB = S::KB, NB = S::NB, NQ = S::NQ, ND = S::ND, NP = S::NP;
   __shared__ __attribute__((aligned(16))) char lds[S::NBUF * S::BUF];
-  __shared__ int32_t odd_at[2];   // 1 + first key of a step whose V has infinities or NaN
+  __shared__ int32_t odd_b, odd_e;   // from the first to the last step with infinities or NaN
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = lane & 31, half = lane >> 5;
   const uint32_t kh = blockIdx.x % uint32_t(a.nk), rest = blockIdx.x / uint32_t(a.nk);
@@ -501,7 +525,10 @@ __device__ void body_pa_tile(const PagedArgs &a) {
   // the last tiles, which see the most keys, first
   const Tile t = find_tile<128>(a, a.tiles - 1 - int32_t(rest / uint32_t(a.splits)));
   if (t.r < 0) return;
-  if (tid < 2) odd_at[tid] = 0;
+  if (tid == 0) {
+    odd_b = 0x7FFFFFFF;
+    odd_e = 0;
+  }
   const int32_t lo = t.p0 < 0 ? 0 : first_key(t.p0, a.window), hi = t.p1 + 1;
   int32_t b, e;
   split_keys(lo, hi, a.splits, split, &b, &e);
@@ -553,20 +580,32 @@ __device__ void body_pa_tile(const PagedArgs &a) {
   };
   u32x4 sk[NP], sv[NP];
   uint64_t seen = 0;     // bit i: key k0 + i of the staged step is there
-  const auto load = [&](int32_t k0, int32_t page) {
-    seen = __ballot(k0 + (lane & (KB - 1)) < e && uint32_t(page) < uint32_t(a.n_pages));
+  const bool one_layout = a.k.ps == a.v.ps && a.k.ss == a.v.ss;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int r = srow + S::RP * i;
-      const int32_t pid = __shfl(page, r);
-      const uint32_t key = uint32_t(k0 + r < e ? k0 + r : e - 1);
-      const int64_t id = (seen >> r) & 1 ? pid : 0;
-      const int64_t in = key - fast_div(key, a.div) * uint32_t(a.page);
-      sk[i] = u32x4{0, 0, 0, 0};
-      sv[i] = u32x4{0, 0, 0, 0};
-      if (inside) {
-        sk[i] = *reinterpret_cast<const u32x4 *>(kp + (id * a.k.ps + in * a.k.ss) * ES + sbyte);
-        sv[i] = *reinterpret_cast<const u32x4 *>(vp + (id * a.v.ps + in * a.v.ss) * ES + sbyte);
+  for (int i = 0; i < NP; ++i) sk[i] = sv[i] = u32x4{0, 0, 0, 0};
+  const auto load = [&](int32_t k0, int32_t page) {
+    // where the lane's key lies (the pool's first page for one that is not
+    // there), handed to the lanes that load its row
+    const int32_t mine = k0 + (lane & (KB - 1));
+    const bool ok = mine < e && uint32_t(page) < uint32_t(a.n_pages);
+    seen = __ballot(ok);
+    const uint32_t key = uint32_t(mine < e ? mine : e - 1);
+    const int64_t id = ok ? page : 0;
+    const int64_t in = key - fast_div(key, a.div) * uint32_t(a.page);
+    const int64_t ko = (id * a.k.ps + in * a.k.ss) * ES;
+    int64_t vo = ko;
+    if (!one_layout) vo = (id * a.v.ps + in * a.v.ss) * ES;
+    int64_t kr[NP], vr[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) kr[i] = vr[i] = __shfl(ko, srow + S::RP * i);
+    if (!one_layout)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) vr[i] = __shfl(vo, srow + S::RP * i);
+    if (inside) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        sk[i] = *reinterpret_cast<const u32x4 *>(kp + kr[i] + sbyte);
+        sv[i] = *reinterpret_cast<const u32x4 *>(vp + vr[i] + sbyte);
       }
     }
   };
@@ -585,14 +624,17 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       *reinterpret_cast<u32x4 *>(kl + r * S::KS + sbyte) = sk[i];
       *reinterpret_cast<u32x4 *>(vl + r * S::VS + sbyte) = sv[i];
     }
-    if (mixed && odd) odd_at[buf] = k0 + 1;
+    if (mixed && odd) {
+      atomicMin(&odd_b, k0);
+      atomicMax(&odd_e, k1);
+    }
   };
 
   uint64_t there = 0;    // `seen` of the step being computed
   int32_t page = 0;
   if (b < e) {
     load(b, look_up(b));
-    __syncthreads();     // odd_at is clear
+    __syncthreads();     // odd_b, odd_e are set
     store(b, 0);
     there = seen;
     if (b + KB < e) {
@@ -609,25 +651,38 @@ __device__ void body_pa_tile(const PagedArgs &a) {
     f32x16 st[NB];
     if (work) {
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) st[j][i] = 0.0f;
+      // product i: vector i / NB of 32 keys i % NB; their reads kAhead products
+      // before them (left to itself the scheduler makes each wait for its own)
+      const auto read_k = [&](int i) {
+        return *reinterpret_cast<const u32x4 *>(kl + (32 * (i % NB) + n) * S::KS + half * 16 +
+                                                32 * (i / NB));
+      };
+      u32x4 k[kAhead];
 #pragma unroll
-        for (int s = 0; s < NQ; ++s) {
-          const u32x4 k = *reinterpret_cast<const u32x4 *>(kl + (32 * j + n) * S::KS + half * 16 +
-                                                           32 * s);
-          if constexpr (DT == kF32) {
+      for (int i = 0; i < kAhead; ++i) k[i] = read_k(i);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              st[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[i]),
-                                                           __uint_as_float(q[s][i]), st[j], 0, 0, 0);
-          } else {
-            st[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
-                                                            __builtin_bit_cast(bf16x8, q[s]), st[j],
-                                                            0, 0, 0);
-          }
+      for (int i = 0; i < NB * NQ; ++i) {
+        f32x16 &x = st[i % NB];
+        const u32x4 y = k[i % kAhead];
+        if constexpr (DT == kF32) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            x = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(y[c]),
+                                                     __uint_as_float(q[i / NB][c]), x, 0, 0, 0);
+        } else {
+          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y),
+                                                      __builtin_bit_cast(bf16x8, q[i / NB]), x, 0, 0,
+                                                      0);
         }
+        if (i + kAhead < NB * NQ) k[i % kAhead] = read_k(i + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
     const uint64_t now = there;
     if constexpr (S::NBUF == 2) {
@@ -641,6 +696,23 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       }
     }
     if (work) {
+      const auto read_v = [&](int i) {
+        const int s = i / ND, d = i % ND;
+        if constexpr (DT == kF32) {
+          return u32x4{*reinterpret_cast<const uint32_t *>(
+                           vl + (8 * (s / 4) + 4 * half + s % 4) * S::VS + (32 * d + n) * 4),
+                       0, 0, 0};
+        } else {
+          // keys 16 s + 4 half + (0..3 and 8..11)
+          const char *x = vl + (16 * s + 4 * half + ((lane & 15) >> 2)) * S::VS +
+                          (32 * d + (lane & 16) + 4 * (lane & 3)) * 2;
+          const u32x2 y0 = lds_transpose(x), y1 = lds_transpose(x + 8 * S::VS);
+          return u32x4{y0[0], y0[1], y1[0], y1[1]};
+        }
+      };
+      u32x4 y[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) y[i] = read_v(i);
       // the lane's keys are k0 + 32 j + 8 (i / 4) + 4 half + i % 4
       const int32_t k1 = k0 + KB < e ? k0 + KB : e;
       const bool mixed = k0 < w_all_lo || k1 > w_all_hi;
@@ -669,69 +741,45 @@ __device__ void body_pa_tile(const PagedArgs &a) {
         for (int d = 0; d < ND; ++d) o[d] *= alpha;
       }
       const float ms = m == kNegInf ? 0.0f : m;
+      // O^T, product i: elements 32 (i % ND) .. of V at keys 16 (i / ND) .. (bf16;
+      // float32: at one key of each half). The reads of V run ahead as those
+      // of K; the weights of the next keys are formed between the products.
+      constexpr int NV = DT == kF32 ? 16 * ND : KB / 16 * ND;
+      constexpr int WC = DT == kF32 ? 1 : 8;          // weights of a lane for ND products
+      constexpr int WP = (WC + ND - 1) / ND;          // formed at each of them
+      const auto weight = [&](int c) {
+        const float x = exp2_hw(fmaf(st[c / 16][c % 16], a.scale, -ms));
+        st[c / 16][c % 16] = x;
+        l += x;
+      };
 #pragma unroll
-      for (int j = 0; j < NB; ++j)
+      for (int c = 0; c < WC; ++c) weight(c);
+      u32x4 p = {0, 0, 0, 0};
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          st[j][i] = exp2_hw(fmaf(st[j][i], a.scale, -ms));
-          l += st[j][i];
-        }
-      if (odd_at[buf] == k0 + 1) {
-#pragma unroll 1
-        for (int x = 0; x < KB; ++x) {
-          if (!((now >> x) & 1)) continue;
-          // lane n + 32 (x / 4 % 2) has the query's weight of key x
-          float w = 0.0f;
+      for (int i = 0; i < NV; ++i) {
+        const int s = i / ND, d = i % ND;
+        if constexpr (DT == kF32) {
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(y[i % kAhead][0]), st[0][s],
+                                                      o[d], 0, 0, 0);
+        } else {
+          if (d == 0) {
 #pragma unroll
-          for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (x / 32 == j && (x % 32) / 8 == i / 4 && x % 4 == i % 4) w = st[j][i];
-          w = __shfl(Elt<DT>::round(w), n + 32 * ((x / 4) % 2));
-          const char *y = vp + slot_offset(table, uint32_t(k0 + x), a, a.v) * ES;
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float z[4];
-#pragma unroll
-              for (int c = 0; c < 4; ++c) z[c] = o[d][4 * i + c];
-              add_not_finite<DT>(y, 32 * d + 8 * i + 4 * half, a.hd, w, sees(k0 + x), z);
-#pragma unroll
-              for (int c = 0; c < 4; ++c) o[d][4 * i + c] = z[c];
-              __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-      }
-      if constexpr (DT == kF32) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const float y = *reinterpret_cast<const float *>(
-                vl + (8 * (i / 4) + 4 * half + i % 4) * S::VS + (32 * d + n) * 4);
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(y, st[0][i], o[d], 0, 0, 0);
+            for (int c = 0; c < 4; ++c)
+              p[c] = Elt<kBF16>::pack2(st[s / 2][8 * (s % 2) + 2 * c],
+                                       st[s / 2][8 * (s % 2) + 2 * c + 1]);
           }
-      } else {
-#pragma unroll
-        for (int s = 0; s < KB / 16; ++s) {
-          // keys 16 s + 4 half + (0..3 and 8..11)
-          u32x4 p;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            p[i] = Elt<kBF16>::pack2(st[s / 2][8 * (s % 2) + 2 * i], st[s / 2][8 * (s % 2) + 2 * i + 1]);
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const char *x = vl + (16 * s + 4 * half + ((lane & 15) >> 2)) * S::VS +
-                            (32 * d + (lane & 16) + 4 * (lane & 3)) * 2;
-            const u32x2 y0 = lds_transpose(x), y1 = lds_transpose(x + 8 * S::VS);
-            const u32x4 y = {y0[0], y0[1], y1[0], y1[1]};
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y),
-                                                           __builtin_bit_cast(bf16x8, p), o[d], 0, 0,
-                                                           0);
-          }
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y[i % kAhead]),
+                                                         __builtin_bit_cast(bf16x8, p), o[d], 0, 0,
+                                                         0);
         }
+        if (i + kAhead < NV) y[i % kAhead] = read_v(i + kAhead);
+#pragma unroll
+        for (int c = WP * d; c < WP * (d + 1) && c < WC; ++c)
+          if (WC * (s + 1) + c < 16 * NB) weight(WC * (s + 1) + c);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
     __syncthreads();
     if constexpr (S::NBUF == 2) {
@@ -747,6 +795,22 @@ __device__ void body_pa_tile(const PagedArgs &a) {
     }
   }
 
+  // (the last step's barrier is behind all of them)
+  for (int32_t x = b < e ? odd_b : e; x < odd_e; ++x) {
+    const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
+    if (at < 0 || !sees(x)) continue;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) z[c] = o[d][4 * i + c];
+        add_not_finite<DT>(vp + at * ES, 32 * d + 8 * i + 4 * half, a.hd, z);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[d][4 * i + c] = z[c];
+      }
+  }
   if (row >= t.rows) return;
   l = sum_32(l);
   const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;

@@ -6,7 +6,7 @@ namespace tri {
 using namespace dev;
 
 template <int HDP>
-__global__ __launch_bounds__(256, HDP == 256 ? 1 : 2) void k_pa_rows_bf16(PagedArgs a) {
+__global__ __launch_bounds__(64 * rows_waves(HDP), 1) void k_pa_rows_bf16(PagedArgs a) {
   body_pa_rows<kBF16, HDP>(a);
 }
 

@@ -27,12 +27,12 @@ __device__ inline int32_t clamp_i32(int32_t v, int32_t lo, int32_t hi) {
   return v < lo ? lo : v > hi ? hi : v;
 }
 
+__device__ inline Request clamped(const PagedArgs &a, int32_t q0, int32_t q1, int32_t kv) {
+  return {clamp_i32(q0, 0, a.T), clamp_i32(q1, 0, a.T), clamp_i32(kv, 0, a.cols * a.page)};
+}
+
 __device__ inline Request request_of(const PagedArgs &a, int32_t r) {
-  Request q;
-  q.q0 = clamp_i32(a.q_start[r], 0, a.T);
-  q.q1 = clamp_i32(a.q_start[r + 1], 0, a.T);
-  q.kv = clamp_i32(a.kv_len[r], 0, a.cols * a.page);
-  return q;
+  return clamped(a, a.q_start[r], a.q_start[r + 1], a.kv_len[r]);
 }
 
 // First key that the row at position p (>= 0) sees.
@@ -58,6 +58,27 @@ __device__ inline void split_keys(int32_t lo, int32_t hi, int32_t splits, int32_
   const int64_t first = lo + s * run, last = first + run;
   *b = first < hi ? int32_t(first) : hi;
   *e = last < hi ? int32_t(last) : hi;
+}
+
+// The last r of [0, R) with first(r), -1 if none, for a first() that does not
+// turn true again after it was false (else some r that it holds for, or -1):
+// 64 requests probed at once, so two rounds of loads find any of 4096. The
+// whole wavefront calls it and gets the same answer.
+template <class F>
+__device__ inline int32_t last_request(int32_t R, F &&first) {
+  const int lane = threadIdx.x & 63;
+  const int32_t step = (R + 63) >> 6;
+  int32_t base = 0;
+  if (step > 1) {
+    const int32_t x = lane * step;
+    const uint64_t hit = __ballot(x < R && first(x < R ? x : 0));
+    if (!hit) return -1;
+    base = (63 - __builtin_clzll(hit)) * step;
+  }
+  const int32_t x = base + lane;
+  const int32_t m = step > 1 && R - base > step ? step : R - base;
+  const uint64_t hit = __ballot(lane < m && first(lane < m ? x : base));
+  return hit ? base + 63 - __builtin_clzll(hit) : -1;
 }
 
 }  // namespace dev

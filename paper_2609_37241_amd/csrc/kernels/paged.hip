@@ -38,24 +38,27 @@ struct SlotReq {
   int32_t more;
 };
 
+// Pages of n >= 0 tokens.
+__device__ inline int32_t pages_of(int32_t n, const KvSlotsArgs &a) {
+  const uint32_t full = fast_div(uint32_t(n), a.div);
+  return int32_t(full + (uint32_t(n) != full * uint32_t(a.page)));
+}
+
 __device__ inline SlotReq slot_req(const KvSlotsArgs &a, int32_t r) {
   SlotReq q;
   q.held = clamp_i32(a.kv_len[r], 0, a.cols * a.page);
   const int32_t n = a.new_len[r];
   q.more = n > 0 ? n : 0;
   q.all = int64_t(q.held) + q.more;
-  const int32_t in = sat_i32(q.all);
-  const uint32_t pages = fast_div(uint32_t(in), a.div);
-  const int64_t need = int64_t(pages) + (uint32_t(in) != pages * uint32_t(a.page));
-  const uint32_t full = fast_div(uint32_t(q.held), a.div);
-  q.have = int32_t(full + (uint32_t(q.held) != full * uint32_t(a.page)));
-  q.want = int32_t(need > a.cols ? a.cols : need) - q.have;
+  const int32_t need = pages_of(sat_i32(q.all), a);
+  q.have = pages_of(q.held, a);
+  q.want = (need > a.cols ? a.cols : need) - q.have;
   return q;
 }
 }  // namespace
 
 __global__ __launch_bounds__(256) void k_kv_slots(KvSlotsArgs a) {
-  __shared__ int32_t row0[kReqMax + 1], page0[kReqMax + 1];
+  __shared__ int32_t row0[kReqMax + 1], page0[kReqMax + 1], held[kReqMax];
   __shared__ int64_t wave_rows[4], wave_pages[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t R = a.R;
@@ -64,8 +67,10 @@ __global__ __launch_bounds__(256) void k_kv_slots(KvSlotsArgs a) {
   const int per = (R + 255) / 256;
   const int r0 = tid * per, r1 = r0 + per < R ? r0 + per : R;
   int64_t rows = 0, pages = 0;
+  SlotReq own{};
   for (int r = r0; r < r1; ++r) {
     const SlotReq q = slot_req(a, r);
+    own = q;
     rows += q.more;
     pages += q.want;
   }
@@ -97,7 +102,8 @@ __global__ __launch_bounds__(256) void k_kv_slots(KvSlotsArgs a) {
   for (int r = r0; r < r1; ++r) {
     row0[r] = sat_i32(sr);
     page0[r] = sat_i32(sp);
-    const SlotReq q = slot_req(a, r);
+    const SlotReq q = per == 1 ? own : slot_req(a, r);
+    held[r] = q.held;
     sr += q.more;
     sp += q.want;
     if (r == R - 1) {
@@ -112,17 +118,17 @@ __global__ __launch_bounds__(256) void k_kv_slots(KvSlotsArgs a) {
     int32_t pos = 0;
     if (t < row0[R]) {
       const int32_t r = last_at_most(row0, R, int32_t(t));
-      const SlotReq q = slot_req(a, r);
-      pos = sat_i32(int64_t(q.held) + (t - row0[r]));
+      const int32_t have = pages_of(held[r], a);
+      pos = sat_i32(int64_t(held[r]) + (t - row0[r]));
       const uint32_t col = fast_div(uint32_t(pos), a.div);
       if (col < uint32_t(a.cols)) {
         // a page held before is the table's, a new one the stack's: the entry
         // that this launch writes is not read
         int32_t id = -1;
-        if (int32_t(col) < q.have) {
+        if (int32_t(col) < have) {
           id = a.table[r * a.table_rs + col];
         } else {
-          const int64_t at = int64_t(count) - 1 - page0[r] - (int32_t(col) - q.have);
+          const int64_t at = int64_t(count) - 1 - page0[r] - (int32_t(col) - have);
           if (at >= 0) id = a.free_pages[at];
         }
         if (id >= 0) slot = int64_t(id) * a.page + (uint32_t(pos) - col * uint32_t(a.page));
@@ -133,9 +139,8 @@ __global__ __launch_bounds__(256) void k_kv_slots(KvSlotsArgs a) {
   }
   for (int64_t j = first; j < page0[R]; j += step) {
     const int32_t r = last_at_most(page0, R, int32_t(j));
-    const SlotReq q = slot_req(a, r);
     const int64_t at = int64_t(count) - 1 - j;
-    a.table[r * a.table_rs + q.have + (j - page0[r])] = at >= 0 ? a.free_pages[at] : -1;
+    a.table[r * a.table_rs + pages_of(held[r], a) + (j - page0[r])] = at >= 0 ? a.free_pages[at] : -1;
   }
   if (blockIdx.x == 0) {
     for (int r = tid; r < R; r += 256) {
@@ -212,11 +217,7 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
     const int64_t row = it / a.splits;
     const int32_t s = int32_t(it - row * a.splits);
     const int32_t t = int32_t(row / a.nq), h = int32_t(row - int64_t(t) * a.nq);
-    int32_t r = -1;
-    for (int32_t b = 0; b < a.R; b += 64) {
-      const int32_t x = b + lane;
-      r += __popcll(__ballot(x < a.R && a.q_start[x < a.R ? x : 0] <= t));
-    }
+    const int32_t r = last_request(a.R, [&](int32_t x) { return a.q_start[x] <= t; });
     if (r < 0) continue;
     const Request rq = request_of(a, r);
     if (t < rq.q0 || t >= rq.q1) continue;
@@ -289,18 +290,43 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
 
 // ---- PA_JOIN -----------------------------------------------------------------------------------
 // out = sum_s 2^(m_s - m) part_s / sum_s 2^(m_s - m) l_s over the splits of a
-// row, m the largest m_s, always in the order of s: the same bits every time.
+// row, m the largest m_s, always in the same order: the same bits every time.
 // A split without a seen key (l_s = 0) left no sums and is passed over. A
-// wavefront per row.
-template <int DT>
-__global__ __launch_bounds__(256) void k_pa_join(PagedArgs a) {
+// wavefront per row, or four where there are many splits: what bounds it is
+// the latency of the sums' loads, so as many lanes as a row leaves free take
+// other splits, eight of them in flight.
+template <int DT, int VEC>
+__device__ void join_rows(const PagedArgs &a) {
+  __shared__ float sums[4][64 * VEC];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rows = int64_t(a.T) * a.nq;
   const int32_t t0 = clamp_i32(a.q_start[0], 0, a.T), t1 = clamp_i32(a.q_start[a.R], 0, a.T);
-  for (int64_t row = int64_t(blockIdx.x) * 4 + wave; row < rows; row += int64_t(gridDim.x) * 4) {
+  const bool four = a.splits > kJoinWave;
+  // lanes across the elements (a power of two), groups across the splits
+  int nl = 1;
+  while (nl < 64 && nl * VEC < a.hd) nl *= 2;
+  const int per_wave = 64 / nl, groups = four ? 4 * per_wave : per_wave;
+  const int group = (four ? wave * per_wave : 0) + lane / nl;
+  const int64_t rows = int64_t(a.T) * a.nq, step = int64_t(gridDim.x) * (four ? 1 : 4);
+  for (int64_t row = four ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + wave; row < rows;
+       row += step) {
     const int32_t t = int32_t(row / a.nq), h = int32_t(row - int64_t(t) * a.nq);
     if (t < t0 || t >= t1) continue;
     const int64_t at = row * a.splits;
+    // the sums, the first eight of a lane before what weighs them is known
+    const auto read = [&](int s, int d, float *x) {
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) x[c] = 0.0f;
+      if (s >= a.splits || d >= a.hd) return;
+      const float *p = a.part + (at + s) * a.hd + d;
+      if constexpr (VEC == 4)
+        Elt<kF32>::unpack(*reinterpret_cast<const u32x4 *>(p), x);
+      else
+        x[0] = *p;
+    };
+    const int e = (lane % nl) * VEC;
+    float x[8][VEC];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) read(i * groups + group, e, x[i]);
     // at most 64 splits: one a lane
     const float m = lane < a.splits ? a.ml[2 * (at + lane)] : kNegInf;
     const float l = lane < a.splits ? a.ml[2 * (at + lane) + 1] : 0.0f;
@@ -313,17 +339,57 @@ __global__ __launch_bounds__(256) void k_pa_join(PagedArgs a) {
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
     const uint64_t there = __ballot(l != 0.0f);
     char *o = static_cast<char *>(a.out) + (int64_t(t) * a.o_ts + int64_t(h) * a.hd) * Elt<DT>::ES;
-    for (int d0 = 0; d0 < a.hd; d0 += 64) {   // every lane stays: __shfl reads from lane s
-      const int d = d0 + lane;
-      float acc = 0.0f;
-      for (int32_t s = 0; s < a.splits; ++s) {
-        if (!((there >> s) & 1)) continue;
-        const float ws = __shfl(w, s);
-        if (d < a.hd) acc = fmaf(ws, a.part[(at + s) * a.hd + d], acc);
+    for (int d0 = 0; d0 < a.hd; d0 += nl * VEC) {   // (every lane stays: they exchange)
+      const int d = d0 + e;
+      float acc[VEC] = {};
+      for (int s0 = 0; s0 < a.splits; s0 += 8 * groups) {
+        if (d0 + s0 > 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) read(s0 + i * groups + group, d, x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int s = s0 + i * groups + group;
+          const float ws = __shfl(w, s & 63);
+          // (a split that left no sums has anything in their place)
+          if (s < a.splits && ((there >> s) & 1)) {
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) acc[c] = fmaf(ws, x[i][c], acc[c]);
+          }
+        }
       }
-      if (d < a.hd) Elt<DT>::st(o, d, sum == 0.0f ? 0.0f : acc / sum);
+      for (int y = nl; y < 64; y *= 2)
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) acc[c] += __shfl_xor(acc[c], y);
+      if (four) {
+        __syncthreads();   // the sums of the elements before are read
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) sums[wave][lane * VEC + c] = acc[c];
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < VEC; ++c)
+          acc[c] = (sums[0][lane * VEC + c] + sums[1][lane * VEC + c]) +
+                   (sums[2][lane * VEC + c] + sums[3][lane * VEC + c]);
+      }
+      if (d < a.hd && lane < nl && (!four || wave == 0)) {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) acc[c] = sum == 0.0f ? 0.0f : acc[c] / sum;
+        if constexpr (VEC == 4 && DT == kF32)
+          st_any<kF32, false>(o + d * 4, Elt<kF32>::pack(acc));
+        else
+#pragma unroll
+          for (int c = 0; c < VEC; ++c) Elt<DT>::st(o, d + c, acc[c]);
+      }
     }
   }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void k_pa_join(PagedArgs a) {
+  if (a.hd % 4 == 0)
+    join_rows<DT, 4>(a);
+  else
+    join_rows<DT, 1>(a);
 }
 
 namespace {

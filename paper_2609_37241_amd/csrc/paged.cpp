@@ -110,30 +110,26 @@ AttnPlan plan_of(const tri_attention_args &a, uint64_t workspace) {
                    attn_keys(a), workspace);
 }
 
-// Lookup for a call whose launches are `grid`: as lookup(), the launches kept
-// for the record of an install after a miss.
-int lookup_paged(tri_cache *c, uint32_t op, const Key &k, int64_t T, const uint32_t *grid, int n,
-                 int32_t *vi, bool *auto_inst) {
-  const int st = lookup(c, op, k, T, vi, auto_inst);
-  if (st == TRI_MISS)
-    for (int i = 0; i < 2; ++i) c->miss_grid[i] = i < n ? grid[i] : 0;
-  return st;
-}
-
-// The launches of a paged op, in order, stopping at the first failure.
+// The launches of a paged op (`block` work-items a workgroup the first, 256
+// any other), in order, stopping at the first failure. On a miss they are kept
+// for the record of an install that follows.
 tri_status run_paged(tri_cache *c, uint32_t op, const Key &k, int64_t T, const uint32_t *grid,
-                     int n, const void *args, uint32_t size, void *stream) {
+                     int n, uint32_t block, const void *args, uint32_t size, void *stream) {
   int32_t vi;
   bool auto_inst = false;
-  const int st = lookup_paged(c, op, k, T, grid, n, &vi, &auto_inst);
-  if (st != TRI_OK) return tri_status(st);
+  const int st = lookup(c, op, k, T, &vi, &auto_inst);
+  if (st != TRI_OK) {
+    for (int i = 0; i < 2; ++i) c->miss_grid[i] = i < n ? grid[i] : 0;
+    c->miss_block = block;
+    return tri_status(st);
+  }
   Version &v = c->versions[vi];
   tri_launch_rec l[3];
   int rc = 0;
   for (int i = 0; i < v.plan.n_launches; ++i) {
-    l[i] = {v.plan.kvariant[i], grid[i], kBlock};
+    l[i] = {v.plan.kvariant[i], grid[i], i == 0 ? block : kBlock};
     if (rc == 0)
-      rc = launch(c, v, i, key_dtype(k), grid[i], kBlock, args, size, stream);
+      rc = launch(c, v, i, key_dtype(k), grid[i], l[i].block_x, args, size, stream);
   }
   record(c, op, v, vi, k, v.plan.n_launches, l, rc ? TRI_E_LAUNCH : TRI_OK);
   return finish(c, v, auto_inst, rc);
@@ -149,12 +145,14 @@ tri_status tri_kv_slots(tri_cache *c, const tri_kv_slots_args *p, void *stream) 
   c->stats.calls++;
   if (!p) return finish_early(c, op, TRI_E_INVALID);
   const tri_kv_slots_args &a = *p;
+  // T is the room in slots and pos: without any, lengths and pages are done all
+  // the same
   int st = check_common(TRI_F32, a.T);
-  if (st != kGo) return finish_early(c, op, st);
+  if (st != kGo && a.T != 0) return finish_early(c, op, st);
   st = check_table(a.table, a.table_rs, a.R, a.cols, a.page);
   if (st != kGo) return finish_early(c, op, st);
   if (a.n_free < 0 || !a.kv_len || !a.new_len || !a.free_count || (a.n_free && !a.free_pages) ||
-      !a.slots || !a.pos || !a.q_start || !a.kv_len_out || !a.free_out)
+      (a.T && (!a.slots || !a.pos)) || !a.q_start || !a.kv_len_out || !a.free_out)
     return finish_early(c, op, TRI_E_INVALID);
   if ((addr(a.kv_len) | addr(a.new_len) | addr(a.free_count) | addr(a.free_pages) | addr(a.pos) |
        addr(a.q_start) | addr(a.kv_len_out) | addr(a.free_out)) % 4 || addr(a.slots) % 8)
@@ -183,7 +181,7 @@ tri_status tri_kv_slots(tri_cache *c, const tri_kv_slots_args *p, void *stream) 
                          a.q_start, a.kv_len_out, a.free_out, a.T, a.table_rs, a.R, a.page,
                          a.cols, a.n_free, fast_div_of(uint32_t(a.page))};
   const uint32_t grid = kv_slots_grid(a.T, a.R);
-  return run_paged(c, op, k, a.T, &grid, 1, &args, sizeof args, stream);
+  return run_paged(c, op, k, a.T, &grid, 1, kBlock, &args, sizeof args, stream);
 }
 
 tri_status tri_kv_write(tri_cache *c, tri_dtype dtype, const void *k, int64_t k_ts, const void *v,
@@ -214,7 +212,7 @@ tri_status tri_kv_write(tri_cache *c, tri_dtype dtype, const void *k, int64_t k_
                          int64_t(kv->n_pages) * kv->page, kv->page, kv->nk, kv->hd,
                          fast_div_of(uint32_t(kv->page)), fast_div_of(items), items};
   const uint32_t grid = kv_write_grid(T, items);
-  return run_paged(c, op, key, T, &grid, 1, &args, sizeof args, stream);
+  return run_paged(c, op, key, T, &grid, 1, kBlock, &args, sizeof args, stream);
 }
 
 tri_status tri_paged_attention(tri_cache *c, const tri_attention_args *p, void *stream) {
@@ -230,6 +228,10 @@ tri_status tri_paged_attention(tri_cache *c, const tri_attention_args *p, void *
                    uint64_t(a.kv.hd), uint64_t(a.nq), uint64_t(a.kv.nk));
   k.k3 = (uint64_t(plan.form) << 16) | (uint64_t(plan.splits > 1) << 24);
   float *part = static_cast<float *>(a.workspace);
+  // K and V that outgrow the last-level cache do not stay for the next call
+  const uint64_t bytes = 2 * uint64_t(a.R) * uint64_t(attn_keys(a)) * uint64_t(a.kv.nk) *
+                         uint64_t(a.kv.hd) * es_of(uint32_t(a.dtype));
+  const bool large = bytes > kCacheBytes;
   const int32_t g = a.nq / a.kv.nk;
   // the weights are 2^(c q.k - maximum), c = |scale| log2 e; for 0 a c so small
   // that all weights are 1 (a masked score stays -inf)
@@ -242,9 +244,10 @@ tri_status tri_paged_attention(tri_cache *c, const tri_attention_args *p, void *
                        plan.splits > 1 ? part + a.T * a.nq * plan.splits * a.kv.hd : nullptr,
                        a.q_ts, a.o_ts, a.table_rs, int32_t(a.T), a.R, a.cols, a.kv.n_pages,
                        a.kv.page, a.nq, a.kv.nk, a.kv.hd, g, plan.splits, plan.tiles, a.window,
-                       c2, a.scale < 0.0f, fast_div_of(uint32_t(a.kv.page)),
+                       c2, uint16_t(a.scale < 0.0f), uint16_t(large), fast_div_of(uint32_t(a.kv.page)),
                        fast_div_of(uint32_t(g))};
-  return run_paged(c, op, k, a.T, plan.grid, plan.splits > 1 ? 2 : 1, &args, sizeof args, stream);
+  return run_paged(c, op, k, a.T, plan.grid, plan.splits > 1 ? 2 : 1, plan.block, &args, sizeof args,
+                   stream);
 }
 
 int64_t tri_paged_attention_workspace(const tri_attention_args *p) {

@@ -219,35 +219,58 @@ FastDiv fast_div_of(uint32_t d) {
 
 uint32_t kv_slots_grid(int64_t T, int32_t R) {
   const int64_t rows = T > R ? T : int64_t(R);
-  const int64_t g = cdiv(rows, 4 * int64_t(kBlock));
-  return uint32_t(g > 256 ? 256 : g);
+  const int64_t g = cdiv(rows, int64_t(kBlock));
+  return uint32_t(g > 512 ? 512 : g);
 }
 
 uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
   return clamp_grid(cdiv(T * int64_t(row_items), kBlock));
 }
 
+// Form. Heads the matrix forms do not hold, or rows that are not aligned, take
+// PA_ANY. Tiles of 16 rows (PA_ROWS) serve decode, and chunks whose tiles of
+// 128 would be few or mostly empty; rpr: rows of a request and K head, were the
+// requests equal. bf16: 16 requests behind 1000 tokens, 32 query and 8 K heads
+// of 128, 2 / 4 / 8 new tokens each (8 / 16 / 32 rows): 24 / 26 / 38 us against
+// PA_TILE's 25 / 28 / 28; one request, 8 + 8 heads, 32 / 128 / 256 new tokens
+// (16 / 64 / 128 tiles of 16 in all): 12 / 18 / 28 against 20 / 26 / 27, but
+// each tile of 16 reads all keys, so this holds for short contexts only.
+// float32, whose products cost 16 times as much, gains from full tiles up to
+// 256 rows: 16 requests of 64 / 128 new tokens, 32 and 8 heads of 128 (256 /
+// 512 rows), 233 / 474 us against 287 / 306; one of 64 / 128: 39 / 62 against
+// 51 / 53.
+//
+// Splits. Few tiles leave compute units idle, so their keys are split until
+// there are `want` workgroups, in runs of at least `run` keys; the join costs
+// 4 us and the traffic of the sums. PA_ROWS wants 1024 (64 requests of up to
+// 8k tokens, where the longest decides: 214 us; 512 workgroups 227, 2048 212)
+// and runs of 1024 (four steps of a workgroup: a request of 500 tokens 10.1 us
+// against 11.5 split in two). PA_TILE wants 256, one a compute unit, rounded
+// down (24 requests with a window, 218 workgroups: 48.8 us against 57.7 split
+// in two), and runs of 512 keys (four prompts of up to 1024 tokens, heads of
+// 256: 40 us against 52 split), 256 in float32, whose steps take longer.
 AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                    bool aligned, int64_t kv_max, uint64_t workspace) {
   AttnPlan p{};
+  const int64_t rows = T * nq, g = nq / nk, f32 = dtype == TRI_F32;
+  // workgroups before any split (PA_ANY: four wavefronts of a row each)
+  int64_t have = cdiv(rows, 4), want = 512, run = 256, tiles = 0;
   p.form = kAttnAny;
-  const int64_t rows = T * nq, g = nq / nk;
-  // workgroups (PA_ANY: of four wavefronts) before any split, those wanted,
-  // and the fewest keys a split is worth
-  int64_t have = cdiv(rows, 4), want = 512, run = 256;
-  int64_t tiles = 0;
+  p.block = kBlock;
   if (aligned && hd % vec_elems(dtype) == 0 && hd <= kAttnMatrixHd) {
-    // rows of a request and K head, were the requests equal
-    p.form = cdiv(T, R) * g <= 16 ? kAttnRows : kAttnTile;
-    const int64_t m = p.form == kAttnRows ? 16 : 128;
+    const int64_t rpr = cdiv(T, R) * g, tiles16 = cdiv(T * g, 16) * nk;
+    const bool few = rpr <= (f32 ? 256 : 16) || (tiles16 <= 64 && kv_max <= 4096);
+    p.form = few ? kAttnRows : kAttnTile;
+    const int64_t m = few ? 16 : 128;
     tiles = T * g / m + R;
     // a request has at least a tile, and no more requests than rows have any
-    const int64_t full = cdiv(T * g, m);
-    have = (full > (R < T ? R : T) ? full : (R < T ? R : T)) * nk;
-    want = p.form == kAttnRows ? 1024 : 512;
-    run = p.form == kAttnRows ? 256 : 512;
+    const int64_t full = cdiv(T * g, m), busy = R < T ? R : T;
+    have = (full > busy ? full : busy) * nk;
+    want = few ? 1024 : 256;
+    run = few ? 1024 : f32 ? 256 : 512;
+    if (few) p.block = uint32_t(64 * rows_waves(attn_hdp(hd)));
   }
-  int64_t s = cdiv(want, have);
+  int64_t s = want / have;
   const int64_t most = cdiv(kv_max, run);
   if (s > most) s = most;
   if (s > TRI_MAX_KV_SPLITS) s = TRI_MAX_KV_SPLITS;
@@ -256,7 +279,7 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
   p.tiles = int32_t(tiles);
   p.grid[0] = p.form == kAttnAny ? clamp_grid(cdiv(rows * p.splits, 4))
                                  : uint32_t(tiles * nk * p.splits);
-  p.grid[1] = clamp_grid(cdiv(rows, 4));
+  p.grid[1] = p.splits < 2 ? 0 : clamp_grid(p.splits > kJoinWave ? rows : cdiv(rows, 4));
   return p;
 }
 
