@@ -584,7 +584,8 @@ tri_status tri_kv_write(tri_cache *cache, tri_dtype dtype, const void *k, int64_
  * tri_paged_attention_workspace gives what the call would use. max_kv only
  * steers the split; a wrong one costs time, not correctness.
  * hd 1..512; nq 1..4096; T * nq below 2^31; cols * page below 2^31; scale
- * finite; window, max_kv >= 0. */
+ * finite; window, max_kv >= 0. A call whose tiles need 2^32 work-items or more
+ * is UNSUPPORTED (not below T * nq = 2^26 and R * nk = 2^22). */
 tri_status tri_paged_attention(tri_cache *cache, const tri_attention_args *args, void *stream);
 
 /* Bytes of workspace that tri_paged_attention would use for these arguments

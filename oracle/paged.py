@@ -101,3 +101,76 @@ def attention(q, kc, vc, table, kv_len, q_start, scale, window=0):
                     slack[t, h] = (2 * (u * (hd + 3) * big + 4 * u * np.abs(s).max())
                                    + (2 * len(s) + 200) * u)
     return out, written, spread, slack
+
+
+# ---- selections ----------------------------------------------------------------------------
+# Which kernels a valid call launches, from the rules alone (Python integers).
+OP_KV_SLOTS, OP_KV_WRITE, OP_PAGED_ATTENTION = 12, 13, 14
+KV_SLOTS, KVW_ANY, KVW_VEC = 80, 82, 83
+PA_ANY, PA_ROWS, PA_TILE, PA_JOIN = 90, 91, 92, 93
+GRID_CAP = 1 << 20
+MAX_SPLITS = 64
+JOIN_WAVE = 8          # splits one wavefront joins
+
+
+def _bucket(T):
+    return max(0, (max(T, 1) - 1).bit_length())
+
+
+def _cdiv(a, b):
+    return -(-a // b)
+
+
+def _k0(op, dtype, T, aligned):
+    return op | dtype << 8 | _bucket(T) << 16 | int(aligned) << 24
+
+
+def kv_slots_selection(T, R):
+    """(key, [(variant, workgroups, work-items)]) of a kv_slots call."""
+    return ((_k0(OP_KV_SLOTS, 0, T, False), 0, 0, 0, 0, 0),
+            [(KV_SLOTS, min(512, _cdiv(max(T, R), 256)), 256)])
+
+
+def kv_write_selection(dtype, T, nk, hd, aligned):
+    """dtype 0: float32, 1: bfloat16; aligned: rows and slots at 16 bytes."""
+    v = 8 if dtype else 4
+    vec = aligned and hd % v == 0
+    items = 2 * nk * hd // (v if vec else 1)
+    return ((_k0(OP_KV_WRITE, dtype, T, aligned), 0, hd | nk << 32, 0, 0, 0),
+            [(KVW_VEC if vec else KVW_ANY, min(GRID_CAP, _cdiv(T * items, 256)), 256)])
+
+
+def attention_workspace(T, nq, hd, splits):
+    return T * nq * splits * (hd + 2) * 4 if splits > 1 else 0
+
+
+def attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
+    """(form, splits, grids, work-items): 0 any, 1 rows, 2 tile; kv_max: the most
+    keys a row can see."""
+    v, g = (8 if dtype else 4), nq // nk
+    if not aligned or hd % v or hd > 256:
+        form, have, want, run, tiles, block = 0, _cdiv(T * nq, 4), 512, 256, 0, 256
+    else:
+        small = _cdiv(T, R) * g <= (16 if dtype else 256)
+        small |= _cdiv(T * g, 16) * nk <= 64 and kv_max <= 4096
+        form, m = (1, 16) if small else (2, 128)
+        tiles = T * g // m + R
+        have = max(_cdiv(T * g, m), min(R, T)) * nk
+        want, run = (1024, 1024) if small else (256, 512 if dtype else 256)
+        block = (256 if hd > 128 else 512) if small else 256
+    s = max(1, min(want // have, _cdiv(kv_max, run), MAX_SPLITS))
+    while s > 1 and attention_workspace(T, nq, hd, s) > workspace:
+        s -= 1
+    first = tiles * nk * s if form else min(GRID_CAP, _cdiv(T * nq * s, 4))
+    join = min(GRID_CAP, T * nq if s > JOIN_WAVE else _cdiv(T * nq, 4))
+    return form, s, [first] + ([join] if s > 1 else []), block
+
+
+def attention_selection(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
+    form, s, grids, block = attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace)
+    key = (_k0(OP_PAGED_ATTENTION, dtype, T, aligned), 0, hd | nq << 16 | nk << 32,
+           form << 16 | int(s > 1) << 24, 0, 0)
+    launches = [((PA_ANY, PA_ROWS, PA_TILE)[form], grids[0], block)]
+    if s > 1:
+        launches.append((PA_JOIN, grids[1], 256))
+    return key, launches

@@ -694,7 +694,9 @@ class SpecCache:
         window > 0 limits a row to its last `window` keys; max_kv, a bound on
         kv_len that the host knows (0: the table's width), steers how the
         work is split. Rows of no request keep what `out` held (an output made
-        here is not initialised)."""
+        here is not initialised). A call that splits its keys takes a
+        workspace from torch's allocator; a prepared one keeps it, so it must
+        not run on two streams at once."""
         if self._rec is None:
             r = self._fast.paged_attention(self, q, k_cache, v_cache, block_table, kv_len, q_start,
                                            scale, window, max_kv, out, stream)

@@ -179,7 +179,8 @@ struct AttnPlan {
   uint32_t form;
   int32_t splits;
   int32_t tiles;         // tiles of queries per K head (matrix forms)
-  uint32_t grid[2];      // the attention launch, and the join's when splits > 1
+  uint32_t grid[2];      // the attention launch (0: more than a launch can have), and the
+                         // join's when splits > 1
   uint32_t block;        // work-items of the first's workgroups
 };
 // `aligned`: every address and stride of q, out and the cache is a multiple of

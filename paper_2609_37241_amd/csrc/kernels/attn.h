@@ -796,7 +796,7 @@ __device__ void body_pa_tile(const PagedArgs &a) {
   }
 
   // (the last step's barrier is behind all of them)
-  for (int32_t x = b < e ? odd_b : e; x < odd_e; ++x) {
+  for (int32_t x = odd_b; b < e && x < odd_e; ++x) {
     const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
     if (at < 0 || !sees(x)) continue;
 #pragma unroll

@@ -50,10 +50,12 @@ __device__ inline int64_t slot_offset(const int32_t *row, uint32_t key, const Pa
   return int64_t(id) * c.ps + int64_t(key - col * uint32_t(a.page)) * c.ss;
 }
 
-// The keys [lo, hi) of a tile cut into `splits` runs of whole 64s: run s.
+// The keys [lo, hi) of a tile cut into `splits` runs of whole 64s: run s, in
+// [lo, hi] (hi < lo, rows before the first key: empty, at lo).
 __device__ inline void split_keys(int32_t lo, int32_t hi, int32_t splits, int32_t s, int32_t *b,
                                   int32_t *e) {
-  const int32_t n = hi > lo ? hi - lo : 0;
+  if (hi < lo) hi = lo;
+  const int32_t n = hi - lo;
   const int64_t run = (int64_t(n) + int64_t(splits) * 64 - 1) / (int64_t(splits) * 64) * 64;
   const int64_t first = lo + s * run, last = first + run;
   *b = first < hi ? int32_t(first) : hi;

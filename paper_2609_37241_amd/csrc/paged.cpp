@@ -224,6 +224,7 @@ tri_status tri_paged_attention(tri_cache *c, const tri_attention_args *p, void *
   const int st = attn_check(a, true);
   if (st != kGo) return finish_early(c, op, st);
   const AttnPlan plan = plan_of(a, uint64_t(a.workspace_bytes));
+  if (!plan.grid[0]) return finish_early(c, op, TRI_E_UNSUPPORTED);
   Key k = make_key(op, uint32_t(a.dtype), a.T, attn_aligned(a) ? kAlign : 0u, 0, 0, 0,
                    uint64_t(a.kv.hd), uint64_t(a.nq), uint64_t(a.kv.nk));
   k.k3 = (uint64_t(plan.form) << 16) | (uint64_t(plan.splits > 1) << 24);

@@ -277,8 +277,11 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
   while (s > 1 && attn_workspace(T, nq, hd, int32_t(s)) > workspace) --s;
   p.splits = s < 1 ? 1 : int32_t(s);
   p.tiles = int32_t(tiles);
-  p.grid[0] = p.form == kAttnAny ? clamp_grid(cdiv(rows * p.splits, 4))
-                                 : uint32_t(tiles * nk * p.splits);
+  const int64_t grid = tiles * nk * p.splits;
+  if (p.form == kAttnAny)
+    p.grid[0] = clamp_grid(cdiv(rows * p.splits, 4));
+  else if (grid * p.block < int64_t(1) << 32)   // the work-items a launch can have
+    p.grid[0] = uint32_t(grid);
   p.grid[1] = p.splits < 2 ? 0 : clamp_grid(p.splits > kJoinWave ? rows : cdiv(rows, 4));
   return p;
 }

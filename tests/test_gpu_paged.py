@@ -282,6 +282,186 @@ def test_attention_offsets_beyond_32_bits(cache):
     assert torch.equal(p["kc"][-1, 15], k[0]) and torch.equal(p["vc"][far - 1, 0], -k[2])
 
 
+# ---- tiles of many rows: every case of these is served by them ------------------------------
+TILE_HEADS = [("bf16", 8, 1, 128), ("bf16", 5, 1, 80), ("bf16", 16, 1, 64), ("bf16", 6, 1, 256),
+              ("bf16", 10, 2, 96), ("bf16", 33, 3, 72), ("bf16", 130, 1, 8), ("f32", 20, 1, 64),
+              ("f32", 20, 1, 80), ("f32", 32, 1, 128), ("f32", 21, 1, 256), ("f32", 80, 2, 20)]
+TILE_BATCHES = {
+    "prompts": [(70, 70), (33, 33), (64, 64)],
+    "chunks": [(100, 30), (0, 0), (300, 129), (31, 1), (257, 60)],
+    "short": [(3, 25), (0, 24), (10, 22)],
+    "pages end": [(65, 40), (127, 31), (16, 16), (49, 33)],
+}
+
+
+def tile_problem(dtype, lens, nq, nk, hd, page=16, **kw):
+    """A problem whose table is wide: more keys than tiles of few rows serve."""
+    p = problem(dtype, lens, nq, nk, hd, page, **kw)
+    wide = torch.full((len(lens), 4200 // page + 1), -1, dtype=torch.int32, device=DEV)
+    wide[:, :p["table"].shape[1]] = p["table"]
+    return dict(p, table=wide)
+
+
+def tile_check(cache, p, dtype, window=0, **kw):
+    got = attend(cache, p, window=window, **kw)
+    assert cache.last_selection().variant == P.PA_TILE
+    return got
+
+
+@pytest.mark.parametrize("batch", list(TILE_BATCHES))
+@pytest.mark.parametrize("dtype,nq,nk,hd", TILE_HEADS)
+def test_tile_heads_and_lengths(cache, dtype, nq, nk, hd, batch):
+    p = tile_problem(dtype, TILE_BATCHES[batch], nq, nk, hd, seed=nq, pad=2)
+    check(tile_check(cache, p, dtype), oracle(p), dtype)
+
+
+@pytest.mark.parametrize("window", [1, 2, 15, 64, 65, 1000])
+@pytest.mark.parametrize("batch", ["chunks", "pages end"])
+@pytest.mark.parametrize("dtype,nq,nk,hd", [TILE_HEADS[0], TILE_HEADS[7], TILE_HEADS[3]])
+def test_tile_window(cache, dtype, nq, nk, hd, batch, window):
+    # (a window bounds the keys: rows of nobody make the tiles too many for the other form)
+    p = tile_problem(dtype, TILE_BATCHES[batch], nq, nk, hd, seed=window, pad=150)
+    check(tile_check(cache, p, dtype, window), oracle(p, window), dtype)
+
+
+@pytest.mark.parametrize("layout", ["slot", "head", "pair"])
+@pytest.mark.parametrize("page", [1, 3, 24, 64, 100])
+@pytest.mark.parametrize("dtype,nq,nk,hd", [("bf16", 16, 2, 128), ("f32", 40, 2, 64)])
+def test_tile_pages_and_layouts(cache, dtype, nq, nk, hd, page, layout):
+    p = tile_problem(dtype, [(130, 40), (65, 30), (48, 48), (97, 1)], nq, nk, hd, page,
+                     layout=layout, seed=page)
+    if layout == "pair":                    # K and V in one tensor, V of other strides
+        p["vc"] = p["vc"].contiguous()
+    check(tile_check(cache, p, dtype), oracle(p), dtype)
+
+
+@pytest.mark.parametrize("dtype,nq,nk,hd", [("bf16", 8, 1, 128), ("bf16", 10, 2, 64), ("f32", 32, 1, 64),
+                                             ("bf16", 5, 1, 80), ("f32", 20, 1, 128)])
+@pytest.mark.parametrize("lens", [[(100, 100)], [(300, 37), (60, 60)], [(150, 70)]])
+def test_tile_infinities_in_hidden_places(cache, dtype, nq, nk, hd, lens):
+    p = tile_problem(dtype, lens, nq, nk, hd, pad=150)
+    inf, nan = float("inf"), float("nan")
+    for i, (r, back) in enumerate([(0, 1), (0, 5), (len(lens) - 1, 33), (0, 36)]):
+        x = lens[r][0] - back
+        pid = int(p["table"][r, x // 16])
+        p["vc"][pid, x % 16, i % nk, 3 * i] = (inf, -inf, nan, inf)[i]
+        if i == 1:
+            p["kc"][pid, x % 16, 0, 2] = nan
+    check(tile_check(cache, p, dtype), oracle(p), dtype)
+    check(tile_check(cache, p, dtype, 4), oracle(p, 4), dtype)
+    check(tile_check(cache, p, dtype, 40), oracle(p, 40), dtype)
+
+
+@pytest.mark.parametrize("dtype,nq,nk,hd", [("bf16", 8, 1, 128), ("f32", 32, 1, 64)])
+def test_tile_special_values(cache, dtype, nq, nk, hd):
+    n = 50
+    p = tile_problem(dtype, [(120, n)], nq, nk, hd)
+    p["q"][0, 1] = float("nan")
+    p["q"][n - 1, 2, 5] = float("inf")
+    check(tile_check(cache, p, dtype), oracle(p), dtype)
+    p = tile_problem(dtype, [(120, n)], nq, nk, hd)
+    p["q"].abs_()
+    p["kc"][int(p["table"][0, 1]), 3] = -float("inf")
+    check(tile_check(cache, p, dtype), oracle(p), dtype)
+    for x in range(120):
+        p["kc"][int(p["table"][0, x // 16]), x % 16] = -float("inf")
+    got = tile_check(cache, p, dtype)
+    assert (f64(got) == 0).all()
+    p = tile_problem(dtype, [(120, n)], nq, nk, hd, peak=100.0)
+    check(tile_check(cache, p, dtype), oracle(p), dtype)
+    for scale in (0.0, -0.3):
+        p["scale"] = scale
+        check(tile_check(cache, p, dtype), oracle(p), dtype)
+    # scores that rise by more than the softmax's reference allows, and fall
+    p = tile_problem(dtype, [(120, n)], nq, nk, hd)
+    p["q"][:] = 1.0
+    for x in range(120):
+        p["kc"][int(p["table"][0, x // 16]), x % 16] = 0.3 * (x if x < 100 else 200 - x)
+    check(tile_check(cache, p, dtype), oracle(p), dtype)
+
+
+@pytest.mark.parametrize("dtype,nq,nk,hd", [("bf16", 8, 1, 128), ("f32", 32, 1, 64)])
+def test_tile_bad_pages_in_place_and_rows_with_gaps(cache, dtype, nq, nk, hd):
+    p = tile_problem(dtype, [(200, 40), (90, 40)], nq, nk, hd)
+    p["table"][0, 2], p["table"][0, 5] = p["kc"].shape[0], -7
+    p["table"][1, :] = 2 ** 31 - 1
+    got = tile_check(cache, p, dtype)
+    check(got, oracle(p), dtype)
+    assert (f64(got)[40:80] == 0).all()
+    p = tile_problem(dtype, [(200, 40), (90, 40)], nq, nk, hd)
+    want = oracle(p)
+    wide = torch.full((80, nq * hd + 16), 7.0, dtype=DT[dtype], device=DEV)
+    view = wide.as_strided((80, nq, hd), (nq * hd + 16, hd, 1))
+    view.copy_(p["q"])
+    p["q"] = view
+    check(tile_check(cache, p, dtype, out=view), want, dtype)      # out is q
+    assert (wide[:, nq * hd:] == 7.0).all()
+    for starts in ([-4, 40, 2 ** 31 - 1], [0, 40, 40], [40, 40, 80], [80, 80, 80]):
+        p["q_start"] = i32(starts)
+        check(attend(cache, p), oracle(p), dtype)
+
+
+@pytest.mark.parametrize("R", [63, 64, 65, 130, 1000, 4096])
+@pytest.mark.parametrize("dtype,nq,nk,hd", [("bf16", 2, 1, 16), ("bf16", 40, 1, 8), ("f32", 2, 2, 5)])
+def test_attention_many_requests(cache, dtype, nq, nk, hd, R):
+    """Requests are found among more than a wavefront has lanes."""
+    r = np.random.Generator(np.random.PCG64(R))
+    new = r.integers(0, 3, R)
+    new[r.random(R) < 0.3] = 0
+    lens = [(int(n + c), int(n)) for n, c in zip(new, r.integers(0, 12, R))]
+    if nq == 40:
+        lens = lens[:1000]
+    p = problem(dtype, lens, nq, nk, hd, 8, seed=R, pad=1)
+    wide = torch.full((len(lens), p["table"].shape[1] + 5), 2 ** 30, dtype=torch.int32, device=DEV)
+    wide[:, :-5] = p["table"]
+    p["table"] = wide[:, :-5]                       # rows with a gap
+    check(attend(cache, p), oracle(p), dtype)
+
+
+def large_oracle(p, window=0):
+    """oracle() in torch's float64 on the GPU, for one request."""
+    q, kv = p["q"].double(), int(p["kv_len"][0])
+    n, g = q.shape[0], q.shape[1] // p["kc"].shape[2]
+    page = p["kc"].shape[1]
+    rows = p["table"][0, :-(-kv // page)].long()
+    K, V = (p[x][rows].flatten(0, 1)[:kv].double() for x in ("kc", "vc"))
+    j = torch.arange(kv, device=DEV)
+    pos = torch.arange(kv - n, kv, device=DEV)[:, None]
+    hide = (j > pos) | ((j <= pos - window) if window else False)
+    out, spread, slack = torch.empty_like(q), torch.empty_like(q), q[..., 0].clone()
+    u, hd = 2.0 ** -24, q.shape[2]
+    for h in range(q.shape[1]):
+        k, v = K[:, h // g].contiguous(), V[:, h // g].contiguous()
+        s = (q[:, h].contiguous() @ k.t().contiguous()) * p["scale"]
+        big = (q[:, h].abs().contiguous() @ k.abs().t().contiguous()).masked_fill(hide, 0).amax(1)
+        top = s.abs().masked_fill(hide, 0).amax(1)
+        w = torch.softmax(s.masked_fill(hide, -float("inf")), 1)
+        out[:, h], spread[:, h] = w @ v, w @ v.abs()
+        slack[:, h] = 2 * (u * (hd + 3) * big * p["scale"] + 4 * u * top) + (2 * kv + 200) * u
+    return f64(out), np.ones(n, dtype=bool), f64(spread), f64(slack)
+
+
+@pytest.mark.parametrize("dtype,kv,n,nq,nk,hd,window,layout", [
+    ("bf16", 5000, 3000, 8, 2, 128, 0, "slot"), ("bf16", 2500, 2500, 5, 1, 64, 700, "head"),
+    ("bf16", 1500, 1300, 4, 4, 256, 0, "slot"), ("bf16", 9000, 400, 40, 1, 80, 0, "pair"),
+    ("f32", 3000, 2000, 4, 2, 128, 0, "head"), ("f32", 1200, 1200, 2, 2, 256, 300, "slot"),
+    ("f32", 40000, 1, 8, 2, 64, 0, "slot"), ("bf16", 70000, 2, 8, 1, 96, 0, "slot"),
+    ("bf16", 1100, 1000, 3, 1, 33, 0, "odd")])
+def test_attention_long_chunks(cache, dtype, kv, n, nq, nk, hd, window, layout):
+    p = problem(dtype, [(kv, n)], nq, nk, hd, 16, layout, seed=kv)
+    check(attend(cache, p, window=window), large_oracle(p, window), dtype)
+
+
+@pytest.mark.parametrize("flag", ["jit", "autotune", "generic", "resident_args"])
+def test_other_caches_give_the_same(cache, tri, flag):
+    other = tri.SpecCache(auto_install=True, **{flag: True})
+    for lens in ([(3000, 1)], [(300, 200), (5, 1)]):
+        p = problem("bf16", lens, 4, 2, 64, 16)
+        assert torch.equal(attend(cache, p), attend(other, p))
+    slots_case(other, *SLOT_CASES[3])
+    other.close()
+
+
 # ---- the store -----------------------------------------------------------------------------
 @pytest.mark.parametrize("layout", ["slot", "head", "odd", "pair"])
 @pytest.mark.parametrize("nk,hd", [(8, 128), (1, 64), (3, 80), (2, 33), (5, 1), (40, 256)])
@@ -368,6 +548,10 @@ def test_slots_many_requests(cache, R):
     need = int(sum(-(-(a + b) // 16) + (-a // 16) for a, b in zip(kv, new)))
     slots_case(cache, kv.tolist(), new.tolist(), 16, 20, need + 5, need + 5 - (R % 2) * 7,
                int(new.sum()) + R % 3)
+
+
+def test_slots_without_rows(cache):
+    slots_case(cache, [5, 0], [4, 9], 4, 5, 6, 6, 0)
 
 
 def test_slots_long_prompt(cache):
