@@ -107,7 +107,7 @@ def attention(q, kc, vc, table, kv_len, q_start, scale, window=0):
 # Which kernels a valid call launches, from the rules alone (Python integers).
 OP_KV_SLOTS, OP_KV_WRITE, OP_PAGED_ATTENTION = 12, 13, 14
 KV_SLOTS, KVW_ANY, KVW_VEC = 80, 82, 83
-PA_ANY, PA_ROWS, PA_TILE, PA_JOIN = 90, 91, 92, 93
+PA_ANY, PA_ROWS, PA_TILE, PA_JOIN, PA_PAIR = 90, 91, 92, 93, 94
 GRID_CAP = 1 << 20
 MAX_SPLITS = 64
 JOIN_WAVE = 8          # splits one wavefront joins
@@ -145,7 +145,7 @@ def attention_workspace(T, nq, hd, splits):
 
 
 def attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
-    """(form, splits, grids, work-items): 0 any, 1 rows, 2 tile; kv_max: the most
+    """(form, splits, grids, work-items): 0 any, 1 rows, 2 tile, 3 pair; kv_max: the most
     keys a row can see."""
     v, g = (8 if dtype else 4), nq // nk
     if not aligned or hd % v or hd > 256:
@@ -158,7 +158,12 @@ def attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
         have = max(_cdiv(T * g, m), min(R, T)) * nk
         want, run = (1024, 1024) if small else (256, 512 if dtype else 256)
         block = (256 if hd > 128 else 512) if small else 256
-    s = max(1, min(want // have, _cdiv(kv_max, run), MAX_SPLITS))
+        if form == 2 and dtype and hd <= 128 and have <= 256 and kv_max >= 2048:
+            form, block = 3, 512
+    s = min(want // have, _cdiv(kv_max, run))
+    if form == 1 and kv_max > 512:
+        s = max(s, min(256 // have, _cdiv(kv_max, 256)))
+    s = max(1, min(s, MAX_SPLITS))
     while s > 1 and attention_workspace(T, nq, hd, s) > workspace:
         s -= 1
     first = tiles * nk * s if form else min(GRID_CAP, _cdiv(T * nq * s, 4))
@@ -170,7 +175,7 @@ def attention_selection(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
     form, s, grids, block = attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace)
     key = (_k0(OP_PAGED_ATTENTION, dtype, T, aligned), 0, hd | nq << 16 | nk << 32,
            form << 16 | int(s > 1) << 24, 0, 0)
-    launches = [((PA_ANY, PA_ROWS, PA_TILE)[form], grids[0], block)]
+    launches = [((PA_ANY, PA_ROWS, PA_TILE, PA_PAIR)[form], grids[0], block)]
     if s > 1:
         launches.append((PA_JOIN, grids[1], 256))
     return key, launches

@@ -63,7 +63,7 @@ int be_resolve(int32_t kvariant, uint32_t dtype, int32_t ksub, void **fn) {
     sym = elt_kernel(kvariant, dtype, ksub);
   else if (kvariant == EMB_SCALAR || kvariant == EMB_VEC)
     sym = emb_kernel(kvariant, dtype);
-  else if (kvariant >= KV_SLOTS && kvariant <= PA_JOIN)
+  else if (kvariant >= KV_SLOTS && kvariant <= PA_PAIR)
     sym = paged_kernel(kvariant, dtype, ksub);
   else if (kvariant == EMPTY)
     sym = empty_kernel();

@@ -23,7 +23,7 @@ enum Variant : int32_t {
   ELT_SCALAR = 60, ELT_FLAT = 61, ELT_FLAT_U2 = 62, ELT_ROWS = 63,
   EMB_SCALAR = 70, EMB_VEC = 71,
   KV_SLOTS = 80, KVW_ANY = 82, KVW_VEC = 83,
-  PA_ANY = 90, PA_ROWS = 91, PA_TILE = 92, PA_JOIN = 93,
+  PA_ANY = 90, PA_ROWS = 91, PA_TILE = 92, PA_JOIN = 93, PA_PAIR = 94,
   EMPTY = 99,
 };
 
@@ -167,8 +167,9 @@ Role emb_role(uint32_t dtype, int64_t H, unsigned flags, int64_t T);
 inline bool is_paged_op(uint32_t op) { return op >= TRI_OP_KV_SLOTS && op <= TRI_OP_PAGED_ATTENTION; }
 // How attention computes: any alignment and head size, a wavefront per row; or
 // on the matrix cores, tiles of few rows whose keys the wavefronts share out,
-// or of many rows that the wavefronts share out.
-enum AttnForm : uint32_t { kAttnAny = 0, kAttnRows = 1, kAttnTile = 2 };
+// or of many rows that the wavefronts share out (in pairs: two groups of them
+// share out the keys).
+enum AttnForm : uint32_t { kAttnAny = 0, kAttnRows = 1, kAttnTile = 2, kAttnPair = 3 };
 constexpr int32_t kAttnMatrixHd = 256;     // head sizes of the matrix forms
 // The head size that a matrix kernel holds: hd rounded up to 64, 128 or 256.
 inline int32_t attn_hdp(int32_t hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }

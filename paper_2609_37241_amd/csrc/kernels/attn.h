@@ -487,6 +487,10 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // next keys' loads are in flight during the products, and go to the other half
 // of LDS between them (one barrier a step).
 //
+// With two groups of four wavefronts (PA_PAIR) each takes every other step, on
+// tiles of its own, and the first adds up both: where the tiles are few, a
+// compute unit has two wavefronts a SIMD all the same.
+//
 // The running maximum is the softmax's reference only; it is raised, and what
 // was summed rescaled, when a score passes it by more than 2^8 (a branch that
 // the first step takes and few others): weights up to 256 lose nothing in
@@ -512,20 +516,24 @@ struct TileShape {
 
 constexpr int kAhead = 4;   // products between an operand's read from LDS and its use
 
-template <int DT, int HDP>
+template <int DT, int HDP, int KG>
 __device__ void body_pa_tile(const PagedArgs &a) {
   typedef TileShape<DT, HDP> S;
   constexpr int ES = S::ES, KB = S::KB, NB = S::NB, NQ = S::NQ, ND = S::ND, NP = S::NP;
-  __shared__ __attribute__((aligned(16))) char lds[S::NBUF * S::BUF];
+  constexpr int GROUP = S::NBUF * S::BUF, STEP = KG * KB;
+  __shared__ __attribute__((aligned(16))) char all_lds[KG * GROUP];
   __shared__ int32_t odd_b, odd_e;   // from the first to the last step with infinities or NaN
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // four wavefronts a group; group g takes the steps g, g + KG, ... of the keys
+  const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const int tid = threadIdx.x & 255, lane = tid & 63, wave = tid >> 6;
+  char *lds = all_lds + group * GROUP;
   const int n = lane & 31, half = lane >> 5;
   const uint32_t kh = blockIdx.x % uint32_t(a.nk), rest = blockIdx.x / uint32_t(a.nk);
   const int32_t split = int32_t(rest % uint32_t(a.splits));
   // the last tiles, which see the most keys, first
   const Tile t = find_tile<128>(a, a.tiles - 1 - int32_t(rest / uint32_t(a.splits)));
   if (t.r < 0) return;
-  if (tid == 0) {
+  if (threadIdx.x == 0) {
     odd_b = 0x7FFFFFFF;
     odd_e = 0;
   }
@@ -632,22 +640,25 @@ __device__ void body_pa_tile(const PagedArgs &a) {
 
   uint64_t there = 0;    // `seen` of the step being computed
   int32_t page = 0;
+  const int32_t first = b + group * KB;
   if (b < e) {
-    load(b, look_up(b));
+    if (first < e) load(first, look_up(first));
     __syncthreads();     // odd_b, odd_e are set
-    store(b, 0);
-    there = seen;
-    if (b + KB < e) {
-      page = look_up(b + KB);
-      load(b + KB, page);
-      if (b + 2 * KB < e) page = look_up(b + 2 * KB);
+    if (first < e) {
+      store(first, 0);
+      there = seen;
+      if (first + STEP < e) {
+        page = look_up(first + STEP);
+        load(first + STEP, page);
+        if (first + 2 * STEP < e) page = look_up(first + 2 * STEP);
+      }
     }
     __syncthreads();
   }
   int buf = 0;
-  for (int32_t k0 = b; k0 < e; k0 += KB) {
+  for (int32_t k0 = first; k0 - group * KB < e; k0 += STEP) {
     const char *kl = lds + buf * S::BUF, *vl = kl + KB * S::KS;
-    const bool work = !idle && k0 < w_hi && k0 + KB > w_lo;
+    const bool work = !idle && k0 < e && k0 < w_hi && k0 + KB > w_lo;
     f32x16 st[NB];
     if (work) {
 #pragma unroll
@@ -686,12 +697,12 @@ __device__ void body_pa_tile(const PagedArgs &a) {
     }
     const uint64_t now = there;
     if constexpr (S::NBUF == 2) {
-      if (k0 + KB < e) {
-        store(k0 + KB, buf ^ 1);
+      if (k0 + STEP < e) {
+        store(k0 + STEP, buf ^ 1);
         there = seen;
-        if (k0 + 2 * KB < e) {
-          load(k0 + 2 * KB, page);
-          if (k0 + 3 * KB < e) page = look_up(k0 + 3 * KB);
+        if (k0 + 2 * STEP < e) {
+          load(k0 + 2 * STEP, page);
+          if (k0 + 3 * STEP < e) page = look_up(k0 + 3 * STEP);
         }
       }
     }
@@ -784,17 +795,57 @@ __device__ void body_pa_tile(const PagedArgs &a) {
     __syncthreads();
     if constexpr (S::NBUF == 2) {
       buf ^= 1;
-    } else if (k0 + KB < e) {
-      store(k0 + KB, 0);
-      there = seen;
-      if (k0 + 2 * KB < e) {
-        load(k0 + 2 * KB, page);
-        if (k0 + 3 * KB < e) page = look_up(k0 + 3 * KB);
+    } else {
+      if (k0 + STEP < e) {
+        store(k0 + STEP, 0);
+        there = seen;
+        if (k0 + 2 * STEP < e) {
+          load(k0 + 2 * STEP, page);
+          if (k0 + 3 * STEP < e) page = look_up(k0 + 3 * STEP);
+        }
       }
       __syncthreads();
     }
   }
 
+  l = sum_32(l);
+  if constexpr (KG == 2) {
+    // the second group's sums, lane by lane, through LDS (the last step's
+    // barrier is behind all reads of the tiles)
+    if (b < e) {
+      f32x4 *x = reinterpret_cast<f32x4 *>(all_lds) + wave * (4 * ND * 64) + lane;
+      float *y = reinterpret_cast<float *>(all_lds + 4 * (4 * ND * 64) * 16) + wave * 128 + lane;
+      if (group == 1) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[(4 * d + i) * 64] = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+        y[0] = m;
+        y[64] = l;
+      }
+      __syncthreads();
+      if (group == 0) {
+        const float m1 = y[0], l1 = y[64];
+        const float top = fmaxf(l != 0.0f ? m : kNegInf, l1 != 0.0f ? m1 : kNegInf);
+        const float ts = top == kNegInf ? 0.0f : top;
+        const float f0 = l != 0.0f ? exp2_hw(m - ts) : 0.0f;
+        const float f1 = l1 != 0.0f ? exp2_hw(m1 - ts) : 0.0f;
+        m = top;
+        l = f0 * l + f1 * l1;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 z = x[(4 * d + i) * 64];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              o[d][4 * i + c] = fmaf(f1, z[c], f0 * o[d][4 * i + c]);
+          }
+      }
+    }
+    if (group == 1) return;
+  }
   // (the last step's barrier is behind all of them)
   for (int32_t x = odd_b; b < e && x < odd_e; ++x) {
     const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
@@ -812,7 +863,6 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       }
   }
   if (row >= t.rows) return;
-  l = sum_32(l);
   const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll

@@ -12,7 +12,7 @@ __global__ __launch_bounds__(64 * rows_waves(HDP), 1) void k_pa_rows_f32(PagedAr
 
 template <int HDP>
 __global__ __launch_bounds__(256, HDP == 256 ? 1 : 2) void k_pa_tile_f32(PagedArgs a) {
-  body_pa_tile<kF32, HDP>(a);
+  body_pa_tile<kF32, HDP, 1>(a);
 }
 
 // hdp: the head size rounded up to 64, 128 or 256.

@@ -406,7 +406,8 @@ const void *paged_kernel(int32_t variant, uint32_t dtype, int32_t sub) {
   const bool f32 = dtype == TRI_F32;
   switch (variant) {
     case PA_ROWS:
-    case PA_TILE: return f32 ? attn_kernel_f32(variant, sub) : attn_kernel_bf16(variant, sub);
+    case PA_TILE:
+    case PA_PAIR: return f32 ? attn_kernel_f32(variant, sub) : attn_kernel_bf16(variant, sub);
     case KV_SLOTS: return sym(&k_kv_slots);
     case KVW_ANY: return f32 ? sym(&k_kv_write<kF32, false>) : sym(&k_kv_write<kBF16, false>);
     case KVW_VEC: return f32 ? sym(&k_kv_write<kF32, true>) : sym(&k_kv_write<kBF16, true>);

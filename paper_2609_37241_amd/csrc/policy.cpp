@@ -238,14 +238,21 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
 // float32, whose products cost 16 times as much, gains from full tiles up to
 // 256 rows: 16 requests of 64 / 128 new tokens, 32 and 8 heads of 128 (256 /
 // 512 rows), 233 / 474 us against 287 / 306; one of 64 / 128: 39 / 62 against
-// 51 / 53.
+// 51 / 53. Where the tiles of 128 are at most one a compute unit and the keys
+// many, two groups of wavefronts share the keys (PA_PAIR: 24 requests of up to
+// 3700 keys, 218 tiles: 75.5 -> 52.6 us; 512 tokens behind 8192, 128: 131 ->
+// 107; behind 512: 35.8 and 34.9; with 1024 keys it loses, 45.5 -> 48.1, as
+// not two of its workgroups fit a compute unit).
 //
 // Splits. Few tiles leave compute units idle, so their keys are split until
 // there are `want` workgroups, in runs of at least `run` keys; the join costs
 // 4 us and the traffic of the sums. PA_ROWS wants 1024 (64 requests of up to
 // 8k tokens, where the longest decides: 214 us; 512 workgroups 227, 2048 212)
-// and runs of 1024 (four steps of a workgroup: a request of 500 tokens 10.1 us
-// against 11.5 split in two). PA_TILE wants 256, one a compute unit, rounded
+// and runs of 1024 (six requests in float32, 300 tiles: 23.4 us, runs of 512
+// 26.6); but idle compute units take shorter ones, of 256 (a step of a
+// workgroup takes 2.2 us, the latency of its loads: a request of 32 heads and
+// 2000 tokens 12.4 us against 18.6), from 512 keys on (500 tokens: 10.1 us against 11.5
+// split in two). PA_TILE wants 256, one a compute unit, rounded
 // down (24 requests with a window, 218 workgroups: 48.8 us against 57.7 split
 // in two), and runs of 512 keys (four prompts of up to 1024 tokens, heads of
 // 256: 40 us against 52 split), 256 in float32, whose steps take longer.
@@ -268,11 +275,19 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
     have = (full > busy ? full : busy) * nk;
     want = few ? 1024 : 256;
     run = few ? 1024 : f32 ? 256 : 512;
+    if (!few && !f32 && hd <= 128 && have <= 256 && kv_max >= 2048) {
+      p.form = kAttnPair;
+      p.block = 2 * kBlock;
+    }
     if (few) p.block = uint32_t(64 * rows_waves(attn_hdp(hd)));
   }
-  int64_t s = want / have;
-  const int64_t most = cdiv(kv_max, run);
-  if (s > most) s = most;
+  const auto splits = [&](int64_t wgs, int64_t keys) {
+    const int64_t x = wgs / have, most = cdiv(kv_max, keys);
+    return x < most ? x : most;
+  };
+  int64_t s = splits(want, run);
+  // one workgroup a compute unit, each a step of its wavefronts
+  if (p.form == kAttnRows && kv_max > 512 && splits(256, 256) > s) s = splits(256, 256);
   if (s > TRI_MAX_KV_SPLITS) s = TRI_MAX_KV_SPLITS;
   while (s > 1 && attn_workspace(T, nq, hd, int32_t(s)) > workspace) --s;
   p.splits = s < 1 ? 1 : int32_t(s);
@@ -348,7 +363,8 @@ static bool paged_key_valid(const Key &k) {
   if (k.k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
   const bool matrix = (key_flags(k) & kAlign) && int32_t(hd) <= kAttnMatrixHd &&
                       hd % uint32_t(vec_elems(key_dtype(k))) == 0;
-  return matrix ? form == kAttnRows || form == kAttnTile : form == kAttnAny;
+  if (form == kAttnPair && (key_dtype(k) == TRI_F32 || hd > 128)) return false;
+  return matrix ? form >= kAttnRows && form <= kAttnPair : form == kAttnAny;
 }
 
 // A key the entry points could have produced (used to check imported keys):
@@ -461,6 +477,7 @@ Plan plan_for_key(const Key &k) {
     case TRI_OP_PAGED_ATTENTION:
       p.variant = p.kvariant[0] = key_attn_form(k) == kAttnRows   ? PA_ROWS
                                   : key_attn_form(k) == kAttnTile ? PA_TILE
+                                  : key_attn_form(k) == kAttnPair ? PA_PAIR
                                                                   : PA_ANY;
       if (p.variant != PA_ANY) p.ksub[0] = attn_hdp(int32_t(key_hd(k)));
       p.n_launches = 1;

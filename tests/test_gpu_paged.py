@@ -303,8 +303,22 @@ def tile_problem(dtype, lens, nq, nk, hd, page=16, **kw):
 
 
 def tile_check(cache, p, dtype, window=0, **kw):
+    """The result of the form that many rows take: with more than 2048 keys in
+    sight (the bound the host knows) and heads of up to 128 in bf16 two groups
+    of wavefronts share them out, else one does. Both are compared where both
+    can be had: rows of nobody make the tiles too many for the first."""
     got = attend(cache, p, window=window, **kw)
-    assert cache.last_selection().variant == P.PA_TILE
+    assert cache.last_selection().variant in (P.PA_TILE, P.PA_PAIR)
+    if "out" in kw:
+        return got
+    T, nq, hd = p["q"].shape
+    nk, dev = p["kc"].shape[2], p["q"].device
+    rows = (256 // nk + 1) * 128 * nk // nq + 1
+    q = torch.cat([p["q"], torch.zeros((rows, nq, hd), dtype=p["q"].dtype, device=dev)])
+    many = attend(cache, dict(p, q=q), window=window)
+    assert cache.last_selection().variant == P.PA_TILE and (f64(many[T:]) == 7.0).all()
+    if cache.last_selection().n_launches == 1:
+        check(many[:T], oracle(p, window), dtype)
     return got
 
 

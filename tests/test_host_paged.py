@@ -249,7 +249,7 @@ def test_attention_selection(lib, fresh):
     h = fresh(4096)
     r = random.Random(2)
     forms = set()
-    for _ in range(1500):
+    for _ in range(6000):
         dt, nk = r.choice([0, 1]), r.choice([1, 2, 8])
         nq, hd = nk * r.choice([1, 4, 5, 40]), r.choice([1, 20, 64, 80, 128, 256, 320, 512])
         R = r.choice([1, 2, 16, 300, 4096])
@@ -278,7 +278,7 @@ def test_attention_selection(lib, fresh):
         key, want = P.attention_selection(dt, T, R, nq, nk, hd, aligned, keys, given)
         got = last(lib, h)
         assert tuple(got.key) == key and launches(got) == want
-    assert len(forms) == 6       # every form, split and not
+    assert forms == {(f, s) for f in range(4) for s in (False, True)}
 
 
 def read_args(lib, n):
@@ -385,8 +385,8 @@ def test_keys_export_and_import(lib, fresh):
     assert lib.tri_paged_attention(g, C.byref(attn()), None) == 0
     bad = {0: [(0, 1 << 8), (0, 1 << 24), (0, 1 << 25), (1, 1), (2, 1), (3, 1 << 16)],
            1: [(0, 1 << 25), (0, 1 << 40), (1, 5), (2, 1 << 16), (2, 1 << 60), (3, 1)],
-           # 9 query heads over 2; form 0 of aligned rows (1 becomes 2 with 3 << 16: valid)
-           2: [(0, 1 << 25), (2, 1 << 16), (3, 1 << 16), (3, 1 << 32), (3, 1), (4, 1), (5, 1)]}
+           # 9 query heads over 2; forms 0 and 5 of aligned rows
+           2: [(0, 1 << 25), (2, 1 << 16), (3, 1 << 16), (3, 1 << 18), (3, 1 << 32), (3, 1), (4, 1), (5, 1)]}
     for i, changes in bad.items():
         for word, bit in changes:
             k = list(buf[6 * i:6 * i + 6])
