@@ -256,7 +256,11 @@ __device__ void body_pa_rows(const PagedArgs &a) {
   // where the lane's key lies (the pool's first page for one that is not
   // there), handed to the lanes that load its row
   const int srow = lane / S::CH, sbyte = (lane % S::CH) * 16;
-  const bool inside = sbyte < hdb, one_layout = a.k.ps == a.v.ps && a.k.ss == a.v.ss;
+  const bool one_layout = a.k.ps == a.v.ps && a.k.ss == a.v.ss;
+  // behind the head's end a lane loads the first vector and clears it on the
+  // way to LDS: loads under a mask measured 2-7 % more
+  const bool padded = hdb < HDP * ES, inside = sbyte < hdb;
+  const int lbyte = inside ? sbyte : 0;
   int64_t ko, vo;
   uint64_t seen = 0;      // bit i: key k0 + i is there
   const auto rows_of = [&](int32_t k0, int32_t page) {
@@ -271,22 +275,30 @@ __device__ void body_pa_rows(const PagedArgs &a) {
     if (!one_layout) vo = (id * a.v.ps + in * a.v.ss) * ES;
   };
   u32x4 k[S::NP], v[S::NP];
-#pragma unroll
-  for (int i = 0; i < S::NP; ++i) k[i] = v[i] = u32x4{0, 0, 0, 0};
   const auto load = [&](u32x4(&x)[S::NP], const char *p, int64_t at) {
     int64_t r[S::NP];
 #pragma unroll
     for (int i = 0; i < S::NP; ++i) r[i] = __shfl(at, srow + S::RP * i);
-    if (!inside) return;
-    if (a.stream) {
+    if (a.stream) {   // (the empty asm keeps the compiler from making one of the two)
+      asm volatile("" ::: "memory");
 #pragma unroll
       for (int i = 0; i < S::NP; ++i)
-        x[i] = ld16<true>(reinterpret_cast<const u32x4 *>(p + r[i] + sbyte));
+        x[i] = ld16<true>(reinterpret_cast<const u32x4 *>(p + r[i] + lbyte));
+      asm volatile("" ::: "memory");
     } else {
 #pragma unroll
       for (int i = 0; i < S::NP; ++i)
-        x[i] = ld16<false>(reinterpret_cast<const u32x4 *>(p + r[i] + sbyte));
+        x[i] = ld16<false>(reinterpret_cast<const u32x4 *>(p + r[i] + lbyte));
     }
+  };
+  const auto to_lds = [&](u32x4(&x)[S::NP], int stride) {
+    if (padded)
+#pragma unroll
+      for (int i = 0; i < S::NP; ++i)
+        if (!inside) x[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < S::NP; ++i)
+      *reinterpret_cast<u32x4 *>(vl + (srow + S::RP * i) * stride + sbyte) = x[i];
   };
 
   const auto sees = [&](int32_t key) { return key >= my_lo && key < my_hi; };
@@ -301,9 +313,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
   for (; k0 < e; k0 += NW * KB) {
     const bool more = k0 + NW * KB < e;
     const uint64_t there = seen;
-#pragma unroll
-    for (int i = 0; i < S::NP; ++i)
-      *reinterpret_cast<u32x4 *>(vl + (srow + S::RP * i) * S::KS + sbyte) = k[i];
+    to_lds(k, S::KS);
     if (more) {
       rows_of(k0 + NW * KB, page);
       load(k, kp, ko);
@@ -346,9 +356,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
         odd_e = k1;
       }
     }
-#pragma unroll
-    for (int i = 0; i < S::NP; ++i)
-      *reinterpret_cast<u32x4 *>(vl + (srow + S::RP * i) * S::VS + sbyte) = v[i];
+    to_lds(v, S::VS);
     if (more) {
       load(v, vp, vo);
       if (k0 + 2 * NW * KB < e) page = look_up(k0 + 2 * NW * KB);
