@@ -522,8 +522,8 @@ tri_status tri_embedding(tri_cache *cache, tri_dtype dtype, const void *table, i
                          void *out, int64_t o_rs, int64_t T, int64_t H, void *stream);
 
 /* ---- the paged KV cache of a serving step (not in the paper: what stands
- * between the RoPE and the output projection of a decode step; vLLM-style
- * pages). A step of R requests calls tri_kv_slots once, then for each layer
+ * between the RoPE and the output projection of a decode step: pages of a fixed
+ * number of slots, a table of pages for each request). A step of R requests calls tri_kv_slots once, then for each layer
  * tri_kv_write after the RoPE and tri_paged_attention. Same cache of versions,
  * same guards (op, dtype, head layout, token bucket, 16-byte alignment;
  * attention also its form and whether it splits the keys).
@@ -548,7 +548,7 @@ tri_status tri_embedding(tri_cache *cache, tri_dtype dtype, const void *table, i
  *     the next call's stack (free_count is clamped to [0, n_free]).
  * The outputs must not overlap each other or an input (kv_len, free_count and
  * free_pages are read while they are written); the table row stride is at
- * least cols. cols * page must be below 2^31, page 1..TRI_MAX_PAGE. All
+ * least cols. cols * page and R * cols must be below 2^31, page 1..TRI_MAX_PAGE. All
  * pointers 4-byte aligned, slots 8. T may be 0 (slots and pos are then not
  * used): lengths and pages are done all the same. */
 tri_status tri_kv_slots(tri_cache *cache, const tri_kv_slots_args *args, void *stream);
@@ -583,7 +583,7 @@ tri_status tri_kv_write(tri_cache *cache, tri_dtype dtype, const void *k, int64_
  * than workspace_bytes allows: with NULL or 0 it does not split.
  * tri_paged_attention_workspace gives what the call would use. max_kv only
  * steers the split; a wrong one costs time, not correctness.
- * hd 1..512; nq 1..4096; T * nq below 2^31; cols * page below 2^31; scale
+ * hd 1..512; nq 1..4096; T * nq below 2^31; cols * page at most 2^31 - 4096; scale
  * finite; window, max_kv >= 0. A call whose tiles need 2^32 work-items or more
  * is UNSUPPORTED (not below T * nq = 2^26 and R * nk = 2^22). */
 tri_status tri_paged_attention(tri_cache *cache, const tri_attention_args *args, void *stream);

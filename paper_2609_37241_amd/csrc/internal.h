@@ -55,6 +55,8 @@ constexpr unsigned kChainQkNorm = 0x40;        // chain key flag: QK-RMSNorm bef
 // The paged KV cache.
 constexpr int32_t kAttnHdMax = 512;        // head sizes of kv_write and attention
 constexpr int64_t kPosLimit = int64_t(1) << 31;   // positions and rows * heads are below this
+// keys of a request in attention: its loops step up to 1536 keys beyond the end
+constexpr int64_t kKeysMax = kPosLimit - 4096;
 
 // ---- key --------------------------------------------------------------------------
 // k0: op | dtype << 8 | bucket << 16 | flags << 24 | RoPE base bits << 32

@@ -68,9 +68,10 @@ int attn_check(const tri_attention_args &a, bool pointers) {
     if (st != kGo) return st;
   } else if (a.R < 1 || a.cols < 1 || a.kv.page < 1 || a.kv.nk < 1 || a.kv.hd < 1 ||
              a.R > TRI_MAX_REQUESTS || a.kv.page > TRI_MAX_PAGE || a.kv.nk > kHeadsMax ||
-             a.kv.hd > kAttnHdMax || int64_t(a.cols) * a.kv.page >= kPosLimit) {
+             a.kv.hd > kAttnHdMax) {
     return TRI_E_INVALID;
   }
+  if (int64_t(a.cols) * a.kv.page > kKeysMax) return TRI_E_UNSUPPORTED;
   if (a.nq < 1) return TRI_E_INVALID;
   if (a.nq > kHeadsMax || a.T * a.nq >= kPosLimit) return TRI_E_UNSUPPORTED;
   if (a.nq % a.kv.nk) return TRI_E_INVALID;
@@ -151,6 +152,7 @@ tri_status tri_kv_slots(tri_cache *c, const tri_kv_slots_args *p, void *stream) 
   if (st != kGo && a.T != 0) return finish_early(c, op, st);
   st = check_table(a.table, a.table_rs, a.R, a.cols, a.page);
   if (st != kGo) return finish_early(c, op, st);
+  if (int64_t(a.R) * a.cols >= kPosLimit) return finish_early(c, op, TRI_E_UNSUPPORTED);
   if (a.n_free < 0 || !a.kv_len || !a.new_len || !a.free_count || (a.n_free && !a.free_pages) ||
       (a.T && (!a.slots || !a.pos)) || !a.q_start || !a.kv_len_out || !a.free_out)
     return finish_early(c, op, TRI_E_INVALID);

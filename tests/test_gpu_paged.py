@@ -282,6 +282,22 @@ def test_attention_offsets_beyond_32_bits(cache):
     assert torch.equal(p["kc"][-1, 15], k[0]) and torch.equal(p["vc"][far - 1, 0], -k[2])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,hd,window", [(1, 64, 300), (1, 64, 3000), (1, 20, 300), (150, 64, 300),
+                                         (150, 64, 2100), (150, 128, 2100)])
+def test_attention_at_the_last_position(cache, dtype, n, hd, window):
+    """2^31 - 4096 keys, the most a request can have, all but the last 3200 in
+    one page: a window sees what it sees in those alone."""
+    page, far = 16, 200
+    p = problem(dtype, [(far * page, n)], 8, 1, hd, page)
+    want = oracle(p, window)
+    cols = (1 << 27) - 256
+    table = torch.full((1, cols), -1, dtype=torch.int32, device=DEV)
+    table[0, cols - far:] = p["table"][0, :far]
+    p["table"], p["kv_len"] = table, i32([cols * page])
+    check(attend(cache, p, window), want, dtype)
+
+
 # ---- tiles of many rows: every case of these is served by them ------------------------------
 TILE_HEADS = [("bf16", 8, 1, 128), ("bf16", 5, 1, 80), ("bf16", 16, 1, 64), ("bf16", 6, 1, 256),
               ("bf16", 10, 2, 96), ("bf16", 33, 3, 72), ("bf16", 130, 1, 8), ("f32", 20, 1, 64),

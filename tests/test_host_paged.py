@@ -93,6 +93,8 @@ SLOT_REFUSALS = [
     (dict(kv_len_out=at(1)), INVALID), (dict(free_out=at(5)), INVALID),
     (dict(free_count=at(10, 4)), INVALID), (dict(pos=at(6, 60)), INVALID),
     (dict(table=at(4, 8)), INVALID), (dict(q_start=at(9, 8)), INVALID),
+    # 2^31 entries: the running sum of new pages is 32 bits
+    (dict(R=4096, page=1, cols=1 << 19, table_rs=1 << 19), UNSUPPORTED),
 ]
 
 
@@ -185,6 +187,9 @@ ATTN_REFUSALS = [
     (dict(scale=float("nan")), INVALID), (dict(window=-1), INVALID), (dict(max_kv=-1), INVALID),
     (dict(workspace_bytes=-1), INVALID), (dict(workspace_bytes=64), INVALID),
     (dict(workspace=at(30, 8), workspace_bytes=64), INVALID),
+    # 2^31 - 4095 .. 2^31 - 1 keys: the step behind the last one would wrap
+    (dict(cols=(1 << 27) - 1, table_rs=1 << 27), UNSUPPORTED),
+    (dict(cols=(1 << 27) - 255, table_rs=1 << 27), UNSUPPORTED),
 ]
 
 
@@ -201,10 +206,13 @@ def test_attention_edges(lib, fresh):
     assert lib.tri_paged_attention(h, None, None) == INVALID
     assert lib.tri_paged_attention_workspace(None) == 0
     assert lib.tri_paged_attention_workspace(C.byref(attn(nq=7))) == 0
+    assert lib.tri_paged_attention_workspace(C.byref(attn(cols=(1 << 27) - 255))) == 0
     empty = L.AttentionArgs(dtype=L.F32, T=0)
     assert lib.tri_paged_attention(h, C.byref(empty), None) == 0
     assert lib.tri_paged_attention_workspace(C.byref(empty)) == 0
     assert lib.trifake_launch_count() == 0
+    most = attn(cols=(1 << 27) - 256, table_rs=1 << 27)
+    assert lib.tri_paged_attention(h, C.byref(most), None) == 0
 
 
 def test_attention_beyond_a_launch(lib, fresh):
