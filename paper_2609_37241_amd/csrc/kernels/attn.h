@@ -323,6 +323,9 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 #pragma unroll
     for (int j = 0; j < MB; ++j) {
       st[j] = f32x4{0, 0, 0, 0};
+      // (float32: four sums side by side, whose rounding errors stay half those
+      // of one sum four times as long)
+      f32x4 sum[4] = {};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const u32x4 x = *reinterpret_cast<const u32x4 *>(vl + (16 * j + n) * S::KS + quarter * 16 +
@@ -330,14 +333,15 @@ __device__ void body_pa_rows(const PagedArgs &a) {
         if constexpr (DT == kF32) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            st[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[i]),
-                                                         __uint_as_float(q[s][i]), st[j], 0, 0, 0);
+            sum[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[i]),
+                                                          __uint_as_float(q[s][i]), sum[i], 0, 0, 0);
         } else {
           st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
                                                           __builtin_bit_cast(bf16x8, q[s]), st[j],
                                                           0, 0, 0);
         }
       }
+      if constexpr (DT == kF32) st[j] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
     // V in K's place; rows that are not there are zero, so that no weight of 0
     // meets a NaN

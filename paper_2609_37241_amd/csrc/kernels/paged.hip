@@ -241,8 +241,14 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
         vo = slot_offset(table, uint32_t(key), a, a.v);
       }
       if (ko >= 0) {
-        float dot = 0.0f;
-        for (int d = 0; d < a.hd; ++d) dot = fmaf(qs[wave][d], Elt<DT>::ld(kp + ko * ES, d), dot);
+        float x[4] = {};   // four sums: shorter chains, smaller errors
+        int d = 0;
+        for (; d + 4 <= a.hd; d += 4)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[i] = fmaf(qs[wave][d + i], Elt<DT>::ld(kp + ko * ES, d + i), x[i]);
+        for (; d < a.hd; ++d) x[0] = fmaf(qs[wave][d], Elt<DT>::ld(kp + ko * ES, d), x[0]);
+        const float dot = (x[0] + x[1]) + (x[2] + x[3]);
         sc = a.flip ? -dot : dot;
       }
       const uint64_t seen = __ballot(ko >= 0);
