@@ -183,7 +183,10 @@ __device__ inline void store4(const PagedArgs &a, int32_t token, int32_t head, i
 // until its step begins, and the pages of the step after are looked up
 // meanwhile. Read in the order of the first product's operand instead, 64
 // bytes of 16 rows a load, 1 GiB came at 6.35 TB/s, in whole rows at 6.95
-// (nontemporal; 6.1 and 6.2 without).
+// (nontemporal; 6.1 and 6.2 without). 64 requests of 8192 keys, 8 K heads of 128
+// in bf16 (2.1 GB), 342 us with the join, 6.3 TB/s; of up to 8192, 193 us, 5.55
+// TB/s: the longest splits end last. Four wavefronts take as long (500 keys: 10.0
+// -> 11.7 us); two steps in flight do not fit the registers (252 us).
 template <int DT, int HDP>
 struct RowsShape {
   static constexpr int ES = Elt<DT>::ES;
@@ -497,7 +500,10 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // instructions and the 32 KiB of LDS that a wavefront reads for them each cost
 // about as much, so two workgroups a compute unit fill each other's gaps. The
 // next keys' loads are in flight during the products, and go to the other half
-// of LDS between them (one barrier a step).
+// of LDS between them (one barrier a step). 2048 rows behind 6144 keys, 32 + 8
+// heads of 128 in bf16: 277 to 297 us, 811 to 871 TFLOP/s by box; the matrix pipes
+// are busy for 37 % of it. Heads of 256, one wavefront a SIMD: a step of 32 keys
+// takes 1.2 us (of 64 the registers spill, 40 -> 48 us in all).
 //
 // With two groups of four wavefronts (PA_PAIR) each takes every other step, on
 // tiles of its own, and the first adds up both: where the tiles are few, a

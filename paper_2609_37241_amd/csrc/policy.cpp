@@ -247,7 +247,8 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
 // Splits. Few tiles leave compute units idle, so their keys are split until
 // there are `want` workgroups, in runs of at least `run` keys; the join costs
 // 4 us and the traffic of the sums. PA_ROWS wants 1024 (64 requests of up to
-// 8k tokens, where the longest decides: 214 us; 512 workgroups 227, 2048 212)
+// 8k tokens, where the longest decides, read without streaming: 214 us; 512
+// workgroups 227, 2048 212; streamed 193 and 193 to 200)
 // and runs of 1024 (six requests in float32, 300 tiles: 23.4 us, runs of 512
 // 26.6); but idle compute units take shorter ones, of 256 (a step of a
 // workgroup takes 2.2 us, the latency of its loads: a request of 32 heads and
