@@ -158,7 +158,7 @@ def attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
         have = max(_cdiv(T * g, m), min(R, T)) * nk
         want, run = (1024, 1024) if small else (256, 512 if dtype else 256)
         block = (256 if hd > 128 else 512) if small else 256
-        if form == 2 and dtype and hd <= 128 and have <= 256 and kv_max >= 2048:
+        if form == 2 and dtype and hd <= 128 and have <= 224:
             form, block = 3, 512
     s = min(want // have, _cdiv(kv_max, run))
     if form == 1 and kv_max > 512:

@@ -70,6 +70,14 @@ __device__ inline float sum_16_32(float x) {
   return sum_32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// The bits of `seen` (bit i: key k0 + i) whose keys are in [lo, hi).
+__device__ inline uint64_t in_range(uint64_t seen, int32_t k0, int32_t lo, int32_t hi) {
+  const int32_t a = clamp_i32(lo - k0, 0, 64), b = clamp_i32(hi - k0, 0, 64);
+  const uint64_t below_b = b == 64 ? ~uint64_t(0) : (uint64_t(1) << b) - 1;
+  const uint64_t below_a = a == 64 ? ~uint64_t(0) : (uint64_t(1) << a) - 1;
+  return seen & below_b & ~below_a;
+}
+
 // Clears the infinities and NaN of a vector; whether there were any.
 template <int DT>
 __device__ inline bool clear_not_finite(u32x4 &v) {
@@ -369,17 +377,19 @@ __device__ void body_pa_rows(const PagedArgs &a) {
       if (k0 + 2 * NW * KB < e) page = look_up(k0 + 2 * NW * KB);
     }
     // softmax: the lane's keys are k0 + 16 j + 4 quarter + i
+    if (partial) {
+      const uint32_t see = uint32_t(in_range(there, k0, my_lo, my_hi) >> (4 * quarter));
+#pragma unroll
+      for (int j = 0; j < MB; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          st[j][i] = (see >> (16 * j + i)) & 1 ? st[j][i] : kNegInf;
+    }
     float top = kNegInf;
 #pragma unroll
     for (int j = 0; j < MB; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (partial) {
-          const int32_t x = 16 * j + 4 * quarter + i;
-          if (!((there >> x) & 1) || !sees(k0 + x)) st[j][i] = kNegInf;
-        }
-        top = fmaxf(top, st[j][i]);
-      }
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, st[j][i]);
     top = max_16_32(top);
     const float mn = fmaxf(m, top == kNegInf ? kNegInf : top * a.scale);
     const float ms = mn == kNegInf ? 0.0f : mn;
@@ -501,9 +511,10 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // about as much, so two workgroups a compute unit fill each other's gaps. The
 // next keys' loads are in flight during the products, and go to the other half
 // of LDS between them (one barrier a step). 2048 rows behind 6144 keys, 32 + 8
-// heads of 128 in bf16: 277 to 297 us, 811 to 871 TFLOP/s by box; the matrix pipes
-// are busy for 37 % of it. Heads of 256, one wavefront a SIMD: a step of 32 keys
-// takes 1.2 us (of 64 the registers spill, 40 -> 48 us in all).
+// heads of 128 in bf16: 269 to 280 us, 858 to 893 TFLOP/s by box; the matrix pipes
+// are busy for 37 % of it. Heads of 256 leave one workgroup a compute unit: four
+// prompts of up to 1024 tokens, 16 heads, 29.6 us; 2048 tokens behind 2048, 203
+// us, 508 TFLOP/s (with steps of 32 keys 31.2 and 219).
 //
 // With two groups of four wavefronts (PA_PAIR) each takes every other step, on
 // tiles of its own, and the first adds up both: where the tiles are few, a
@@ -516,7 +527,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 template <int DT, int HDP>
 struct TileShape {
   static constexpr int ES = Elt<DT>::ES;
-  static constexpr int KB = DT == kF32 || HDP > 128 ? 32 : 64;
+  static constexpr int KB = DT == kF32 ? 32 : 64;
   static constexpr int NB = KB / 32;
   static constexpr int NQ = HDP * ES / 32;                // 16-byte vectors of a lane's query
   static constexpr int ND = HDP / 32;
@@ -526,7 +537,6 @@ struct TileShape {
   static constexpr int KS = HDP * ES + 16;
   static constexpr int VS = HDP * ES + (DT == kF32 ? 32 : 64);
   static constexpr int BUF = KB * (KS + VS);
-  static constexpr int NBUF = BUF <= 40 * 1024 ? 2 : 1;
   static constexpr int CH = HDP * ES / 16;                // vectors of a row
   static constexpr int RP = 256 / CH;                     // rows that a pass stages
   static constexpr int NP = KB / RP;
@@ -538,7 +548,7 @@ template <int DT, int HDP, int KG>
 __device__ void body_pa_tile(const PagedArgs &a) {
   typedef TileShape<DT, HDP> S;
   constexpr int ES = S::ES, KB = S::KB, NB = S::NB, NQ = S::NQ, ND = S::ND, NP = S::NP;
-  constexpr int GROUP = S::NBUF * S::BUF, STEP = KG * KB;
+  constexpr int GROUP = 2 * S::BUF, STEP = KG * KB;
   __shared__ __attribute__((aligned(16))) char all_lds[KG * GROUP];
   __shared__ int32_t odd_b, odd_e;   // from the first to the last step with infinities or NaN
   // four wavefronts a group; group g takes the steps g, g + KG, ... of the keys
@@ -714,14 +724,12 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       __builtin_amdgcn_s_setprio(0);
     }
     const uint64_t now = there;
-    if constexpr (S::NBUF == 2) {
-      if (k0 + STEP < e) {
-        store(k0 + STEP, buf ^ 1);
-        there = seen;
-        if (k0 + 2 * STEP < e) {
-          load(k0 + 2 * STEP, page);
-          if (k0 + 3 * STEP < e) page = look_up(k0 + 3 * STEP);
-        }
+    if (k0 + STEP < e) {
+      store(k0 + STEP, buf ^ 1);
+      there = seen;
+      if (k0 + 2 * STEP < e) {
+        load(k0 + 2 * STEP, page);
+        if (k0 + 3 * STEP < e) page = look_up(k0 + 3 * STEP);
       }
     }
     if (work) {
@@ -746,13 +754,12 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       const int32_t k1 = k0 + KB < e ? k0 + KB : e;
       const bool mixed = k0 < w_all_lo || k1 > w_all_hi;
       if (mixed || now != ~uint64_t(0)) {
+        const uint64_t see = in_range(now, k0, my_lo, my_hi) >> (4 * half);
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int32_t x = 32 * j + 8 * (i / 4) + 4 * half + i % 4;
-            if (!((now >> x) & 1) || !sees(k0 + x)) st[j][i] = kNegInf;
-          }
+          for (int i = 0; i < 16; ++i)
+            st[j][i] = (uint32_t(see >> (32 * j)) >> (8 * (i / 4) + i % 4)) & 1 ? st[j][i] : kNegInf;
       }
       float top = kNegInf;
 #pragma unroll
@@ -767,7 +774,12 @@ __device__ void body_pa_tile(const PagedArgs &a) {
         m = mn;
         l *= alpha;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] *= alpha;
+        for (int d = 0; d < ND; ++d) {
+          // (these sums live in accumulation registers; without this they
+          // are copied at every step, before the branch)
+          if constexpr (HDP > 128) asm volatile("" : "+a"(o[d]));
+          o[d] *= alpha;
+        }
       }
       const float ms = m == kNegInf ? 0.0f : m;
       // O^T, product i: elements 32 (i % ND) .. of V at keys 16 (i / ND) .. (bf16;
@@ -811,19 +823,7 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       __builtin_amdgcn_s_setprio(0);
     }
     __syncthreads();
-    if constexpr (S::NBUF == 2) {
-      buf ^= 1;
-    } else {
-      if (k0 + STEP < e) {
-        store(k0 + STEP, 0);
-        there = seen;
-        if (k0 + 2 * STEP < e) {
-          load(k0 + 2 * STEP, page);
-          if (k0 + 3 * STEP < e) page = look_up(k0 + 3 * STEP);
-        }
-      }
-      __syncthreads();
-    }
+    buf ^= 1;
   }
 
   l = sum_32(l);

@@ -231,32 +231,33 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
 // PA_ANY. Tiles of 16 rows (PA_ROWS) serve decode, and chunks whose tiles of
 // 128 would be few or mostly empty; rpr: rows of a request and K head, were the
 // requests equal. bf16: 16 requests behind 1000 tokens, 32 query and 8 K heads
-// of 128, 2 / 4 / 8 new tokens each (8 / 16 / 32 rows): 24 / 26 / 38 us against
-// PA_TILE's 25 / 28 / 28; one request, 8 + 8 heads, 32 / 128 / 256 new tokens
-// (16 / 64 / 128 tiles of 16 in all): 12 / 18 / 28 against 20 / 26 / 27, but
+// of 128, 2 / 4 / 8 new tokens each (8 / 16 / 32 rows): 24 / 27 / 38 us against
+// tiles' 25 / 28 / 23; one request, 8 + 8 heads, 32 / 128 / 256 new tokens
+// (16 / 64 / 128 tiles of 16 in all): 12 / 13 / 28 against 20 / 26 / 21, but
 // each tile of 16 reads all keys, so this holds for short contexts only.
 // float32, whose products cost 16 times as much, gains from full tiles up to
 // 256 rows: 16 requests of 64 / 128 new tokens, 32 and 8 heads of 128 (256 /
-// 512 rows), 233 / 474 us against 287 / 306; one of 64 / 128: 39 / 62 against
-// 51 / 53. Where the tiles of 128 are at most one a compute unit and the keys
-// many, two groups of wavefronts share the keys (PA_PAIR: 24 requests of up to
-// 3700 keys, 218 tiles: 75.5 -> 52.6 us; 512 tokens behind 8192, 128: 131 ->
-// 107; behind 512: 35.8 and 34.9; with 1024 keys it loses, 45.5 -> 48.1, as
-// not two of its workgroups fit a compute unit).
+// 512 rows), 253 / 474 us against 287 / 304; one of 64 / 128: 39 / 62 against
+// 51 / 53. Where the tiles of 128 leave some compute units without one, two
+// groups of wavefronts share a tile's keys (PA_PAIR, which fills a unit's LDS:
+// 24 requests of up to 3700 keys, 218 tiles: 74.6 -> 52.7 us; 512 tokens behind
+// 8192, 128: 130 -> 104; 12 requests of 64 behind 1000, 192: 43 -> 30; 700
+// alone, 176: 24.7 -> 21.0); with a tile for every unit some get two (16 of 64
+// behind 1000, 256: 43.8 -> 54.4).
 //
 // Splits. Few tiles leave compute units idle, so their keys are split until
 // there are `want` workgroups, in runs of at least `run` keys; the join costs
 // 4 us and the traffic of the sums. PA_ROWS wants 1024 (64 requests of up to
 // 8k tokens, where the longest decides, read without streaming: 214 us; 512
 // workgroups 227, 2048 212; streamed 193 and 193 to 200)
-// and runs of 1024 (six requests in float32, 300 tiles: 23.4 us, runs of 512
-// 26.6); but idle compute units take shorter ones, of 256 (a step of a
+// and runs of 1024 (six requests in float32, 300 tiles: 22.6 us, runs of 512
+// about 3 more); but idle compute units take shorter ones, of 256 (a step of a
 // workgroup takes 2.2 us, the latency of its loads: a request of 32 heads and
 // 2000 tokens 12.4 us against 18.6), from 512 keys on (500 tokens: 10.1 us against 11.5
 // split in two). PA_TILE wants 256, one a compute unit, rounded
-// down (24 requests with a window, 218 workgroups: 48.8 us against 57.7 split
+// down (24 requests with a window, 218 workgroups: 42.5 us against 61.8 split
 // in two), and runs of 512 keys (four prompts of up to 1024 tokens, heads of
-// 256: 40 us against 52 split), 256 in float32, whose steps take longer.
+// 256: 29.6 us against 42.8 split), 256 in float32, whose steps take longer.
 AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                    bool aligned, int64_t kv_max, uint64_t workspace) {
   AttnPlan p{};
@@ -276,7 +277,7 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
     have = (full > busy ? full : busy) * nk;
     want = few ? 1024 : 256;
     run = few ? 1024 : f32 ? 256 : 512;
-    if (!few && !f32 && hd <= 128 && have <= 256 && kv_max >= 2048) {
+    if (!few && !f32 && hd <= 128 && have <= 224) {
       p.form = kAttnPair;
       p.block = 2 * kBlock;
     }
