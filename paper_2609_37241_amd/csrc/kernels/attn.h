@@ -512,7 +512,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // next keys' loads are in flight during the products, and go to the other half
 // of LDS between them (one barrier a step). 2048 rows behind 6144 keys, 32 + 8
 // heads of 128 in bf16: 269 to 280 us, 858 to 893 TFLOP/s by box; the matrix pipes
-// are busy for 37 % of it. Heads of 256 leave one workgroup a compute unit: four
+// are busy for 41 % of it. Heads of 256 leave one workgroup a compute unit: four
 // prompts of up to 1024 tokens, 16 heads, 29.6 us; 2048 tokens behind 2048, 203
 // us, 508 TFLOP/s (with steps of 32 keys 31.2 and 219).
 //
