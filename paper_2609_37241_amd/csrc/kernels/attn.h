@@ -513,8 +513,8 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // of LDS between them (one barrier a step). 2048 rows behind 6144 keys, 32 + 8
 // heads of 128 in bf16: 269 to 280 us, 858 to 893 TFLOP/s by box; the matrix pipes
 // are busy for 41 % of it. Heads of 256 leave one workgroup a compute unit: four
-// prompts of up to 1024 tokens, 16 heads, 29.6 us; 2048 tokens behind 2048, 203
-// us, 508 TFLOP/s (with steps of 32 keys 31.2 and 219).
+// prompts of up to 1024 tokens, 16 heads, 28.8 us; 2048 tokens behind 2048, 195
+// us, 530 TFLOP/s (with steps of 32 keys 8 % more).
 //
 // With two groups of four wavefronts (PA_PAIR) each takes every other step, on
 // tiles of its own, and the first adds up both: where the tiles are few, a
@@ -608,7 +608,9 @@ __device__ void body_pa_tile(const PagedArgs &a) {
 
   // staging: this work-item's vector of rows srow + RP i
   const int srow = tid / S::CH, sbyte = (tid % S::CH) * 16;
-  const bool inside = sbyte < hdb;
+  // (behind the head's end as in PA_ROWS)
+  const bool padded = hdb < HDP * ES, inside = sbyte < hdb;
+  const int lbyte = inside ? sbyte : 0;
   // the page of key k0 + lane % KB (beyond the end: the last key's)
   const auto look_up = [&](int32_t k0) {
     const int32_t key = k0 + (lane & (KB - 1));
@@ -617,8 +619,6 @@ __device__ void body_pa_tile(const PagedArgs &a) {
   u32x4 sk[NP], sv[NP];
   uint64_t seen = 0;     // bit i: key k0 + i of the staged step is there
   const bool one_layout = a.k.ps == a.v.ps && a.k.ss == a.v.ss;
-#pragma unroll
-  for (int i = 0; i < NP; ++i) sk[i] = sv[i] = u32x4{0, 0, 0, 0};
   const auto load = [&](int32_t k0, int32_t page) {
     // where the lane's key lies (the pool's first page for one that is not
     // there), handed to the lanes that load its row
@@ -637,12 +637,10 @@ __device__ void body_pa_tile(const PagedArgs &a) {
     if (!one_layout)
 #pragma unroll
       for (int i = 0; i < NP; ++i) vr[i] = __shfl(vo, srow + S::RP * i);
-    if (inside) {
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        sk[i] = *reinterpret_cast<const u32x4 *>(kp + kr[i] + sbyte);
-        sv[i] = *reinterpret_cast<const u32x4 *>(vp + vr[i] + sbyte);
-      }
+    for (int i = 0; i < NP; ++i) {
+      sk[i] = *reinterpret_cast<const u32x4 *>(kp + kr[i] + lbyte);
+      sv[i] = *reinterpret_cast<const u32x4 *>(vp + vr[i] + lbyte);
     }
   };
   // rows of V that are not there are zero, so that no weight of 0 meets a NaN
@@ -652,11 +650,20 @@ __device__ void body_pa_tile(const PagedArgs &a) {
     const bool mixed = k0 < all_lo || k1 > all_hi;
     const bool some = seen != ~uint64_t(0);   // (32 keys: their bits twice)
     bool odd = false;
+    if (padded)
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        if (!inside) sk[i] = sv[i] = u32x4{0, 0, 0, 0};
+    if (some)
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        if (!((seen >> (srow + S::RP * i)) & 1)) sv[i] = u32x4{0, 0, 0, 0};
+    if (mixed)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) odd |= clear_not_finite<DT>(sv[i]);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = srow + S::RP * i;
-      if (some && !((seen >> r) & 1)) sv[i] = u32x4{0, 0, 0, 0};
-      if (mixed) odd |= clear_not_finite<DT>(sv[i]);
       *reinterpret_cast<u32x4 *>(kl + r * S::KS + sbyte) = sk[i];
       *reinterpret_cast<u32x4 *>(vl + r * S::VS + sbyte) = sv[i];
     }

@@ -257,7 +257,7 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
 // split in two). PA_TILE wants 256, one a compute unit, rounded
 // down (24 requests with a window, 218 workgroups: 42.5 us against 61.8 split
 // in two), and runs of 512 keys (four prompts of up to 1024 tokens, heads of
-// 256: 29.6 us against 42.8 split), 256 in float32, whose steps take longer.
+// 256: 28.8 us against 42.8 split), 256 in float32, whose steps take longer.
 AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                    bool aligned, int64_t kv_max, uint64_t workspace) {
   AttnPlan p{};
