@@ -319,10 +319,10 @@ def tile_problem(dtype, lens, nq, nk, hd, page=16, **kw):
 
 
 def tile_check(cache, p, dtype, window=0, **kw):
-    """The result of the form that many rows take: with more than 2048 keys in
-    sight (the bound the host knows) and heads of up to 128 in bf16 two groups
-    of wavefronts share them out, else one does. Both are compared where both
-    can be had: rows of nobody make the tiles too many for the first."""
+    """The result of the form that many rows take: with few tiles and heads of
+    up to 128 in bf16 two groups of wavefronts share the keys, else one has
+    them. Both are compared where both can be had: rows of nobody make the
+    tiles too many for the first."""
     got = attend(cache, p, window=window, **kw)
     assert cache.last_selection().variant in (P.PA_TILE, P.PA_PAIR)
     if "out" in kw:

@@ -1,13 +1,17 @@
 """The paged ops in the native cache core (CPU, recording backend): refusals,
 selections against the model, argument blocks, misses, keys, statistics."""
 import ctypes as C
+import os
 import random
+import subprocess
+import sys
 
 import pytest
 
 from oracle import paged as P
 from paper_2609_37241_amd import _lib as L
 from tests.native_libs import load_fake
+from tests.test_host_sanitized import ROOT, _runtime
 
 A = 0x7F0000000000
 INVALID, UNSUPPORTED = L.E_INVALID, L.E_UNSUPPORTED
@@ -416,3 +420,20 @@ def test_other_cache_flags(lib, fresh, flags):
     info = L.ResidentInfo()
     lib.tri_spec_resident_info(h, C.byref(info))
     assert info.held == 0
+
+
+def test_under_sanitizers():
+    """These tests again, on the core built with the address and the undefined
+    behaviour sanitizer."""
+    asan, ubsan = _runtime("libasan.so"), _runtime("libubsan.so")
+    if not asan or not ubsan:
+        pytest.skip("gcc sanitizer runtimes not found")
+    env = dict(os.environ, TRI_FAKE_SANITIZE="1", LD_PRELOAD=f"{asan}:{ubsan}",
+               ASAN_OPTIONS="detect_leaks=0:halt_on_error=1",
+               UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-p", "no:cacheprovider",
+                        "-k", "not sanitizers", "tests/test_host_paged.py"], cwd=ROOT, env=env,
+                       capture_output=True, text=True, timeout=600)
+    tail = (r.stdout + r.stderr)[-4000:]
+    assert r.returncode == 0, tail
+    assert "ERROR: AddressSanitizer" not in tail and "runtime error:" not in tail, tail
