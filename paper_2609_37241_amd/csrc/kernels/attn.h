@@ -13,10 +13,9 @@
 // by the transposing read (16 lanes exchange 4 rows of 16 elements), float32
 // ones element by element.
 //
-// The weights are 2^(c x - m) with x = q.k, c = |scale| log2 e > 0 (a negative
-// scale changes q's sign) and m the running maximum of c x, in one fused
-// operation: c x is not rounded by itself, and an error in m is common to all
-// of a row's weights. Sums and products accumulate in float32. In bf16 the
+// The weights are 2^(c (x - m)) with x = q.k, c = |scale| log2 e > 0 (a negative
+// scale changes q's sign) and m the running maximum of x. Sums and products
+// accumulate in float32. In bf16 the
 // weights are rounded to bf16 (at most half a step, 2^-8, of each; the sum
 // they are divided by takes them unrounded): the matrix instruction takes both
 // operands in one type, and V's exponents do not fit float16.
@@ -394,16 +393,16 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, st[j][i]);
     top = max_16_32(top);
-    const float mn = fmaxf(m, top == kNegInf ? kNegInf : top * a.scale);
+    const float mn = fmaxf(m, top);
     const float ms = mn == kNegInf ? 0.0f : mn;
-    const float alpha = exp2_hw(m - ms);
+    const float alpha = weight_of(m, ms, a.scale);
     m = mn;
     l *= alpha;
 #pragma unroll
     for (int j = 0; j < MB; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        st[j][i] = exp2_hw(fmaf(st[j][i], a.scale, -ms));
+        st[j][i] = weight_of(st[j][i], ms, a.scale);
         l += st[j][i];
       }
 #pragma unroll
@@ -471,7 +470,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
   for (int w = 0; w < NW; ++w) {
     f[w] = 0.0f;
     if (wave_l[w][row] != 0.0f) {
-      f[w] = exp2_hw(wave_m[w][row] - ts);
+      f[w] = weight_of(wave_m[w][row], ts, a.scale);
       sum += f[w] * wave_l[w][row];
     }
   }
@@ -777,10 +776,9 @@ __device__ void body_pa_tile(const PagedArgs &a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, st[j][i]);
       top = max_32(top);
-      top = top == kNegInf ? kNegInf : top * a.scale;
-      if (__ballot(top > m + 8.0f)) {
+      if (__ballot((top - m) * a.scale > 8.0f)) {
         const float mn = fmaxf(m, top);
-        const float alpha = exp2_hw(m - (mn == kNegInf ? 0.0f : mn));
+        const float alpha = weight_of(m, mn == kNegInf ? 0.0f : mn, a.scale);
         m = mn;
         l *= alpha;
 #pragma unroll
@@ -799,7 +797,7 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       constexpr int WC = DT == kF32 ? 1 : 8;          // weights of a lane for ND products
       constexpr int WP = (WC + ND - 1) / ND;          // formed at each of them
       const auto weight = [&](int c) {
-        const float x = exp2_hw(fmaf(st[c / 16][c % 16], a.scale, -ms));
+        const float x = weight_of(st[c / 16][c % 16], ms, a.scale);
         st[c / 16][c % 16] = x;
         l += x;
       };
@@ -857,8 +855,8 @@ __device__ void body_pa_tile(const PagedArgs &a) {
         const float m1 = y[0], l1 = y[64];
         const float top = fmaxf(l != 0.0f ? m : kNegInf, l1 != 0.0f ? m1 : kNegInf);
         const float ts = top == kNegInf ? 0.0f : top;
-        const float f0 = l != 0.0f ? exp2_hw(m - ts) : 0.0f;
-        const float f1 = l1 != 0.0f ? exp2_hw(m1 - ts) : 0.0f;
+        const float f0 = l != 0.0f ? weight_of(m, ts, a.scale) : 0.0f;
+        const float f1 = l1 != 0.0f ? weight_of(m1, ts, a.scale) : 0.0f;
         m = top;
         l = f0 * l + f1 * l1;
 #pragma unroll

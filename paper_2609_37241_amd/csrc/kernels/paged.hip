@@ -259,10 +259,10 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
       float top = sc;
 #pragma unroll
       for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-      const float mn = fmaxf(m, top == kNegInf ? kNegInf : top * a.scale);
+      const float mn = fmaxf(m, top);
       const float ms = mn == kNegInf ? 0.0f : mn;
-      const float alpha = exp2_hw(m - ms);
-      const float w = ko >= 0 ? exp2_hw(fmaf(sc, a.scale, -ms)) : 0.0f;
+      const float alpha = weight_of(m, ms, a.scale);
+      const float w = ko >= 0 ? weight_of(sc, ms, a.scale) : 0.0f;
       float sum = w;
 #pragma unroll
       for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
 }
 
 // ---- PA_JOIN -----------------------------------------------------------------------------------
-// out = sum_s 2^(m_s - m) part_s / sum_s 2^(m_s - m) l_s over the splits of a
+// out = sum_s w_s part_s / sum_s w_s l_s, w_s = 2^(c (m_s - m)), over the splits of a
 // row, m the largest m_s, always in the same order: the same bits every time.
 // A split without a seen key (l_s = 0) left no sums and is passed over. A
 // wavefront per row, or four where there are many splits: what bounds it is
@@ -344,7 +344,7 @@ __device__ void join_rows(const PagedArgs &a) {
     float top = l != 0.0f ? m : kNegInf;
 #pragma unroll
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float w = l != 0.0f ? exp2_hw(m - (top == kNegInf ? 0.0f : top)) : 0.0f;
+    const float w = l != 0.0f ? weight_of(m, top == kNegInf ? 0.0f : top, a.scale) : 0.0f;
     float sum = l != 0.0f ? w * l : 0.0f;
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);

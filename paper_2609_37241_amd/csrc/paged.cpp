@@ -239,10 +239,11 @@ tri_status tri_paged_attention(tri_cache *c, const tri_attention_args *p, void *
                          uint64_t(a.kv.hd) * es_of(uint32_t(a.dtype));
   const bool large = bytes > kCacheBytes && (a.T + a.R - 1) / a.R * (a.nq / a.kv.nk) <= 16;
   const int32_t g = a.nq / a.kv.nk;
-  // the weights are 2^(c q.k - maximum), c = |scale| log2 e; for 0 a c so small
-  // that all weights are 1 (a masked score stays -inf)
+  // the weights are 2^(c (q.k - maximum)), c = |scale| log2 e; for 0 the least
+  // float32 above it: 2^128 of it is 2^-21, so all weights are 1 but for a masked
+  // score's, which stays -inf
   float c2 = float(fabs(double(a.scale)) * 1.4426950408889634);
-  if (!(c2 >= 1e-36f)) c2 = 1e-36f;
+  if (!(c2 >= 0x1p-149f)) c2 = 0x1p-149f;
   if (!(c2 <= 3e38f)) c2 = 3e38f;
   const PagedArgs args{a.q, a.out, {a.kv.k, a.kv.k_ps, a.kv.k_ss, a.kv.k_hs},
                        {a.kv.v, a.kv.v_ps, a.kv.v_ss, a.kv.v_hs}, a.table, a.kv_len, a.q_start,
