@@ -100,8 +100,12 @@ __device__ inline bool clear_not_finite(u32x4 &v) {
 // a product over all keys would make NaN of their weight of 0. So in the steps
 // whose keys the rows see differently such elements go to LDS as zeros, and
 // where there were any, the lanes whose query sees their key add them to its
-// sums in the end, from memory. Weights are above 0 and have no say in what an
-// infinity or NaN makes of a sum; one that was in it already changes nothing.
+// sums in the end, from memory. A weight above 0 has no say in what an infinity
+// or NaN makes of a sum, and one that was in it already changes nothing. A weight
+// of 0 (a score of -inf, or too far below the maximum for float32) makes NaN of
+// them in the products and leaves them as they are here: such a row's element is
+// one or the other. So parts of a row that are joined come in with all they
+// hold, also those of no weight; a row of no weight at all is zero.
 // v: the key's V; e: the first of four elements.
 template <int DT>
 __device__ inline void add_not_finite(const char *v, int32_t e, int32_t hd, float *o) {
@@ -435,16 +439,17 @@ __device__ void body_pa_rows(const PagedArgs &a) {
     }
   }
 
-  for (int32_t x = odd_b; x < odd_e; ++x) {
-    const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
-    if (at < 0 || !sees(x)) continue;
+  for (int32_t x0 = odd_b; x0 < odd_e; x0 += NW * KB)   // (the wavefront's own steps)
+    for (int32_t x = x0; x < odd_e && x < x0 + KB; ++x) {
+      const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
+      if (at < 0 || !sees(x)) continue;
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
-      add_not_finite<DT>(vp + at * ES, 16 * d + 4 * quarter, a.hd, z);
-      o[d] = f32x4{z[0], z[1], z[2], z[3]};
+      for (int d = 0; d < ND; ++d) {
+        float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
+        add_not_finite<DT>(vp + at * ES, 16 * d + 4 * quarter, a.hd, z);
+        o[d] = f32x4{z[0], z[1], z[2], z[3]};
+      }
     }
-  }
 
   // join the wavefronts
   l = sum_16_32(l);
@@ -484,7 +489,6 @@ __device__ void body_pa_rows(const PagedArgs &a) {
     f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      if (wave_l[w][row] == 0.0f) continue;
       const f32x4 x = *reinterpret_cast<const f32x4 *>(
           reinterpret_cast<const float *>(lds + w * S::WAVE_LDS) + row * S::OS + d);
 #pragma unroll
@@ -495,7 +499,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
     } else {
       float y[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = acc[i] * inv;
+      for (int i = 0; i < 4; ++i) y[i] = sum == 0.0f ? 0.0f : acc[i] * inv;
       store4<DT>(a, token, head, d, y);
     }
   }
@@ -890,7 +894,8 @@ __device__ void body_pa_tile(const PagedArgs &a) {
   }
   if (row >= t.rows) return;
   const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const bool zero = a.splits == 1 && l == 0.0f;
+  const float f = a.splits > 1 ? 1.0f : 1.0f / l;
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -899,7 +904,7 @@ __device__ void body_pa_tile(const PagedArgs &a) {
       if (e0 >= a.hd) continue;
       float y[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) y[x] = a.splits > 1 ? o[d][4 * i + x] : o[d][4 * i + x] * inv;
+      for (int x = 0; x < 4; ++x) y[x] = zero ? 0.0f : o[d][4 * i + x] * f;
       if (a.splits > 1)
         *reinterpret_cast<u32x4 *>(a.part + at * a.hd + e0) = Elt<kF32>::pack(y);
       else

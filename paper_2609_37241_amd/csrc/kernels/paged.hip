@@ -301,7 +301,7 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
 // ---- PA_JOIN -----------------------------------------------------------------------------------
 // out = sum_s w_s part_s / sum_s w_s l_s, w_s = 2^(c (m_s - m)), over the splits of a
 // row, m the largest m_s, always in the same order: the same bits every time.
-// A split without a seen key (l_s = 0) left no sums and is passed over. A
+// A split without a weight (l_s = 0) has no say in m. A
 // wavefront per row, or four where there are many splits: what bounds it is
 // the latency of the sums' loads, so as many lanes as a row leaves free take
 // other splits, eight of them in flight. 32 rows of 64 splits, 4.7 us; 2048 of
@@ -348,7 +348,6 @@ __device__ void join_rows(const PagedArgs &a) {
     float sum = l != 0.0f ? w * l : 0.0f;
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    const uint64_t there = __ballot(l != 0.0f);
     char *o = static_cast<char *>(a.out) + (int64_t(t) * a.o_ts + int64_t(h) * a.hd) * Elt<DT>::ES;
     for (int d0 = 0; d0 < a.hd; d0 += nl * VEC) {   // (every lane stays: they exchange)
       const int d = d0 + e;
@@ -362,8 +361,7 @@ __device__ void join_rows(const PagedArgs &a) {
         for (int i = 0; i < 8; ++i) {
           const int s = s0 + i * groups + group;
           const float ws = __shfl(w, s & 63);
-          // (a split that left no sums has anything in their place)
-          if (s < a.splits && ((there >> s) & 1)) {
+          if (s < a.splits) {
 #pragma unroll
             for (int c = 0; c < VEC; ++c) acc[c] = fmaf(ws, x[i][c], acc[c]);
           }
