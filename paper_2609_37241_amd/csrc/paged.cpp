@@ -112,18 +112,18 @@ AttnPlan plan_of(const tri_attention_args &a, uint64_t workspace) {
 }
 
 // The launches of a paged op (`block` work-items a workgroup the first, 256
-// any other), in order, stopping at the first failure. On a miss they are kept
-// for the record of an install that follows.
+// any other), in order, stopping at the first failure. On a miss, installed by
+// the call itself or not, they are kept for tri_spec_install_last_miss.
 tri_status run_paged(tri_cache *c, uint32_t op, const Key &k, int64_t T, const uint32_t *grid,
                      int n, uint32_t block, const void *args, uint32_t size, void *stream) {
   int32_t vi;
   bool auto_inst = false;
   const int st = lookup(c, op, k, T, &vi, &auto_inst);
-  if (st != TRI_OK) {
+  if (st != TRI_OK || auto_inst) {
     for (int i = 0; i < 2; ++i) c->miss_grid[i] = i < n ? grid[i] : 0;
     c->miss_block = block;
-    return tri_status(st);
   }
+  if (st != TRI_OK) return tri_status(st);
   Version &v = c->versions[vi];
   tri_launch_rec l[3];
   int rc = 0;
