@@ -20,6 +20,7 @@ for every call (some 2-4 us more of host time each), and importing warns.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import warnings
 from typing import Optional, Tuple
@@ -144,6 +145,20 @@ def _stream_ptr(stream, device: int = -1) -> Optional[int]:
     if _raw_stream is not None:
         return _raw_stream(device) or None
     return torch.cuda.current_stream(device).cuda_stream or None
+
+
+def _making_on(stream, dev: int):
+    """A context whose allocations on GPU `dev` belong to `stream` (None: the
+    current one): outputs and workspaces are made where the call writes them, so
+    that torch's allocator hands their memory on only after that work."""
+    if stream is None:
+        return _ON_CURRENT
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=dev)
+    return torch.cuda.stream(stream)
+
+
+_ON_CURRENT = contextlib.nullcontext()
 
 
 def _rows(t: torch.Tensor, name: str, W: int) -> int:
@@ -314,7 +329,12 @@ class Prepared:
 
 
 class SpecCache:
-    """One native specialization cache (bound to the current device)."""
+    """One native specialization cache (bound to the current device).
+
+    An op's `stream` (default: the device's current one) is where it runs and
+    where its outputs and workspaces are made when they are not given, as
+    torch's own ops do under torch.cuda.stream: used on another stream, a
+    result needs its wait and its record_stream there."""
 
     _fast = _PythonForm()      # the native op calls (set with the handle)
 
@@ -415,6 +435,17 @@ class SpecCache:
             raise TriError(st, "tri_spec_install_last_miss")
         return sel
 
+    def _made(self, given, like, stream, shape=None, dtype=None) -> torch.Tensor:
+        """`given`, or a new tensor made on the call's stream: as `like`, or of
+        `shape` (and `dtype`, by default like's) on its device."""
+        if given is not None:
+            return given
+        with _making_on(stream, self._dev):
+            if shape is None:
+                return torch.empty_like(like)
+            return torch.empty(shape, dtype=like.dtype if dtype is None else dtype,
+                               device=like.device)
+
     # ---- ops ---------------------------------------------------------------
     def rmsnorm(self, x: torch.Tensor, w: torch.Tensor, eps: float = 1e-6,
                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -423,7 +454,7 @@ class SpecCache:
             if r is not None:
                 return r
         T, H = _dims(x, "x", 2, self._dev)
-        y = torch.empty_like(x) if out is None else out
+        y = self._made(out, x, stream)
         _like(y, "out", x.shape, x.dtype, self._dev)
         _vector(w, "w", H, x.dtype, self._dev)
         self._call("tri_rmsnorm", _dll.tri_rmsnorm, dtype_code(x.dtype), x.data_ptr(),
@@ -439,8 +470,7 @@ class SpecCache:
                 return r
         T, H = _dims(x, "x", 2, self._dev)
         _like(residual, "residual", x.shape, x.dtype, self._dev)
-        y = torch.empty_like(x) if out is None else out
-        ro = torch.empty_like(residual) if residual_out is None else residual_out
+        y, ro = self._made(out, x, stream), self._made(residual_out, residual, stream)
         _like(y, "out", x.shape, x.dtype, self._dev)
         _like(ro, "residual_out", x.shape, x.dtype, self._dev)
         _vector(w, "w", H, x.dtype, self._dev)
@@ -551,7 +581,7 @@ class SpecCache:
                 return r
         T, I = _dims(gate, "gate", 2, self._dev)
         _like(up, "up", gate.shape, gate.dtype, self._dev)
-        o = torch.empty_like(gate) if out is None else out
+        o = self._made(out, gate, stream)
         _like(o, "out", gate.shape, gate.dtype, self._dev)
         self._call("tri_swiglu", _dll.tri_swiglu, dtype_code(gate.dtype), gate.data_ptr(),
                    _rows(gate, "gate", I), up.data_ptr(), _rows(up, "up", I), o.data_ptr(),
@@ -566,7 +596,7 @@ class SpecCache:
             if r is not None:
                 return r
         T, W = _dims(x, "x", 2, self._dev)
-        o = torch.empty_like(x) if out is None else out
+        o = self._made(out, x, stream)
         _like(o, "out", x.shape, x.dtype, self._dev)
         self._call("tri_silu", _dll.tri_silu, dtype_code(x.dtype), x.data_ptr(),
                    _rows(x, "x", W), o.data_ptr(), _rows(o, "out", W), T, W,
@@ -581,7 +611,7 @@ class SpecCache:
                 return r
         T, W = _dims(a, "a", 2, self._dev)
         _like(b, "b", a.shape, a.dtype, self._dev)
-        o = torch.empty_like(a) if out is None else out
+        o = self._made(out, a, stream)
         _like(o, "out", a.shape, a.dtype, self._dev)
         self._call("tri_add", _dll.tri_add, dtype_code(a.dtype), a.data_ptr(),
                    _rows(a, "a", W), b.data_ptr(), _rows(b, "b", W), o.data_ptr(),
@@ -600,7 +630,7 @@ class SpecCache:
         if mask.shape != x.shape:
             raise ValueError(f"mask: expected {tuple(x.shape)}, got {tuple(mask.shape)}")
         _on(mask, "mask", self._dev)
-        o = torch.empty_like(x) if out is None else out
+        o = self._made(out, x, stream)
         _like(o, "out", x.shape, x.dtype, self._dev)
         self._call("tri_masked_fill", _dll.tri_masked_fill, dtype_code(x.dtype), x.data_ptr(),
                    _rows(x, "x", W), mask.data_ptr(), _rows(mask, "mask", W), value,
@@ -620,7 +650,7 @@ class SpecCache:
         if T > 1 and ids.stride(0) != 1:
             raise ValueError("ids must be contiguous")
         _on(ids, "ids", self._dev)
-        o = torch.empty((T, H), dtype=table.dtype, device=table.device) if out is None else out
+        o = self._made(out, table, stream, (T, H))
         _like(o, "out", (T, H), table.dtype, self._dev)
         self._call("tri_embedding", _dll.tri_embedding, dtype_code(table.dtype),
                    table.data_ptr(), _rows(table, "table", H), n_rows, ids.data_ptr(),
@@ -652,7 +682,7 @@ class SpecCache:
         fc = _int32(free_count, "free_count", -1, dev)
 
         def new(t, n, dtype=torch.int32):
-            return torch.empty(n, dtype=dtype, device=block_table.device) if t is None else t
+            return self._made(t, block_table, stream, n, dtype)
 
         slots, pos = new(slots, T, torch.int64), new(pos, T)
         q_start, kv_len_out, free_out = new(q_start, R + 1), new(kv_len_out, R), new(free_out, 2)
@@ -704,7 +734,7 @@ class SpecCache:
                 return r
         dev = self._dev
         T, nq, hd = _dims(q, "q", 3, dev)
-        o = torch.empty((T, nq, hd), dtype=q.dtype, device=q.device) if out is None else out
+        o = self._made(out, q, stream, (T, nq, hd))
         _like(o, "out", q.shape, q.dtype, dev)
         R, cols, rs = _table(block_table, "block_table", dev)
         kv = _kv_cache(k_cache, v_cache, q.dtype, dev)
@@ -717,10 +747,7 @@ class SpecCache:
                             hd ** -0.5 if scale is None else scale, window, max_kv, None, 0, kv)
         need = _dll.tri_paged_attention_workspace(C.byref(a))
         if need:
-            # on the call's stream: the allocator may hand the block on once
-            # the work queued there so far is done
-            with torch.cuda.stream(stream):
-                a._workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            a._workspace = self._made(None, q, stream, need, torch.uint8)
             a.workspace, a.workspace_bytes = a._workspace.data_ptr(), need
         self._call("tri_paged_attention", _dll.tri_paged_attention, C.byref(a),
                    _stream_ptr(stream, dev))
@@ -819,8 +846,9 @@ class SpecCache:
                      k_norm_w=None, qk_eps=None, rope: Optional[RopeExt] = None):
         """Residual+RMSNorm, in-place (QK-RMSNorm +) RoPE of q/k and SwiGLU in
         one entry call. Returns (y, residual_out, out)."""
-        a, outs = self.chain_args(x, residual, w, q, k, pos, gate, up, eps, base, y,
-                                  residual_out, out, q_norm_w, k_norm_w, qk_eps, rope)
+        with _making_on(stream, self._dev):
+            a, outs = self.chain_args(x, residual, w, q, k, pos, gate, up, eps, base, y,
+                                      residual_out, out, q_norm_w, k_norm_w, qk_eps, rope)
         self.decode_chain_args(a, stream)
         return outs
 
