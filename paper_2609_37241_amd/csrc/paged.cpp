@@ -235,9 +235,9 @@ tri_status tri_paged_attention(tri_cache *c, const tri_attention_args *p, void *
   // where one tile reads them they are streamed (PA_ROWS; 64 requests of up to
   // 8k tokens, 8 K heads of 128 in bf16, 1 GB: 214 -> 193 us; 262 MB: 52 -> 56;
   // three tiles over 1 GB in float32, 195 -> 223)
-  const uint64_t bytes = 2 * uint64_t(a.R) * uint64_t(attn_keys(a)) * uint64_t(a.kv.nk) *
-                         uint64_t(a.kv.hd) * es_of(uint32_t(a.dtype));
-  const bool large = bytes > kCacheBytes && (a.T + a.R - 1) / a.R * (a.nq / a.kv.nk) <= 16;
+  const double bytes = 2.0 * double(a.R) * double(attn_keys(a)) * double(a.kv.nk) *
+                       double(a.kv.hd) * double(es_of(uint32_t(a.dtype)));   // (up to 2^67)
+  const bool large = bytes > double(kCacheBytes) && (a.T + a.R - 1) / a.R * (a.nq / a.kv.nk) <= 16;
   const int32_t g = a.nq / a.kv.nk;
   // the weights are 2^(c (q.k - maximum)), c = |scale| log2 e; for 0 the least
   // float32 above it: 2^128 of it is 2^-21, so all weights are 1 but for a masked
