@@ -337,11 +337,10 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 #pragma unroll
     for (int j = 0; j < MB; ++j) {
       st[j] = f32x4{0, 0, 0, 0};
-      // float32: several sums side by side, each with a part of the rounding
-      // errors of one (which lost up to 2.5 times what a blocked product
-      // loses). Heads of 64, two: 21.7 us for six ragged requests, 0.24 to 1.3 times
-      // the loss; four: 23.6, 0.28 to 1.05; one: 21.8, 0.78 to 2.1.
-      constexpr int SUMS = HDP > 64 ? 4 : 2;
+      // (float32: four sums side by side, whose rounding errors stay half those
+      // of one sum four times as long. Two would leave heads of 64 another
+      // wavefront a SIMD: six ragged requests 23.3 -> 21.5 us, but 64 of up to
+      // 8192 keys 193 -> 207, and up to 1.24 times the plain form's error)
       f32x4 sum[4] = {};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
@@ -350,8 +349,8 @@ __device__ void body_pa_rows(const PagedArgs &a) {
         if constexpr (DT == kF32) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            sum[i % SUMS] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                __uint_as_float(x[i]), __uint_as_float(q[s][i]), sum[i % SUMS], 0, 0, 0);
+            sum[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[i]),
+                                                          __uint_as_float(q[s][i]), sum[i], 0, 0, 0);
         } else {
           st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
                                                           __builtin_bit_cast(bf16x8, q[s]), st[j],

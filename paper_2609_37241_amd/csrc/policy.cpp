@@ -250,7 +250,7 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
 // 4 us and the traffic of the sums. PA_ROWS wants 1024 (64 requests of up to
 // 8k tokens, where the longest decides, read without streaming: 214 us; 512
 // workgroups 227, 2048 212; streamed 193 and 193 to 200)
-// and runs of 1024 (six requests in float32, 300 tiles: 21.7 us, runs of 512
+// and runs of 1024 (six requests in float32, 300 tiles: 22.6 us, runs of 512
 // about 3 more); but idle compute units take shorter ones, of 256 (a step of a
 // workgroup takes 2.2 us, the latency of its loads: a request of 32 heads and
 // 2000 tokens 12.4 us against 18.6), from 512 keys on (500 tokens: 10.1 us against 11.5
