@@ -573,9 +573,8 @@ tri_status tri_kv_write(tri_cache *cache, tri_dtype dtype, const void *k, int64_
  * rounded to bf16 before they meet V). Keys that are not seen contribute
  * nothing, whatever their slots hold (NaN and infinities included); a row that
  * sees no key, or whose scores are all -inf, is zero. In any other row a NaN or
- * an infinity in V at a key that it sees is in the row's element too: the
- * infinity, or NaN, where the key's weight is 0 in float32 one of the two,
- * whichever the tile's other rows make of it. Rows of out before
+ * an infinity in V at a key that it sees is in the row's element as it is,
+ * whatever the key's weight. Rows of out before
  * q_start[0] and from q_start[R] on are left as they were. kv_len is clamped
  * to [0, cols * page], q_start to [0, T] and must not decrease (rows that two
  * requests claim hold either's result). out may alias q exactly.

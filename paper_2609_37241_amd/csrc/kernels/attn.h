@@ -96,25 +96,66 @@ __device__ inline bool clear_not_finite(u32x4 &v) {
 }
 
 // V may hold infinities or NaN at a key that some rows of a tile see and others
-// must not (a later token of the same chunk, an earlier one than the window):
-// a product over all keys would make NaN of their weight of 0. So in the steps
-// whose keys the rows see differently such elements go to LDS as zeros, and
-// where there were any, the lanes whose query sees their key add them to its
-// sums in the end, from memory. A weight above 0 has no say in what an infinity
-// or NaN makes of a sum, and one that was in it already changes nothing. A weight
-// of 0 (a score of -inf, or too far below the maximum for float32) makes NaN of
-// them in the products and leaves them as they are here: such a row's element is
-// one or the other. So parts of a row that are joined come in with all they
-// hold, also those of no weight; a row of no weight at all is zero.
-// v: the key's V; e: the first of four elements.
+// must not (a later token of the same chunk, an earlier one than the window): a
+// product over all keys would make NaN of their weight of 0. So in the steps
+// whose keys the rows see differently such elements go to LDS as zeros. In the
+// other steps the products make an infinity or NaN of them, which of the two
+// depends on whether float32 has the weight as 0. So where there were any in the
+// end, an element of a row is formed again: the sum of those that it sees, from
+// memory, whatever their weights (above 0, a weight has no say in it); a row's
+// result then does not depend on the other rows of its tile. The look at the sums
+// is within what boxes differ by; one at every step's V took 2 % of the 128-row
+// tiles and 13 % of float32 heads of 256.
+
+// Whether a row's sums, at weights that are finite, hold an infinity or NaN.
+template <int N, class F>
+__device__ inline bool holds_not_finite(const F *o, int n, float l) {
+  float z[4] = {};
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+    for (int i = 0; i < n; ++i) z[i % 4] = fmaf(o[d][i], 0.0f, z[i % 4]);
+  const float all = (z[0] + z[1]) + (z[2] + z[3]);
+  return all != all && fabsf(l) < __builtin_inff();
+}
+
+// Whether the hdb bytes of a key's V hold one.
 template <int DT>
-__device__ inline void add_not_finite(const char *v, int32_t e, int32_t hd, float *o) {
-  if (e >= hd) return;
+__device__ inline bool row_not_finite(const char *v, int hdb) {
+  bool odd = false;
+  for (int c = 0; c < hdb; c += 16) {
+    u32x4 x = *reinterpret_cast<const u32x4 *>(v + c);
+    odd |= clear_not_finite<DT>(x);
+  }
+  return odd;
+}
+
+// Four elements of a row's sums, the first of them e, from the key's V at v where
+// the row sees it: the first infinity or NaN (bit `at` of `had` is clear) takes the
+// element's place. Without branches, whose masks would not fit the registers.
+template <int DT>
+__device__ inline void add_not_finite(const char *v, bool sees, int32_t e, int32_t hd, int at,
+                                      uint32_t *had, float *o) {
+  const bool inside = e < hd;
+  float y[4];
+  if constexpr (DT == kF32) {
+    Elt<kF32>::unpack(*reinterpret_cast<const u32x4 *>(v + (inside ? e : 0) * 4), y);
+  } else {
+    const u32x2 x = *reinterpret_cast<const u32x2 *>(v + (inside ? e : 0) * 2);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      y[2 * i] = __uint_as_float(x[i] << 16);
+      y[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float y = Elt<DT>::ld(v, e + i);
-    if (!(fabsf(y) < __builtin_inff())) o[i] += y;
+    const bool odd = inside & sees & !(fabsf(y[i]) < __builtin_inff());
+    const uint32_t bit = 1u << ((at + i) & 31);
+    const float z = *had & bit ? o[i] + y[i] : y[i];
+    o[i] = odd ? z : o[i];
+    *had |= odd ? bit : 0u;
   }
+  __builtin_amdgcn_sched_barrier(0);   // (or all elements' masks live at once)
 }
 
 // The tile of queries that a workgroup computes: M rows of request r's n * g
@@ -438,20 +479,33 @@ __device__ void body_pa_rows(const PagedArgs &a) {
     }
   }
 
-  for (int32_t x0 = odd_b; x0 < odd_e; x0 += NW * KB)   // (the wavefront's own steps)
-    for (int32_t x = x0; x < odd_e && x < x0 + KB; ++x) {
-      const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
-      if (at < 0 || !sees(x)) continue;
+  l = sum_16_32(l);
+  if (__ballot(holds_not_finite<ND>(o, 4, l))) {
+    odd_b = b + wave * KB;
+    odd_e = e;
+  }
+  uint32_t had[(ND + 7) / 8] = {};
+  for (int32_t x0 = odd_b; x0 < odd_e; x0 += NW * KB) {   // (the wavefront's own steps)
+    int64_t mine = -1;
+    if (lane < KB && x0 + lane < e) mine = slot_offset(table, uint32_t(x0 + lane), a, a.v);
+    uint64_t keys = __ballot(mine >= 0 && row_not_finite<DT>(vp + mine * ES, hdb));
+    for (; keys; keys &= keys - 1) {
+      const int i = __builtin_ctzll(keys);
+      const char *x = vp + __shfl(mine, i) * ES;
+      const bool seen_here = sees(x0 + i);
+      int32_t hd = a.hd;
+      asm volatile("" : "+s"(hd));   // (else the masks of elements inside are shared with
+                                     // the stores below and live all along)
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
-        add_not_finite<DT>(vp + at * ES, 16 * d + 4 * quarter, a.hd, z);
+        add_not_finite<DT>(x, seen_here, 16 * d + 4 * quarter, hd, 4 * d, &had[d / 8], z);
         o[d] = f32x4{z[0], z[1], z[2], z[3]};
       }
     }
+  }
 
   // join the wavefronts
-  l = sum_16_32(l);
   if (quarter == 0) {
     wave_m[wave][n] = m;
     wave_l[wave][n] = l;
@@ -486,12 +540,23 @@ __device__ void body_pa_rows(const PagedArgs &a) {
     const int d = 4 * PR * c + 4 * part;
     if (d >= a.hd) break;
     f32x4 acc = {0, 0, 0, 0};
+    const auto sum_of = [&](int w) {
+      return *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(lds + w * S::WAVE_LDS) +
+                                              row * S::OS + d);
+    };
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(
-          reinterpret_cast<const float *>(lds + w * S::WAVE_LDS) + row * S::OS + d);
+      const f32x4 x = sum_of(w);
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], x[i], acc[i]);
+    }
+    if (holds_not_finite<1>(&acc, 4, sum)) {
+      acc = f32x4{0, 0, 0, 0};
+      for (int w = 0; w < NW; ++w) {
+        const float fw = wave_l[w][row] != 0.0f ? weight_of(wave_m[w][row], ts, a.scale) : 0.0f;
+        const f32x4 x = sum_of(w);
+        for (int i = 0; i < 4; ++i) acc[i] = add_part(fw, x[i], acc[i]);
+      }
     }
     if (a.splits > 1) {
       *reinterpret_cast<f32x4 *>(a.part + at * a.hd + d) = acc;
@@ -875,21 +940,37 @@ __device__ void body_pa_tile(const PagedArgs &a) {
     }
     if (group == 1) return;
   }
-  // (the last step's barrier is behind all of them)
-  for (int32_t x = odd_b; b < e && x < odd_e; ++x) {
-    const int64_t at = slot_offset(table, uint32_t(x), a, a.v);
-    if (at < 0 || !sees(x)) continue;
+  // (the last step's barrier is behind what set odd_b and odd_e)
+  int32_t x0 = b < e ? odd_b : 0, x1 = b < e ? odd_e : 0;
+  if (__ballot(holds_not_finite<ND>(o, 16, l))) {
+    x0 = b;
+    x1 = e;
+  }
+  uint32_t had[(ND + 1) / 2] = {};
+  for (; x0 < x1; x0 += 64) {
+    int64_t mine = -1;
+    if (x0 + lane < x1) mine = slot_offset(table, uint32_t(x0 + lane), a, a.v);
+    uint64_t keys = __ballot(mine >= 0 && row_not_finite<DT>(vp + mine * ES, hdb));
+    for (; keys; keys &= keys - 1) {
+      const int i = __builtin_ctzll(keys);
+      const char *x = vp + __shfl(mine, i) * ES;
+      const bool seen_here = sees(x0 + i);
+      int32_t hd = a.hd;
+      asm volatile("" : "+s"(hd));   // (else the masks of elements inside are shared with
+                                     // the stores below and live all along)
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+      for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float z[4];
+        for (int j = 0; j < 4; ++j) {
+          float z[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) z[c] = o[d][4 * i + c];
-        add_not_finite<DT>(vp + at * ES, 32 * d + 8 * i + 4 * half, a.hd, z);
+          for (int c = 0; c < 4; ++c) z[c] = o[d][4 * j + c];
+          add_not_finite<DT>(x, seen_here, 32 * d + 8 * j + 4 * half, hd, 16 * d + 4 * j,
+                             &had[d / 2], z);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[d][4 * i + c] = z[c];
-      }
+          for (int c = 0; c < 4; ++c) o[d][4 * j + c] = z[c];
+        }
+    }
   }
   if (row >= t.rows) return;
   const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;

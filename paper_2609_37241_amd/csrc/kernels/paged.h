@@ -23,6 +23,12 @@ constexpr float kNegInf = -__builtin_inff();
 // one operation a weight: 2048 tokens behind 6144, 274.5 -> 278.7 us.
 __device__ inline float weight_of(float x, float m, float c) { return exp2_hw((x - m) * c); }
 
+// acc + f x for a part x of a row's sum, taken against another reference; an
+// infinity or NaN of V that the part holds stays what it is where f is 0.
+__device__ inline float add_part(float f, float x, float acc) {
+  return f == 0.0f && !(fabsf(x) < __builtin_inff()) ? acc + x : fmaf(f, x, acc);
+}
+
 // The keys that the rows of one request see. Lengths and starts are device
 // data and may hold anything: clamped so that every row lies in [0, T) and
 // every key in the table.

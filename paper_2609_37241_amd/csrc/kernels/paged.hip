@@ -236,6 +236,7 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
     const char *kp = static_cast<const char *>(a.k.p) + int64_t(kh) * a.k.hs * ES;
     const char *vp = static_cast<const char *>(a.v.p) + int64_t(kh) * a.v.hs * ES;
     float m = kNegInf, l = 0.0f, acc[NI] = {};
+    float odd[NI] = {};   // the infinities and NaN of V: what they make of a sum no weight changes
     for (int32_t k0 = b; k0 < e; k0 += 64) {
       const int32_t key = k0 + lane;
       int64_t ko = -1, vo = -1;
@@ -276,9 +277,16 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
         const char *v = vp + __shfl(vo, j) * ES;
 #pragma unroll
         for (int i = 0; i < NI; ++i)
-          if (lane + 64 * i < a.hd) acc[i] = fmaf(wj, Elt<DT>::ld(v, lane + 64 * i), acc[i]);
+          if (lane + 64 * i < a.hd) {
+            const float y = Elt<DT>::ld(v, lane + 64 * i);
+            const bool fine = fabsf(y) < __builtin_inff();
+            acc[i] = fmaf(wj, fine ? y : 0.0f, acc[i]);
+            odd[i] += fine ? 0.0f : y;
+          }
       }
     }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) acc[i] += odd[i];
     if (a.splits > 1) {
       const int64_t at = row * a.splits + s;
       if (lane == 0) {
@@ -379,6 +387,19 @@ __device__ void join_rows(const PagedArgs &a) {
         for (int c = 0; c < VEC; ++c)
           acc[c] = (sums[0][lane * VEC + c] + sums[1][lane * VEC + c]) +
                    (sums[2][lane * VEC + c] + sums[3][lane * VEC + c]);
+      }
+      bool odd = false;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) odd |= !(fabsf(acc[c]) < __builtin_inff());
+      if (__ballot(odd)) {   // infinities or NaN of V, maybe where a weight is 0
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) acc[c] = 0.0f;
+        for (int s = 0; s < a.splits; ++s) {
+          read(s, d, x[0]);
+          const float ws = __shfl(w, s);
+#pragma unroll
+          for (int c = 0; c < VEC; ++c) acc[c] = add_part(ws, x[0][c], acc[c]);
+        }
       }
       if (d < a.hd && lane < nl && (!four || wave == 0)) {
 #pragma unroll

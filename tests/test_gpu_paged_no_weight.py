@@ -73,3 +73,34 @@ def test_half_the_keys_have_no_weight(cache, case):  # noqa: F811
         want = oracle({k: v for k, v in dict(p, q=p["q"][:rows]).items() if k != "max_kv"})
         check(torch.from_numpy(got[:rows]), want, dtype)
         assert np.isfinite(f64(torch.from_numpy(got[:rows]))).all()
+
+
+@pytest.mark.parametrize("gap", [3.0, 60.0, 300.0, 650.0])
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("case", list(CASES))
+def test_infinities_behind_small_weights(cache, case, back, gap):  # noqa: F811
+    """An infinity or NaN in V at a key whose score is `gap` below the largest is
+    in the element of each row that sees the key, as it is: also where float32
+    has the weight as 0, and whatever the other rows of the tile see. The key is
+    an early one, which all rows of a tile see, or one of the last that some
+    do not; the largest score is far from it or beside it."""
+    dtype, lens = CASES[case][:2]
+    hd = CASES[case][4]
+    p, rows = make(case, 10)
+    p["q"][:] = 1.0
+    page = p["kc"].shape[1]
+    for far in (True, False):
+        q = dict(p, kc=p["kc"].clone(), vc=p["vc"].clone())
+        for r, (kv, n) in enumerate(lens):
+            for x in range(kv):
+                fill(q, "kc", r, x, 0.0)
+            marks = sorted({max(kv - n, 0), kv - 1, kv - 1 - n // 2} if back else {0, 1, kv // 4})
+            top = (0 if back else kv - n) if far else max(marks[0] - 1, 0)
+            if top in marks:
+                marks.remove(top)
+            fill(q, "kc", r, top, gap / (hd * float(np.float32(p["scale"]))))
+            for i, x in enumerate(marks):
+                q["vc"][int(q["table"][r, x // page]), x % page, :, i % hd] = (INF, -INF, NAN)[i]
+        got = run(cache, case, q)
+        want = oracle({k: v for k, v in dict(q, q=q["q"][:rows]).items() if k != "max_kv"})
+        check(torch.from_numpy(got[:rows]), want, dtype)
