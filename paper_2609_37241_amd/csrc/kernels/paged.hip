@@ -236,7 +236,6 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
     const char *kp = static_cast<const char *>(a.k.p) + int64_t(kh) * a.k.hs * ES;
     const char *vp = static_cast<const char *>(a.v.p) + int64_t(kh) * a.v.hs * ES;
     float m = kNegInf, l = 0.0f, acc[NI] = {};
-    float odd[NI] = {};   // the infinities and NaN of V: what they make of a sum no weight changes
     for (int32_t k0 = b; k0 < e; k0 += 64) {
       const int32_t key = k0 + lane;
       int64_t ko = -1, vo = -1;
@@ -277,16 +276,29 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
         const char *v = vp + __shfl(vo, j) * ES;
 #pragma unroll
         for (int i = 0; i < NI; ++i)
-          if (lane + 64 * i < a.hd) {
-            const float y = Elt<DT>::ld(v, lane + 64 * i);
-            const bool fine = fabsf(y) < __builtin_inff();
-            acc[i] = fmaf(wj, fine ? y : 0.0f, acc[i]);
-            odd[i] += fine ? 0.0f : y;
-          }
+          if (lane + 64 * i < a.hd) acc[i] = fmaf(wj, Elt<DT>::ld(v, lane + 64 * i), acc[i]);
       }
     }
+    // an infinity or NaN of V is in its element as it is, whatever its weight:
+    // sums that are not finite, at weights that are, are formed again from those
+    float z = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) acc[i] += odd[i];
+    for (int i = 0; i < NI; ++i) z = fmaf(acc[i], 0.0f, z);
+    if (__ballot(z != z && fabsf(l) < __builtin_inff())) {
+      bool had[NI] = {};
+      for (int32_t key = b; key < e; ++key) {
+        const int64_t at = slot_offset(table, uint32_t(key), a, a.v);
+        if (at < 0) continue;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if (lane + 64 * i >= a.hd) continue;
+          const float y = Elt<DT>::ld(vp + at * ES, lane + 64 * i);
+          if (fabsf(y) < __builtin_inff()) continue;
+          acc[i] = had[i] ? acc[i] + y : y;
+          had[i] = true;
+        }
+      }
+    }
     if (a.splits > 1) {
       const int64_t at = row * a.splits + s;
       if (lane == 0) {
