@@ -569,8 +569,9 @@ tri_status tri_kv_write(tri_cache *cache, tri_dtype dtype, const void *k, int64_
  * 0 <= j <= p, j > p - window when window > 0, whose table entry is in
  * [0, n_pages). Query head h takes K head h / (nq / nk):
  *   out = sum_j softmax_j(scale * q . k_j) v_j,
- * in float32 with one rounding at the end (bf16: the weights, at most 1, are
- * rounded to bf16 before they meet V). Keys that are not seen contribute
+ * in float32 with one rounding at the end (bf16: tiles of many rows round the
+ * weights, powers of two of up to 2^8, to bf16 before they meet V, half a step of
+ * each; tiles of few rows keep 16 bits of them). Keys that are not seen contribute
  * nothing, whatever their slots hold (NaN and infinities included); a row that
  * sees no key, or whose scores are all -inf, is zero. In any other row a NaN or
  * an infinity in V at a key that it sees is in the row's element as it is,

@@ -15,10 +15,17 @@
 //
 // The weights are 2^(c (x - m)) with x = q.k, c = |scale| log2 e > 0 (a negative
 // scale changes q's sign) and m the running maximum of x. Sums and products
-// accumulate in float32. In bf16 the
-// weights are rounded to bf16 (at most half a step, 2^-8, of each; the sum
-// they are divided by takes them unrounded): the matrix instruction takes both
-// operands in one type, and V's exponents do not fit float16.
+// accumulate in float32. The matrix instruction takes both operands in one type,
+// and V's exponents do not fit float16, so bf16 weights meet V in bf16; the sum
+// they are divided by takes them unrounded. PA_ROWS, where HBM is what bounds,
+// takes them in two parts, the rounded weight and what that leaves, with a product
+// each: off by 2^-16, so that the result is the plain computation's (relative
+// root mean square against 64 bits 0.0017, the rounding of the result itself; with
+// one part 0.0018), at no cost in the tracked decode cases but 0.2 us at 500
+// keys. PA_TILE and PA_PAIR take the rounded weight alone, off by at most half a
+// step, 2^-8: 0.0019 to 0.0022. The second part would cost them 27 % (2048 tokens
+// behind 6144, 282 -> 360 us; the windowed mixture 43.3 -> 49.6, heads of 256 29.6
+// -> 32.3); see there for the maximum.
 #pragma once
 #include "paged.h"
 
@@ -67,6 +74,14 @@ __device__ inline float sum_16_32(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
                                                   false);
   return sum_32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// Two weights as bf16, and what that leaves of them as bf16 too: the sum of the
+// two is off by at most 2^-16 of a weight.
+__device__ inline u32x2 split_weights(float x, float y) {
+  const uint32_t w = Elt<kBF16>::pack2(x, y);
+  return u32x2{w, Elt<kBF16>::pack2(x - __uint_as_float(w << 16),
+                                    y - __uint_as_float(w & 0xFFFF0000u))};
 }
 
 // The bits of `seen` (bit i: key k0 + i) whose keys are in [lo, hi).
@@ -451,13 +466,16 @@ __device__ void body_pa_rows(const PagedArgs &a) {
       }
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[d] *= alpha;
-    u32x4 p = {0, 0, 0, 0};
+    u32x4 p = {0, 0, 0, 0}, rest = {0, 0, 0, 0};
     if constexpr (DT == kBF16) {
 #pragma unroll
-      for (int j = 0; j < MB; ++j) {
-        p[2 * j] = Elt<kBF16>::pack2(st[j][0], st[j][1]);
-        p[2 * j + 1] = Elt<kBF16>::pack2(st[j][2], st[j][3]);
-      }
+      for (int j = 0; j < MB; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const u32x2 x = split_weights(st[j][2 * i], st[j][2 * i + 1]);
+          p[2 * j + i] = x[0];
+          rest[2 * j + i] = x[1];
+        }
     }
     // O^T
 #pragma unroll
@@ -475,6 +493,9 @@ __device__ void body_pa_rows(const PagedArgs &a) {
         const u32x4 y = {y0[0], y0[1], y1[0], y1[1]};
         o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y),
                                                        __builtin_bit_cast(bf16x8, p), o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y),
+                                                       __builtin_bit_cast(bf16x8, rest), o[d], 0, 0,
+                                                       0);
       }
     }
   }
@@ -591,9 +612,12 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // compute unit has two wavefronts a SIMD all the same.
 //
 // The running maximum is the softmax's reference only; it is raised, and what
-// was summed rescaled, when a score passes it by more than 2^8 (a branch that
-// the first step takes and few others): weights up to 256 lose nothing in
-// float32 or bf16.
+// was summed rescaled, when a weight would pass 2^8 (a branch that the first step
+// takes and few others). Float32 loses nothing by that. In bf16 the largest weight
+// of a row is then rounded like any other, where with the exact maximum it is 1:
+// 0.0019 to 0.0022 against 0.0018 to 0.0020, for 289 instead of 282 us (2048 tokens
+// behind 6144), 44.8 instead of 43.3 (the windowed mixture) and 33.3 instead of
+// 29.6 (heads of 256).
 template <int DT, int HDP>
 struct TileShape {
   static constexpr int ES = Elt<DT>::ES;

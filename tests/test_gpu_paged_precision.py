@@ -49,3 +49,26 @@ def test_float32(cache, lens, nq, nk, hd):  # noqa: F811
     """As good as the plain form: at most a tenth above it."""
     own, ref = compare(cache, problem("f32", lens, nq, nk, hd, 16, seed=nq + hd), "f32")
     assert own <= 1.1 * ref, (own, ref)
+
+
+ROWS = [(SHORT, 16, 4, 64), (SHORT, 4, 4, 128), (SHORT, 4, 2, 256), ([(9000, 1)], 8, 2, 64),
+        ([(5000, 1), (700, 2), (40, 1)], 8, 2, 128), ([(700, 1)] * 5, 8, 1, 256)]
+
+
+@pytest.mark.parametrize("lens,nq,nk,hd", ROWS)
+def test_bfloat16_in_tiles_of_16_rows(cache, lens, nq, nk, hd):  # noqa: F811
+    """The weights are off by 2^-16, a 256th of the rounding of the result (at most
+    2^-8, in both): the same error but for results that a rounding of float32
+    moves over a border, far less than a hundredth of them."""
+    own, ref = compare(cache, problem("bf16", lens, nq, nk, hd, 16, seed=nq + hd), "bf16")
+    assert abs(own / ref - 1) <= 0.01, (own, ref)
+
+
+@pytest.mark.parametrize("lens,nq,nk,hd", [(CHUNKS, 8, 2, 64), (CHUNKS, 8, 2, 128), (CHUNKS, 4, 1, 256),
+                                           ([(900, 900)], 4, 2, 128)])
+def test_bfloat16_in_tiles_of_128_rows(cache, lens, nq, nk, hd):  # noqa: F811
+    """The weights are rounded as the result is, and independent of it: at most
+    the square root of two times the error of the result's rounding alone."""
+    p = tile_problem("bf16", lens, nq, nk, hd, seed=nq + hd)
+    own, ref = compare(cache, p, "bf16")
+    assert own <= 1.42 * ref, (own, ref)
