@@ -158,7 +158,11 @@ def attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
         have = max(_cdiv(T * g, m), min(R, T)) * nk
         want, run = (1024, 1024) if small else (256, 512 if dtype else 256)
         block = (256 if hd > 128 else 512) if small else 256
-        if form == 2 and dtype and hd <= 128 and have <= 224:
+        if T % R == 0:                       # the tiles to expect: of equal chunks, or ragged ones
+            fits = R * _cdiv(T // R * g, 128) * nk < (256 if R > 1 else 257)
+        else:
+            fits = (_cdiv(T * g, 128) + min(R, T) // 2) * nk <= 288
+        if form == 2 and dtype and hd <= 128 and fits:
             form, block = 3, 512
     s = min(want // have, _cdiv(kv_max, run))
     if form == 1 and kv_max > 512:

@@ -227,6 +227,8 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
   return clamp_grid(cdiv(T * int64_t(row_items), kBlock));
 }
 
+static constexpr int64_t kUnits = 256;   // compute units
+
 // Form. Heads the matrix forms do not hold, or rows that are not aligned, take
 // PA_ANY. Tiles of 16 rows (PA_ROWS) serve decode, and chunks whose tiles of
 // 128 would be few or mostly empty; rpr: rows of a request and K head, were the
@@ -238,12 +240,18 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items) {
 // float32, whose products cost 16 times as much, gains from full tiles up to
 // 256 rows: 16 requests of 64 / 128 new tokens, 32 and 8 heads of 128 (256 /
 // 512 rows), 253 / 474 us against 287 / 304; one of 64 / 128: 39 / 62 against
-// 51 / 53. Where the tiles of 128 leave some compute units without one, two
-// groups of wavefronts share a tile's keys (PA_PAIR, which fills a unit's LDS:
-// 24 requests of up to 3700 keys, 218 tiles: 74.6 -> 52.7 us; 512 tokens behind
-// 8192, 128: 130 -> 104; 12 requests of 64 behind 1000, 192: 43 -> 30; 700
-// alone, 176: 24.7 -> 21.0); with a tile for every unit some get two (16 of 64
-// behind 1000, 256: 43.8 -> 54.4).
+// 51 / 53. Where no compute unit gets two tiles of 128, two groups of
+// wavefronts share a tile's keys (PA_PAIR, which fills a unit's LDS), so what
+// counts is the tiles to expect against the 256 units: of one request, or of
+// chunks that may be equal, those of equal chunks; else half a tile more for each
+// request. Two groups against one, tiles expected: 700 tokens alone (176) 20.9
+// us against 24.6; 1000 alone (256) 26.5, 33.1; 14 of 60 behind 2000 (224) 50.6,
+// 73.8; 15 of 64 behind 3000 (240) 70.6, 102.9; ragged chunks (208 to 256) 45.1,
+// 60.8; 41.8, 50.8; 47.7, 59.1. Beyond, some units get two, and equal tiles end
+// together, so one such unit doubles the call: 16 of 64 behind 3000 (256) 124
+// against 103; 11 of 70 behind 2000 (264) 83.7, 72.1; 9 of 100 (288) 87.5, 74.3.
+// Ragged ones end unevenly all the same and bear an eighth more (264: 53.8, 66.1;
+// 284: 43.6, 57.5; but 312: 65.5, 63.7; 348: 70.4, 61.0).
 //
 // Splits. Few tiles leave compute units idle, so their keys are split until
 // there are `want` workgroups, in runs of at least `run` keys; the join costs
@@ -277,7 +285,10 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
     have = (full > busy ? full : busy) * nk;
     want = few ? 1024 : 256;
     run = few ? 1024 : f32 ? 256 : 512;
-    if (!few && !f32 && hd <= 128 && have <= 224) {
+    const bool equal = T % R == 0;
+    const int64_t expected = (equal ? R * cdiv(T / R * g, 128) : full + busy / 2) * nk;
+    const int64_t most = !equal ? kUnits * 9 / 8 : R > 1 ? kUnits - 1 : kUnits;
+    if (!few && !f32 && hd <= 128 && expected <= most) {
       p.form = kAttnPair;
       p.block = 2 * kBlock;
     }

@@ -4,6 +4,7 @@ import ctypes as C
 
 import pytest
 
+from oracle import paged as P
 from paper_2609_37241_amd import _lib as L
 from tests.native_libs import load_fake
 from tests.test_host_paged import at, attn, kv, last, launches, read_args, slots_args
@@ -77,3 +78,18 @@ def test_the_bytes_of_the_largest_caches(lib, fresh):
     c = kv(n_pages=9, page=65536, nk=4096, hd=256)
     for R, cols in ((2048, 1 << 14), (1024, (1 << 15) - 1), (4095, (1 << 15) - 1)):
         assert stream_flag(lib, fresh, L.F32, 1, R, 4096, cols, c) == 1
+
+
+@pytest.mark.parametrize("R,T,nq,nk,form", [
+    (15, 15 * 64, 32, 8, P.PA_PAIR), (16, 16 * 64, 32, 8, P.PA_TILE),     # 240, 256 equal tiles
+    (14, 14 * 60, 32, 8, P.PA_PAIR), (11, 11 * 70, 32, 8, P.PA_TILE),     # 224, 264
+    (1, 1024, 32, 8, P.PA_PAIR), (1, 1025, 32, 8, P.PA_TILE),             # 256, 264 of one request
+    (22, 800, 32, 8, P.PA_PAIR), (23, 831, 32, 8, P.PA_TILE),             # 288, 296 ragged ones
+    (24, 1740, 16, 2, P.PA_PAIR), (40, 601, 32, 4, P.PA_PAIR), (48, 1301, 32, 4, P.PA_TILE)])
+def test_pairs_where_no_unit_gets_two_tiles(lib, fresh, R, T, nq, nk, form):
+    c = kv(n_pages=9, nk=nk, hd=128)
+    a = attn(L.BF16, T, R, nq, 400, c)
+    assert lib.tri_paged_attention(fresh, C.byref(a), None) == 0
+    s = last(lib, fresh)
+    assert s.variant == form
+    assert launches(s) == P.attention_selection(1, T, R, nq, nk, 128, True, 6400, 0)[1]
