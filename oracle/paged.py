@@ -162,7 +162,7 @@ def attention_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
             fits = R * _cdiv(T // R * g, 128) * nk < (256 if R > 1 else 257)
         else:
             fits = (_cdiv(T * g, 128) + min(R, T) // 2) * nk <= 288
-        if form == 2 and dtype and hd <= 128 and fits:
+        if form == 2 and dtype and hd <= 128 and fits and _cdiv(T * g, 128) * nk <= 256:
             form, block = 3, 512
     s = min(want // have, _cdiv(kv_max, run))
     if form == 1 and kv_max > 512:

@@ -250,8 +250,8 @@ static constexpr int64_t kUnits = 256;   // compute units
 // 60.8; 41.8, 50.8; 47.7, 59.1. Beyond, some units get two, and equal tiles end
 // together, so one such unit doubles the call: 16 of 64 behind 3000 (256) 124
 // against 103; 11 of 70 behind 2000 (264) 83.7, 72.1; 9 of 100 (288) 87.5, 74.3.
-// Ragged ones end unevenly all the same and bear an eighth more (264: 53.8, 66.1;
-// 284: 43.6, 57.5; but 312: 65.5, 63.7; 348: 70.4, 61.0).
+// Ragged ones end unevenly all the same and bear an eighth more, if not of full
+// tiles (264: 53.8, 66.1; 284: 43.6, 57.5; but 312: 65.5, 63.7; 348: 70.4, 61.0).
 //
 // Splits. Few tiles leave compute units idle, so their keys are split until
 // there are `want` workgroups, in runs of at least `run` keys; the join costs
@@ -288,7 +288,7 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
     const bool equal = T % R == 0;
     const int64_t expected = (equal ? R * cdiv(T / R * g, 128) : full + busy / 2) * nk;
     const int64_t most = !equal ? kUnits * 9 / 8 : R > 1 ? kUnits - 1 : kUnits;
-    if (!few && !f32 && hd <= 128 && expected <= most) {
+    if (!few && !f32 && hd <= 128 && full * nk <= kUnits && expected <= most) {
       p.form = kAttnPair;
       p.block = 2 * kBlock;
     }

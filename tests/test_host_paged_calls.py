@@ -85,7 +85,7 @@ def test_the_bytes_of_the_largest_caches(lib, fresh):
     (14, 14 * 60, 32, 8, P.PA_PAIR), (11, 11 * 70, 32, 8, P.PA_TILE),     # 224, 264
     (1, 1024, 32, 8, P.PA_PAIR), (1, 1025, 32, 8, P.PA_TILE),             # 256, 264 of one request
     (22, 800, 32, 8, P.PA_PAIR), (23, 831, 32, 8, P.PA_TILE),             # 288, 296 ragged ones
-    (24, 1740, 16, 2, P.PA_PAIR), (40, 601, 32, 4, P.PA_PAIR), (48, 1301, 32, 4, P.PA_TILE)])
+    (24, 1740, 16, 2, P.PA_PAIR), (3, 1027, 32, 8, P.PA_TILE), (40, 601, 32, 4, P.PA_PAIR), (48, 1301, 32, 4, P.PA_TILE)])
 def test_pairs_where_no_unit_gets_two_tiles(lib, fresh, R, T, nq, nk, form):
     c = kv(n_pages=9, nk=nk, hd=128)
     a = attn(L.BF16, T, R, nq, 400, c)
