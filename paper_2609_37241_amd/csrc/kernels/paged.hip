@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
   constexpr int ES = Elt<DT>::ES;
   constexpr int NI = 8;   // 512 / 64
   __shared__ float qs[4][512];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t items = int64_t(a.T) * a.nq * a.splits;
   for (int64_t it = int64_t(blockIdx.x) * 4 + wave; it < items; it += int64_t(gridDim.x) * 4) {
     const int64_t row = it / a.splits;
@@ -285,17 +285,19 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) z = fmaf(acc[i], 0.0f, z);
     if (__ballot(z != z && fabsf(l) < __builtin_inff())) {
-      bool had[NI] = {};
+      uint32_t had = 0;   // bit i: acc[i] holds only those
+#pragma unroll 1
       for (int32_t key = b; key < e; ++key) {
         const int64_t at = slot_offset(table, uint32_t(key), a, a.v);
         if (at < 0) continue;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          if (lane + 64 * i >= a.hd) continue;
-          const float y = Elt<DT>::ld(vp + at * ES, lane + 64 * i);
-          if (fabsf(y) < __builtin_inff()) continue;
-          acc[i] = had[i] ? acc[i] + y : y;
-          had[i] = true;
+          const int d = lane + 64 * i;
+          const float y = d < a.hd ? Elt<DT>::ld(vp + at * ES, d) : 0.0f;
+          const bool odd = !(fabsf(y) < __builtin_inff());
+          const float sum = had & (1u << i) ? acc[i] + y : y;
+          acc[i] = odd ? sum : acc[i];
+          had |= odd ? 1u << i : 0u;
         }
       }
     }
@@ -329,7 +331,7 @@ __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
 template <int DT, int VEC>
 __device__ void join_rows(const PagedArgs &a) {
   __shared__ float sums[4][64 * VEC];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t t0 = clamp_i32(a.q_start[0], 0, a.T), t1 = clamp_i32(a.q_start[a.R], 0, a.T);
   const bool four = a.splits > kJoinWave;
   // lanes across the elements (a power of two), groups across the splits
@@ -368,7 +370,18 @@ __device__ void join_rows(const PagedArgs &a) {
     float sum = l != 0.0f ? w * l : 0.0f;
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    char *o = static_cast<char *>(a.out) + (int64_t(t) * a.o_ts + int64_t(h) * a.hd) * Elt<DT>::ES;
+    const auto put = [&](int d, float *acc) {
+      if (d >= a.hd || lane >= nl || (four && wave != 0)) return;
+      char *o = static_cast<char *>(a.out) + (int64_t(t) * a.o_ts + int64_t(h) * a.hd) * Elt<DT>::ES;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) acc[c] = sum == 0.0f ? 0.0f : acc[c] / sum;
+      if constexpr (VEC == 4 && DT == kF32)
+        st_any<kF32, false>(o + d * 4, Elt<kF32>::pack(acc));
+      else
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) Elt<DT>::st(o, d + c, acc[c]);
+    };
+    bool odd = false;
     for (int d0 = 0; d0 < a.hd; d0 += nl * VEC) {   // (every lane stays: they exchange)
       const int d = d0 + e;
       float acc[VEC] = {};
@@ -400,27 +413,22 @@ __device__ void join_rows(const PagedArgs &a) {
           acc[c] = (sums[0][lane * VEC + c] + sums[1][lane * VEC + c]) +
                    (sums[2][lane * VEC + c] + sums[3][lane * VEC + c]);
       }
-      bool odd = false;
 #pragma unroll
       for (int c = 0; c < VEC; ++c) odd |= !(fabsf(acc[c]) < __builtin_inff());
-      if (__ballot(odd)) {   // infinities or NaN of V, maybe where a weight is 0
-#pragma unroll
-        for (int c = 0; c < VEC; ++c) acc[c] = 0.0f;
+      put(d, acc);
+    }
+    if (__ballot(odd)) {   // infinities or NaN of V, maybe where a weight is 0: once more
+      for (int d0 = 0; d0 < a.hd; d0 += nl * VEC) {
+        const int d = d0 + e;
+        float acc[VEC] = {};
+#pragma unroll 1
         for (int s = 0; s < a.splits; ++s) {
-          read(s, d, x[0]);
           const float ws = __shfl(w, s);
 #pragma unroll
-          for (int c = 0; c < VEC; ++c) acc[c] = add_part(ws, x[0][c], acc[c]);
+          for (int c = 0; c < VEC; ++c)
+            if (d < a.hd) acc[c] = add_part(ws, a.part[(at + s) * a.hd + d + c], acc[c]);
         }
-      }
-      if (d < a.hd && lane < nl && (!four || wave == 0)) {
-#pragma unroll
-        for (int c = 0; c < VEC; ++c) acc[c] = sum == 0.0f ? 0.0f : acc[c] / sum;
-        if constexpr (VEC == 4 && DT == kF32)
-          st_any<kF32, false>(o + d * 4, Elt<kF32>::pack(acc));
-        else
-#pragma unroll
-          for (int c = 0; c < VEC; ++c) Elt<DT>::st(o, d + c, acc[c]);
+        put(d, acc);
       }
     }
   }
