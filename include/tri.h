@@ -128,7 +128,8 @@ enum {
 typedef struct tri_launch_rec {
   int32_t variant;     /* kernel variant id (the install policy table)       */
   uint32_t grid_x;     /* workgroups                                          */
-  uint32_t block_x;    /* work-items per workgroup (256; 1024 for variant 19) */
+  uint32_t block_x;    /* work-items per workgroup: 256; 1024 for variant 19;
+                        * 512 for variant 91 with heads of up to 128, and 94  */
 } tri_launch_rec;
 
 /* Words of the packed guard key. */
@@ -546,6 +547,10 @@ tri_status tri_embedding(tri_cache *cache, tri_dtype dtype, const void *table, i
  *     entry, beyond the table); rows from q_start[R] on: slots -1, pos 0;
  *   free_out = {pages left on the stack, pages that were missing}: the count of
  *     the next call's stack (free_count is clamped to [0, n_free]).
+ * kv_len_out and q_start count tokens that found no place too: beyond the table
+ * (kv_len_out > cols * page) or beyond T (q_start[R] > T). tri_paged_attention
+ * clamps both, which moves the positions of that request's rows: room for all
+ * tokens of a step is the caller's to see to.
  * The outputs must not overlap each other or an input (kv_len, free_count and
  * free_pages are read while they are written); the table row stride is at
  * least cols. cols * page and R * cols must be below 2^31, page 1..TRI_MAX_PAGE. All
@@ -557,7 +562,7 @@ tri_status tri_kv_slots(tri_cache *cache, const tri_kv_slots_args *args, void *s
  * K[slots[t] / page][slots[t] % page] = k[t], V likewise. A slot outside
  * [0, n_pages * page) is skipped. The slots of one call must be distinct: of
  * two rows with one slot either may remain, vector by vector. k and v must not
- * overlap the cache. hd 1..512, nk 1..4096. */
+ * overlap the cache, nor slots of K those of V. hd 1..512, nk 1..4096. */
 tri_status tri_kv_write(tri_cache *cache, tri_dtype dtype, const void *k, int64_t k_ts,
                         const void *v, int64_t v_ts, const int64_t *slots, int64_t T,
                         const tri_kv_cache *kv, void *stream);

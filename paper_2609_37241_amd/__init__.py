@@ -668,7 +668,8 @@ class SpecCache:
         (int32 [R, cols], updated in place; -1 where the stack is empty). Returns slots
         (int64 [T], -1 without a page and past the last request), pos (int32 [T]), q_start
         (int32 [R + 1]), kv_len_out (int32 [R]) and free_out (int32 [2]: pages left, pages
-        missing; the next step's free_count)."""
+        missing; the next step's free_count). T rows and the table are to hold all tokens of the
+        step: lengths count those that find no place too, and attention clamps them."""
         if self._rec is None:
             r = self._fast.kv_slots(self, kv_len, new_len, block_table, free_pages, free_count,
                                     page, T, slots, pos, q_start, kv_len_out, free_out, stream)

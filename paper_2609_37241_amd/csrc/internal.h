@@ -173,6 +173,10 @@ inline bool is_paged_op(uint32_t op) { return op >= TRI_OP_KV_SLOTS && op <= TRI
 // share out the keys).
 enum AttnForm : uint32_t { kAttnAny = 0, kAttnRows = 1, kAttnTile = 2, kAttnPair = 3 };
 constexpr int32_t kAttnMatrixHd = 256;     // head sizes of the matrix forms
+// Whether they serve a head size: whole 16-byte vectors at 16-byte alignment.
+inline bool attn_matrix(uint32_t dtype, bool aligned, int32_t hd) {
+  return aligned && hd % vec_elems(dtype) == 0 && hd <= kAttnMatrixHd;
+}
 // The head size that a matrix kernel holds: hd rounded up to 64, 128 or 256.
 inline int32_t attn_hdp(int32_t hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }
 inline uint32_t key_attn_form(const Key &k) { return uint32_t((k.k3 >> 16) & 0xFF); }
@@ -195,7 +199,6 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
 inline uint64_t attn_workspace(int64_t T, int32_t nq, int32_t hd, int32_t splits) {
   return splits > 1 ? uint64_t(T) * uint64_t(nq) * uint64_t(splits) * uint64_t(hd + 2) * 4 : 0;
 }
-// Whether the matrix forms serve a head size at 16-byte alignment.
 uint32_t kv_slots_grid(int64_t T, int32_t R);
 uint32_t kv_write_grid(int64_t T, uint32_t row_items);
 // n / d by multiplication (kernargs.h).

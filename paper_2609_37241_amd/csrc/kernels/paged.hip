@@ -207,9 +207,11 @@ __global__ __launch_bounds__(256) void k_kv_write(KvWriteArgs a) {
 // one key's score from the query in LDS, the running maximum and sum of the
 // softmax are the wavefront's, and for the sums of V lane l holds the elements
 // l, l + 64, ... of the head. No alignment, any head size up to 512; a key that
-// is not seen is never read. It serves what the matrix forms do not, at the
-// rate of its element-wise reads: 8 requests of 2000 keys, 32 + 8 heads of 36 in
-// bf16, 125 us (aligned heads of 40 in PA_ROWS: 16).
+// is not seen is never read. It serves what the matrix forms do not: rows at any
+// alignment, heads of no whole number of vectors, and all heads of more than 256,
+// also aligned ones. An element a load bounds it: 8 requests of 2000 keys, 32 + 8
+// heads, bf16 of 36 125 us (aligned heads of 40 in PA_ROWS: 16) and of 512 920, float32
+// of 33 130 and of 320 697.
 template <int DT>
 __global__ __launch_bounds__(256) void k_pa_any(PagedArgs a) {
   constexpr int ES = Elt<DT>::ES;

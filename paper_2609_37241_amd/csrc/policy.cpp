@@ -274,7 +274,7 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
   int64_t have = cdiv(rows, 4), want = 512, run = 256, tiles = 0;
   p.form = kAttnAny;
   p.block = kBlock;
-  if (aligned && hd % vec_elems(dtype) == 0 && hd <= kAttnMatrixHd) {
+  if (attn_matrix(dtype, aligned, hd)) {
     const int64_t rpr = cdiv(T, R) * g, tiles16 = cdiv(T * g, 16) * nk;
     const bool few = rpr <= (f32 ? 256 : 16) || (tiles16 <= 64 && kv_max <= 4096);
     p.form = few ? kAttnRows : kAttnTile;
@@ -374,8 +374,7 @@ static bool paged_key_valid(const Key &k) {
   const uint32_t form = key_attn_form(k);
   if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
   if (k.k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
-  const bool matrix = (key_flags(k) & kAlign) && int32_t(hd) <= kAttnMatrixHd &&
-                      hd % uint32_t(vec_elems(key_dtype(k))) == 0;
+  const bool matrix = attn_matrix(key_dtype(k), key_flags(k) & kAlign, int32_t(hd));
   if (form == kAttnPair && (key_dtype(k) == TRI_F32 || hd > 128)) return false;
   return matrix ? form >= kAttnRows && form <= kAttnPair : form == kAttnAny;
 }
