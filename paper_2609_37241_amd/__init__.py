@@ -22,6 +22,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import operator
 import warnings
 from typing import Optional, Tuple
 
@@ -220,6 +221,15 @@ def _vector(t: torch.Tensor, name: str, n: int, dtype, dev: int) -> None:
     _on(t, name, dev)
 
 
+def _whole(v, name: str, bits: int = 32) -> int:
+    """An integer that a signed field of `bits` holds: ctypes would cut any other
+    down to one that does."""
+    n = operator.index(v)
+    if not -(1 << (bits - 1)) <= n < 1 << (bits - 1):
+        raise ValueError(f"{name}: {n} is beyond {bits} bits")
+    return n
+
+
 def _kv_view(t: torch.Tensor, name: str, n: int, page: int, nk: int, hd: int) -> tuple:
     """Page, slot and head strides (elements) of a cache [n_pages, page, nk, hd]
     whose heads are contiguous; dimensions of one report what a packed cache has."""
@@ -233,7 +243,7 @@ def _kv_view(t: torch.Tensor, name: str, n: int, page: int, nk: int, hd: int) ->
 
 def _kv_cache(k: torch.Tensor, v: torch.Tensor, dtype, dev: int) -> L.KvCache:
     """The tri_kv_cache of k and v [n_pages, page, nk, hd]."""
-    n, page, nk, hd = _dims(k, "k_cache", 4, dev)
+    n, page, nk, hd = (_whole(x, "k_cache") for x in _dims(k, "k_cache", 4, dev))
     _like(v, "v_cache", k.shape, dtype, dev)
     _like(k, "k_cache", k.shape, dtype, dev)
     return L.KvCache(k.data_ptr(), v.data_ptr(), *_kv_view(k, "k_cache", n, page, nk, hd),
@@ -255,7 +265,7 @@ def _table(t: torch.Tensor, name: str, dev: int) -> tuple:
     R, cols = _dims(t, name, 2, dev)
     if t.dtype != torch.int32:
         raise ValueError(f"{name}: expected int32, got {t.dtype}")
-    return R, cols, _rows(t, name, cols)
+    return _whole(R, name), _whole(cols, name), _rows(t, name, cols)
 
 
 class Graph:
@@ -677,7 +687,7 @@ class SpecCache:
                 return r
         dev = self._dev
         R, cols, rs = _table(block_table, "block_table", dev)
-        T = int(T)
+        T, page = _whole(int(T), "T", 64), _whole(page, "page")
         kv, nw = _int32(kv_len, "kv_len", R, dev), _int32(new_len, "new_len", R, dev)
         fp = _int32(free_pages, "free_pages", free_pages.numel(), dev)
         fc = _int32(free_count, "free_count", -1, dev)
@@ -689,7 +699,7 @@ class SpecCache:
         q_start, kv_len_out, free_out = new(q_start, R + 1), new(kv_len_out, R), new(free_out, 2)
         _vector(slots, "slots", T, torch.int64, dev)
         a = L.KvSlotsArgs(T, R, page, kv, nw, block_table.data_ptr(), rs, cols,
-                          free_pages.shape[0], fp, fc, slots.data_ptr(),
+                          _whole(free_pages.shape[0], "free_pages"), fp, fc, slots.data_ptr(),
                           _int32(pos, "pos", T, dev), _int32(q_start, "q_start", R + 1, dev),
                           _int32(kv_len_out, "kv_len_out", R, dev),
                           _int32(free_out, "free_out", 2, dev))
@@ -741,11 +751,12 @@ class SpecCache:
         kv = _kv_cache(k_cache, v_cache, q.dtype, dev)
         if kv.hd != hd:
             raise ValueError(f"k_cache: expected heads of {hd}, got {kv.hd}")
-        a = L.AttentionArgs(dtype_code(q.dtype), nq, T, R, cols, q.data_ptr(),
+        a = L.AttentionArgs(dtype_code(q.dtype), _whole(nq, "q"), T, R, cols, q.data_ptr(),
                             _tokens(q, "q", nq, hd), o.data_ptr(), _tokens(o, "out", nq, hd),
                             block_table.data_ptr(), rs, _int32(kv_len, "kv_len", R, dev),
                             _int32(q_start, "q_start", R + 1, dev),
-                            hd ** -0.5 if scale is None else scale, window, max_kv, None, 0, kv)
+                            hd ** -0.5 if scale is None else scale, _whole(window, "window"),
+                            _whole(max_kv, "max_kv", 64), None, 0, kv)
         need = _dll.tri_paged_attention_workspace(C.byref(a))
         if need:
             a._workspace = self._made(None, q, stream, need, torch.uint8)
