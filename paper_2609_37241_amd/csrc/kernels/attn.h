@@ -602,10 +602,11 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // about as much, so two workgroups a compute unit fill each other's gaps. The
 // next keys' loads are in flight during the products, and go to the other half
 // of LDS between them (one barrier a step). 2048 rows behind 6144 keys, 32 + 8
-// heads of 128 in bf16: 269 to 280 us, 858 to 893 TFLOP/s by box; the matrix pipes
-// are busy for 41 % of it. Heads of 256 leave one workgroup a compute unit: four
-// prompts of up to 1024 tokens, 16 heads, 28.8 us; 2048 tokens behind 2048, 195
-// us, 530 TFLOP/s (with steps of 32 keys 8 % more).
+// heads of 128 in bf16: 275 to 304 us, 792 to 875 TFLOP/s by box (a call back to
+// back with others; alone after a pause, or under a profiler, 5 % more); the matrix
+// pipes are busy for 40 % of it. Heads of 256 leave one workgroup a compute unit:
+// four prompts of up to 1024 tokens, 16 heads, 29.5 us; 2048 tokens behind 2048,
+// 194 us, 530 TFLOP/s (with steps of 32 keys 8 % more).
 //
 // With two groups of four wavefronts (PA_PAIR) each takes every other step, on
 // tiles of its own, and the first adds up both: where the tiles are few, a

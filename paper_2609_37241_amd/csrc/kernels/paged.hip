@@ -161,7 +161,9 @@ __global__ __launch_bounds__(256) void k_kv_slots(KvSlotsArgs a) {
 // V; a row's items are the K row's, then the V row's, so a workgroup writes
 // whole heads. The load does not wait for the slot. HBM-bound from about a
 // thousand rows on, latency below: 8192 rows of 8 + 8 heads of 128 in bf16 (67
-// MB) 13.0 us, 5.2 TB/s; 8 rows 2.4 us.
+// MB) 13.0 us, 5.2 TB/s; 8 rows 2.4 us. An element a work-item (KVW_ANY) is bound
+// by the number of its loads and stores: 8192 rows of 8 + 8 heads of 36 in bf16 (19
+// MB) 15 us, of 33 in float32 (35 MB) 16; of 40 by vectors 5.4.
 template <int DT, bool VEC>
 __global__ __launch_bounds__(256) void k_kv_write(KvWriteArgs a) {
   constexpr int N = VEC ? Elt<DT>::V : 1;

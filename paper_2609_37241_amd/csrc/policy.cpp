@@ -258,14 +258,14 @@ static constexpr int64_t kUnits = 256;   // compute units
 // 4 us and the traffic of the sums. PA_ROWS wants 1024 (64 requests of up to
 // 8k tokens, where the longest decides, read without streaming: 214 us; 512
 // workgroups 227, 2048 212; streamed 193 and 193 to 200)
-// and runs of 1024 (six requests in float32, 300 tiles: 22.6 us, runs of 512
+// and runs of 1024 (six requests in float32, 300 tiles: 23.0 us, runs of 512
 // about 3 more); but idle compute units take shorter ones, of 256 (a step of a
 // workgroup takes 2.2 us, the latency of its loads: a request of 32 heads and
 // 2000 tokens 12.4 us against 18.6), from 512 keys on (500 tokens: 10.1 us against 11.5
 // split in two). PA_TILE wants 256, one a compute unit, rounded
-// down (24 requests with a window, 218 workgroups: 42.5 us against 61.8 split
+// down (24 requests with a window, 218 workgroups: 43.3 us against 61.8 split
 // in two), and runs of 512 keys (four prompts of up to 1024 tokens, heads of
-// 256: 28.8 us against 42.8 split), 256 in float32, whose steps take longer.
+// 256: 29.5 us against 42.8 split), 256 in float32, whose steps take longer.
 AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                    bool aligned, int64_t kv_max, uint64_t workspace) {
   AttnPlan p{};
