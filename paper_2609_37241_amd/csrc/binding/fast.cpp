@@ -26,7 +26,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <stdexcept>
 #include <vector>
 
 #include "tri.h"
@@ -117,26 +116,17 @@ bool stream_of(const Handle *h, PyObject *o, void **s) {
   return false;
 }
 
-// While it lives torch allocates on the call's stream, where the outputs and
-// workspaces made meanwhile are written: their memory is handed on only after
-// that work. Nothing for the current stream (None); a C++ exception, and so the
-// Python form, for an object without torch's three numbers of a stream.
+// While it lives torch allocates on the call's stream `s` (given as `o`), where
+// the outputs and workspaces made meanwhile are written: their memory is handed
+// on only after that work. Nothing where no stream was given: it is the current.
+// (The allocator knows streams by their address, so any wrapper of it will do.)
 struct MakingOn {
   c10::OptionalStreamGuard g;
-  explicit MakingOn(PyObject *stream) {
-    if (stream == Py_None) return;
-    const char *names[3] = {"stream_id", "device_index", "device_type"};
-    int64_t v[3];
-    for (int i = 0; i < 3; ++i) {
-      PyObject *o = PyObject_GetAttrString(stream, names[i]);
-      v[i] = o ? PyLong_AsLongLong(o) : -1;
-      Py_XDECREF(o);
-      if (PyErr_Occurred()) {
-        PyErr_Clear();
-        throw std::invalid_argument(names[i]);
-      }
-    }
-    g.reset_stream(c10::Stream::unpack3(v[0], c10::DeviceIndex(v[1]), c10::DeviceType(v[2])));
+  MakingOn(const Handle *h, PyObject *o, void *s) {
+    if (o == Py_None) return;
+    const auto d = c10::DeviceIndex(h->dev);
+    g.reset_stream(c10::Stream(c10::Stream::UNSAFE, c10::Device(at::kCUDA, d),
+                               c10::hip::getStreamFromExternal(hipStream_t(s), d).id()));
   }
 };
 
@@ -187,14 +177,14 @@ bool issue(PyObject *owner, const char *what, F &&call, int64_t misses = 1) {
 struct Out {
   at::Tensor t;
   PyObject *given = nullptr;
-  bool take(PyObject *o, const at::Tensor &like, int dev, PyObject *stream) {
+  bool take(PyObject *o, const at::Tensor &like, const Handle *h, PyObject *stream, void *s) {
     if (o == Py_None) {
-      MakingOn on(stream);
+      MakingOn on(h, stream, s);
       NoGil g;
       t = at::empty_like(like);
       return true;
     }
-    const at::Tensor *p = plain(o, dev);
+    const at::Tensor *p = plain(o, h->dev);
     if (!p || !same(*p, like)) return false;
     t = *p;
     given = o;
@@ -244,7 +234,7 @@ PyObject *rmsnorm(Handle *h, PyObject *owner, PyObject *const *a) {
     Py_RETURN_NONE;
   const int64_t T = x->size(0), H = x->size(1), xs = rows(*x);
   Out y;
-  if (xs < 0 || !y.take(a[3], *x, h->dev, a[4])) Py_RETURN_NONE;
+  if (xs < 0 || !y.take(a[3], *x, h, a[4], s)) Py_RETURN_NONE;
   const int64_t ys = rows(y.t);
   if (ys < 0) Py_RETURN_NONE;
   const tri_dtype dt = tri_dtype(dtype_of(*x));
@@ -266,8 +256,8 @@ PyObject *residual_rmsnorm(Handle *h, PyObject *owner, PyObject *const *a) {
     Py_RETURN_NONE;
   const int64_t T = x->size(0), H = x->size(1), xs = rows(*x), rs = rows(*r);
   Out y, o;
-  if (xs < 0 || rs < 0 || !y.take(a[4], *x, h->dev, a[6]) ||
-      !o.take(a[5], *r, h->dev, a[6]))
+  if (xs < 0 || rs < 0 || !y.take(a[4], *x, h, a[6], s) ||
+      !o.take(a[5], *r, h, a[6], s))
     Py_RETURN_NONE;
   const int64_t ys = rows(y.t), os = rows(o.t);
   if (ys < 0 || os < 0) Py_RETURN_NONE;
@@ -294,7 +284,7 @@ PyObject *flat(Handle *h, PyObject *owner, PyObject *const *a) {
     Py_RETURN_NONE;
   const int64_t T = x->size(0), W = x->size(1), xs = rows(*x), bs = rows(*b);
   Out y;
-  if (xs < 0 || bs < 0 || !y.take(rest[0], *x, h->dev, rest[1])) Py_RETURN_NONE;
+  if (xs < 0 || bs < 0 || !y.take(rest[0], *x, h, rest[1], s)) Py_RETURN_NONE;
   const int64_t ys = rows(y.t);
   if (ys < 0) Py_RETURN_NONE;
   const tri_dtype dt = tri_dtype(dtype_of(*x));
@@ -324,7 +314,7 @@ PyObject *masked_fill(Handle *h, PyObject *owner, PyObject *const *a) {
     Py_RETURN_NONE;
   const int64_t T = x->size(0), W = x->size(1), xs = rows(*x), ms = rows(*m);
   Out y;
-  if (xs < 0 || ms < 0 || !y.take(a[3], *x, h->dev, a[4])) Py_RETURN_NONE;
+  if (xs < 0 || ms < 0 || !y.take(a[3], *x, h, a[4], s)) Py_RETURN_NONE;
   const int64_t ys = rows(y.t);
   if (ys < 0) Py_RETURN_NONE;
   const tri_dtype dt = tri_dtype(dtype_of(*x));
@@ -350,7 +340,7 @@ PyObject *embedding(Handle *h, PyObject *owner, PyObject *const *a) {
   if (ts < 0 || (T > 1 && ids->stride(0) != 1)) Py_RETURN_NONE;
   Out y;
   if (a[2] == Py_None) {
-    MakingOn on(a[3]);
+    MakingOn on(h, a[3], s);
     NoGil g;
     y.t = at::empty({T, H}, t->options());
   } else {
@@ -544,7 +534,7 @@ PyObject *kv_slots(Handle *h, PyObject *owner, PyObject *const *a) {
   // what the next step takes (kv_len_out, free_out) another
   at::Tensor made[5];
   {
-    MakingOn on(a[12]);
+    MakingOn on(h, a[12], s);
     NoGil g;
     for (int b = 0; b < 5; b = b ? 5 : 3) {
       const int e = b ? 5 : 3;
@@ -633,7 +623,7 @@ PyObject *paged_attention(Handle *h, PyObject *owner, PyObject *const *a) {
     Py_RETURN_NONE;
   Out y;
   if (a[9] == Py_None && !q->is_contiguous()) Py_RETURN_NONE;
-  if (!y.take(a[9], *q, h->dev, a[10])) Py_RETURN_NONE;
+  if (!y.take(a[9], *q, h, a[10], s)) Py_RETURN_NONE;
   x.dtype = dtype_of(*q);
   x.nq = int32_t(q->size(1));
   x.T = q->size(0);
@@ -650,7 +640,7 @@ PyObject *paged_attention(Handle *h, PyObject *owner, PyObject *const *a) {
   x.window = int32_t(window);
   at::Tensor work;
   if (const int64_t need = tri_paged_attention_workspace(&x)) {
-    MakingOn on(a[10]);
+    MakingOn on(h, a[10], s);
     NoGil g;
     work = at::empty({need}, q->options().dtype(at::kByte));
     x.workspace = work.data_ptr();
