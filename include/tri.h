@@ -582,8 +582,9 @@ tri_status tri_kv_write(tri_cache *cache, tri_dtype dtype, const void *k, int64_
  * an infinity in V at a key that it sees is in the row's element as it is,
  * whatever the key's weight. Rows of out before
  * q_start[0] and from q_start[R] on are left as they were. kv_len is clamped
- * to [0, cols * page], q_start to [0, T] and must not decrease (rows that two
- * requests claim hold either's result). out may alias q exactly.
+ * to [0, cols * page], q_start to [0, T] and must not decrease (else the rows that
+ * two requests claim, or none between q_start[0] and q_start[R], hold anything).
+ * out may alias q exactly.
  * The keys of a tile of queries may be split over several workgroups that
  * leave partial results in `workspace` (16-byte aligned device memory of the
  * caller, its contents undefined before and after; two calls that may run at

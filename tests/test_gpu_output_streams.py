@@ -69,6 +69,19 @@ def test_made_outputs(cache, op):
     assert owner(made[0] if isinstance(made, tuple) else made) == there.cuda_stream
 
 
+@pytest.mark.parametrize("op", OPS)
+def test_the_default_stream_from_another(cache, op):
+    args = operands()[op]
+    there, default = torch.cuda.Stream(), torch.cuda.default_stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(there):
+        made = getattr(cache, op)(*args, stream=default)
+        assert torch.cuda.current_stream() == there
+        torch.cuda.synchronize()
+    for t in made if isinstance(made, tuple) else (made,):
+        assert owner(t) == default.cuda_stream
+
+
 @pytest.mark.parametrize("op", ["rmsnorm", "paged_attention"])
 def test_a_stream_that_torch_did_not_make(cache, op):
     """Anything with the address of a stream is taken as before."""
