@@ -23,7 +23,7 @@
 // root mean square against 64 bits 0.0017, the rounding of the result itself; with
 // one part 0.0018), at no cost in the tracked decode cases but 0.2 us at 500
 // keys. PA_TILE and PA_PAIR take the rounded weight alone, off by at most half a
-// step, 2^-8: 0.0019 to 0.0022. The second part would cost them 27 % (2048 tokens
+// step, 2^-8: 0.0019 to 0.0023. The second part would cost them 27 % (2048 tokens
 // behind 6144, 282 -> 360 us; the windowed mixture 43.3 -> 49.6, heads of 256 29.6
 // -> 32.3); see there for the maximum.
 #pragma once
@@ -616,7 +616,7 @@ __device__ void body_pa_rows(const PagedArgs &a) {
 // was summed rescaled, when a weight would pass 2^8 (a branch that the first step
 // takes and few others). Float32 loses nothing by that. In bf16 the largest weight
 // of a row is then rounded like any other, where with the exact maximum it is 1:
-// 0.0019 to 0.0022 against 0.0018 to 0.0020, for 289 instead of 282 us (2048 tokens
+// 0.0019 to 0.0023 against 0.0018 to 0.0020, for 289 instead of 282 us (2048 tokens
 // behind 6144), 44.8 instead of 43.3 (the windowed mixture) and 33.3 instead of
 // 29.6 (heads of 256).
 template <int DT, int HDP>
