@@ -90,8 +90,14 @@ typedef enum tri_op {
   TRI_OP_SWIGLU = 4, TRI_OP_CHAIN = 5, TRI_OP_QK_NORM_ROPE = 6,
   TRI_OP_CHAIN_LAYERS = 7,  /* selection records of tri_decode_chain_layers */
   TRI_OP_SILU = 8, TRI_OP_ADD = 9, TRI_OP_MASKED_FILL = 10, TRI_OP_EMBEDDING = 11,
-  TRI_OP_KV_SLOTS = 12, TRI_OP_KV_WRITE = 13, TRI_OP_PAGED_ATTENTION = 14
+  TRI_OP_KV_SLOTS = 12, TRI_OP_KV_WRITE = 13, TRI_OP_PAGED_ATTENTION = 14,
+  TRI_OP_KV_WRITE_Q8 = 15, TRI_OP_KV_READ_Q8 = 16, TRI_OP_PAGED_ATTENTION_Q8 = 17
 } tri_op;
+
+/* The codes of a KV cache in 8 bits: signed integers (-127 .. 127 as written), or floats
+ * of a sign, 4 exponent and 3 mantissa bits without infinities (E4M3: up to 448, 0x7F and
+ * 0xFF are NaN). */
+typedef enum tri_code { TRI_INT8 = 0, TRI_E4M3 = 1 } tri_code;
 
 enum { TRI_MAX_LAYERS = 1024 };   /* layers per tri_decode_chain_layers call */
 
@@ -311,6 +317,35 @@ typedef struct tri_attention_args {
   void *workspace; int64_t workspace_bytes;
   tri_kv_cache kv;
 } tri_attention_args;
+
+/* What a paged KV cache of 8-bit codes has beside its tri_kv_cache (whose strides
+ * then count bytes): a float32 scale for each block of `block` neighbouring slots of a page and
+ * each head, k_scale and v_scale [n_pages, page / block, nk], strides in elements
+ * from page to page (ps), block to block (bs) and head to head (hs), in any order
+ * that does not overlap. A slot's element is worth code * scale. */
+typedef struct tri_kv_q8 {
+  int32_t code;              /* tri_code                                       */
+  int32_t block;             /* slots that share a scale, divides kv.page      */
+  float *k_scale, *v_scale;
+  int64_t k_ps, k_bs, k_hs;
+  int64_t v_ps, v_bs, v_hs;
+} tri_kv_q8;
+
+/* Arguments of tri_kv_write_quant and tri_kv_read_quant. */
+typedef struct tri_kv_rows_args {
+  int32_t dtype;             /* tri_dtype of k and v                           */
+  int32_t R;                 /* requests, 1..TRI_MAX_REQUESTS                  */
+  int64_t T;                 /* rows of k and v                                */
+  void *k; int64_t k_ts;     /* [T, nk, hd], heads packed                      */
+  void *v; int64_t v_ts;
+  const int32_t *table; int64_t table_rs;   /* [R, cols] block table           */
+  const int32_t *kv_len;     /* [R] tokens in the cache, the rows' included    */
+  const int32_t *q_start;    /* [R + 1] first row of each request              */
+  int32_t cols;
+  int32_t reserved;          /* padding; ignored                               */
+  tri_kv_cache kv;           /* the codes                                      */
+  tri_kv_q8 q8;              /* their scales                                   */
+} tri_kv_rows_args;
 
 /* ---- cache ---------------------------------------------------------------- */
 
@@ -601,6 +636,55 @@ tri_status tri_paged_attention(tri_cache *cache, const tri_attention_args *args,
  * (its workspace fields are ignored, pointers are not read); 0 when it does
  * not split or the arguments are not valid. */
 int64_t tri_paged_attention_workspace(const tri_attention_args *args);
+
+/* The same cache in 8 bits: codes, and a float32 scale for each block of slots and
+ * head. The three calls find a token by its place in its request, as
+ * tri_paged_attention does: rows q_start[r] .. q_start[r + 1] are the last n of request
+ * r's kv_len[r] tokens, row i stands at p = kv_len[r] - n + i in slot p % page of page
+ * table[r][p / page] (kv_len and q_start clamped alike). A step calls tri_kv_slots,
+ * then for each layer tri_kv_write_quant and tri_paged_attention_quant; slots are not
+ * needed. Tokens with p < 0, or whose page is not in the pool, have no place: the write
+ * skips them, a read gives zeros, attention does not see them.
+ *
+ * Write: k, v [T, nk, hd] into codes, blocks of `block` tokens and a head at a time. With
+ * a the largest magnitude among the block's rows of this call, they need the scale
+ *   TRI_INT8: a / 127 in float32;  TRI_E4M3: the least power of two >= a / 448;
+ * at least 2^-100. A block none of whose tokens was there before takes it
+ * (what its slots and its scale held does not count). One that goes on takes the larger of it
+ * and its scale s; if that grows to s', the codes c of its earlier tokens become the nearest
+ * to c * s / s'. The rows' codes are the nearest to x / scale, ties to even
+ * (TRI_INT8 of the exact quotient; TRI_E4M3 of its float32 value, the same thing
+ * where the scale is a power of two). Slots behind kv_len are left as they
+ * were. A NaN or an infinity among a block's rows makes its scale NaN and their codes 0:
+ * the block reads as NaN until it is begun anew. Codes off by rounding: TRI_INT8
+ * half of a scale, and half of one more each time the block's scale grew;
+ * TRI_E4M3 2^-4 of the value, or half of 2^-9 scales near zero. The pages that a
+ * call writes to must be distinct (of two tokens with one slot either may remain, and the
+ * block's scale may fit neither). k and v are only read, and must not overlap the cache
+ * or the scales.
+ *
+ * block 1..page, a divisor of page. nk 1..4096, hd 1..512; cols * page below 2^31. */
+tri_status tri_kv_write_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
+
+/* The tokens' values code * scale, rounded once, into rows of k and v (which the call
+ * writes; they must not overlap the cache). With kv_len = lengths and q_start their running
+ * sum: all tokens. Rows before q_start[0] and from q_start[R] on are left as they were. */
+tri_status tri_kv_read_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
+
+/* tri_paged_attention over codes: args->kv holds their addresses and strides, args->dtype is
+ * the type of q and out. The codes are taken as they are (exact in every product; float32
+ * queries and their weights in three parts of 8 bits), scores times the key's K scale, weights
+ * times its V scale in float32. What tri_paged_attention says of bf16 weights, rows
+ * without keys, unseen keys, outputs, splits and the workspace holds here. Codes and
+ * scales of unseen keys may be anything; a NaN code, or scale, at a key that a row sees makes
+ * NaN of the row (K), or of its element or elements (V). Scales are to be finite or NaN,
+ * and their product with `scale` to stay in float32's range. Heads of a multiple of 16
+ * elements up to 256 with all rows at 16-byte alignment run on the matrix cores. */
+tri_status tri_paged_attention_quant(tri_cache *cache, const tri_attention_args *args,
+                                  const tri_kv_q8 *q8, void *stream);
+
+/* As tri_paged_attention_workspace. */
+int64_t tri_paged_attention_quant_workspace(const tri_attention_args *args);
 
 /* For callers that cannot allocate device memory (code under HIP graph
  * capture, tight serving loops, harnesses that forbid allocation):

@@ -52,7 +52,7 @@ def kv_write(k, v, slots, kc, vc):
     return kc, vc
 
 
-def attention(q, kc, vc, table, kv_len, q_start, scale, window=0):
+def attention(q, kc, vc, table, kv_len, q_start, scale, window=0, more=0):
     """(out, written, spread, slack) for q [T, nq, hd] in float64.
 
     out [T, nq, hd]; written [T]: rows that belong to a request; spread
@@ -62,7 +62,8 @@ def attention(q, kc, vc, table, kv_len, q_start, scale, window=0):
     scaled, is off by at most u (hd + 3) B_j, and its distance to the maximum
     rounds by at most 2 u max|s|, taken to a power (twice, for the weight and
     for the sum it is divided by): 2 (u (hd + 3) max B + 4 u max|s|); the
-    powers, the rescaling and the sums of n weights add (2 n + 200) u."""
+    powers, the rescaling and the sums of n weights add (2 n + 200) u. `more`
+    roundings of a score to be counted beside those."""
     q, kc, vc = (np.asarray(a, dtype=np.float64) for a in (q, kc, vc))
     T, nq, hd = q.shape
     n_pages, page, nk, _ = kc.shape
@@ -98,9 +99,102 @@ def attention(q, kc, vc, table, kv_len, q_start, scale, window=0):
                     out[t, h] = (w[:, None] * Vh).sum(0)
                     spread[t, h] = (w[:, None] * np.abs(Vh)).sum(0)
                     big = (np.abs(Kh) * np.abs(q[t, h])).sum(-1).max() * abs(scale)
-                    slack[t, h] = (2 * (u * (hd + 3) * big + 4 * u * np.abs(s).max())
+                    slack[t, h] = (2 * (u * (hd + 3) * big + (4 + more) * u * np.abs(s).max())
                                    + (2 * len(s) + 200) * u)
     return out, written, spread, slack
+
+
+# ---- the cache in 8 bits ----
+# Codes are held as the numbers they are (float64: whole numbers, or e4m3's values), scales
+# [n_pages, page / block, nk] as float32's; what a slot holds is code * scale.
+INT8, E4M3 = 0, 1
+CODE_MAX = (127.0, 448.0)
+
+
+def _places(r, table, kv_len, q_start, T, page, n_pages):
+    """(row, position, page id or -1) of each row of request r, and its tokens' number."""
+    clamp = lambda x, hi: min(max(int(x), 0), hi)  # noqa: E731
+    a, b = clamp(q_start[r], T), clamp(q_start[r + 1], T)
+    kv = clamp(kv_len[r], np.shape(table)[1] * page)
+    out = []
+    for t in range(a, b):
+        p = kv - (b - t)
+        pid = int(table[r][p // page]) if p >= 0 else -1
+        out.append((t, p, pid if 0 <= pid < n_pages else -1))
+    return out
+
+
+def nearest_code(y, code):
+    """The code nearest to y, ties to the even one: whole numbers, or three bits behind the
+    leading one, in steps of no less than 2^-9."""
+    y = np.asarray(y, dtype=np.float64)
+    if code == INT8:
+        return np.rint(y)
+    with np.errstate(divide="ignore"):
+        e = np.maximum(np.floor(np.log2(np.abs(y))), -6.0)
+    step = 2.0 ** (e - 3)
+    return np.rint(y / step) * step
+
+
+def scale_for(most, code):
+    """The float32 scale of values up to `most`."""
+    if not np.isfinite(most):
+        return np.float32(np.nan)
+    if code == INT8:
+        s = np.float32(most) / np.float32(127)
+    else:
+        m, e = np.frexp(np.float64(most) / 448)      # (the power of two at or above)
+        s = np.ldexp(1.0, int(e) - (m == 0.5)) if most else 0.0
+    return np.float32(max(float(s), 2.0 ** -100))
+
+
+def kv_write_q8(k, v, kc, vc, ks, vs, table, kv_len, q_start, code):
+    """(kc, vc, ks, vs) after the call, block by block and head by head."""
+    kc, vc, ks, vs = (np.array(x) for x in (kc, vc, ks, vs))
+    n_pages, page, nk, _ = kc.shape
+    block = page // ks.shape[1]
+    for r in range(len(table)):
+        blocks = {}
+        for t, p, pid in _places(r, table, kv_len, q_start, len(k), page, n_pages):
+            if pid >= 0:
+                blocks.setdefault((pid, p % page // block), []).append((t, p % page))
+        for (pid, b), rows in blocks.items():
+            held = list(range(b * block, rows[0][1]))
+            slots = [s for _, s in rows]
+            for x, c, sc in ((k, kc, ks), (v, vc, vs)):
+                for h in range(nk):
+                    y = np.asarray(x[[t for t, _ in rows], h], dtype=np.float64)
+                    need, was = scale_for(np.abs(y).max(), code), sc[pid, b, h]
+                    now = was if held and not (need > was or np.isnan(need)) else need
+                    if held and now > was:
+                        z = c[pid, held, h] * np.float64(was) / np.float64(now)
+                        c[pid, held, h] = nearest_code(z, code)
+                    sc[pid, b, h] = now
+                    if np.isnan(now):
+                        c[pid, slots, h] = 0.0
+                        continue
+                    z = y / np.float64(now)
+                    c[pid, slots, h] = nearest_code(z if code == INT8 else np.float32(z), code)
+    return kc, vc, ks, vs
+
+
+def values_q8(c, s):
+    """What the slots of a cache hold."""
+    with np.errstate(all="ignore"):
+        return np.asarray(c, np.float64) * np.repeat(np.float64(s), c.shape[1] // s.shape[1], 1)[..., None]
+
+
+def kv_read_q8(kc, vc, ks, vs, table, kv_len, q_start, T):
+    """(k, v [T, nk, hd], which rows belong to a request)."""
+    k, v = (np.zeros((T,) + kc.shape[2:]) for _ in range(2))
+    written = np.zeros(T, dtype=bool)
+    K, V = values_q8(kc, ks), values_q8(vc, vs)
+    for r in range(len(table)):
+        for t, p, pid in _places(r, table, kv_len, q_start, T, kc.shape[1], len(kc)):
+            written[t] = True
+            if pid >= 0:
+                k[t], v[t] = K[pid, p % kc.shape[1]], V[pid, p % kc.shape[1]]
+    return k, v, written
 
 
 # ---- selections ----------------------------------------------------------------------------
@@ -108,6 +202,9 @@ def attention(q, kc, vc, table, kv_len, q_start, scale, window=0):
 OP_KV_SLOTS, OP_KV_WRITE, OP_PAGED_ATTENTION = 12, 13, 14
 KV_SLOTS, KVW_ANY, KVW_VEC = 80, 82, 83
 PA_ANY, PA_ROWS, PA_TILE, PA_JOIN, PA_PAIR = 90, 91, 92, 93, 94
+OP_KV_WRITE_Q8, OP_KV_READ_Q8, OP_PAGED_ATTENTION_Q8 = 15, 16, 17
+Q8W_ANY, Q8W_VEC, Q8R_ANY, Q8R_VEC = 100, 101, 102, 103
+PA8_ANY, PA8_ROWS, PA8_TILE, PA8_PAIR = 104, 105, 106, 107
 GRID_CAP = 1 << 20
 MAX_SPLITS = 64
 JOIN_WAVE = 8          # splits one wavefront joins

@@ -55,6 +55,7 @@ class _PythonForm:
 
     rmsnorm = residual_rmsnorm = swiglu = silu = add = masked_fill = embedding = _decline
     rope = chain = layers = close = kv_slots = kv_write = paged_attention = _decline
+    kv_write_q8 = kv_read_q8 = paged_attention_q8 = _decline
 
 
 def _native_calls():
@@ -248,6 +249,33 @@ def _kv_cache(k: torch.Tensor, v: torch.Tensor, dtype, dev: int) -> L.KvCache:
     _like(k, "k_cache", k.shape, dtype, dev)
     return L.KvCache(k.data_ptr(), v.data_ptr(), *_kv_view(k, "k_cache", n, page, nk, hd),
                      *_kv_view(v, "v_cache", n, page, nk, hd), n, page, nk, hd)
+
+
+_CODES = {torch.int8: L.INT8, torch.float8_e4m3fn: L.E4M3}
+
+
+def _kv_q8(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+           dev: int) -> Tuple[L.KvCache, L.KvQ8]:
+    """The tri_kv_cache of codes k and v [n_pages, page, nk, hd] and the tri_kv_q8 of
+    their float32 scales [n_pages, blocks of a page, nk]."""
+    if k.dtype not in _CODES:
+        raise TypeError(f"k_cache: expected int8 or float8_e4m3fn, got {k.dtype}")
+    kv = _kv_cache(k, v, k.dtype, dev)
+    n, blocks, nk = _dims(k_scale, "k_scale", 3, dev)
+    if n != kv.n_pages or nk != kv.nk or blocks < 1 or kv.page % blocks:
+        raise ValueError(f"k_scale: expected ({kv.n_pages}, a divisor of {kv.page}, {kv.nk}), "
+                         f"got {tuple(k_scale.shape)}")
+    _like(k_scale, "k_scale", k_scale.shape, torch.float32, dev)
+    _like(v_scale, "v_scale", k_scale.shape, torch.float32, dev)
+
+    def strides(t):   # (dimensions of one report what a packed tensor has)
+        st = t.stride()
+        hs = st[2] if nk > 1 else 1
+        bs = st[1] if blocks > 1 else nk * hs
+        return st[0] if n > 1 else blocks * max(bs, nk * hs), bs, hs
+
+    return kv, L.KvQ8(_CODES[k.dtype], kv.page // blocks, k_scale.data_ptr(), v_scale.data_ptr(),
+                      *strides(k_scale), *strides(v_scale))
 
 
 def _int32(t: torch.Tensor, name: str, n: int, dev: int) -> int:
@@ -762,6 +790,95 @@ class SpecCache:
             a._workspace = self._made(None, q, stream, need, torch.uint8)
             a.workspace, a.workspace_bytes = a._workspace.data_ptr(), need
         self._call("tri_paged_attention", _dll.tri_paged_attention, C.byref(a),
+                   _stream_ptr(stream, dev))
+        return o
+
+    def _rows_q8(self, k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_len,
+                 q_start) -> L.KvRowsArgs:
+        dev = self._dev
+        T, nk, hd = _dims(k, "k", 3, dev)
+        _like(v, "v", k.shape, k.dtype, dev)
+        kv, q8 = _kv_q8(k_cache, v_cache, k_scale, v_scale, dev)
+        if (kv.nk, kv.hd) != (nk, hd):
+            raise ValueError(f"k_cache: expected heads ({nk}, {hd}), got ({kv.nk}, {kv.hd})")
+        R, cols, rs = _table(block_table, "block_table", dev)
+        return L.KvRowsArgs(dtype_code(k.dtype), R, T, k.data_ptr(), _tokens(k, "k", nk, hd),
+                            v.data_ptr(), _tokens(v, "v", nk, hd), block_table.data_ptr(), rs,
+                            _int32(kv_len, "kv_len", R, dev),
+                            _int32(q_start, "q_start", R + 1, dev), cols, 0, kv, q8)
+
+    def kv_write_q8(self, k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, q_start,
+                    stream=None):
+        """Quantise k and v [T, nk, hd] into a paged cache of 8-bit codes [n_pages, page, nk, hd]
+        (int8 or float8_e4m3fn) with a float32 scale for each block of tokens and head, k_scale
+        and v_scale [n_pages, blocks of a page, nk] (tri_kv_write_quant): rows
+        q_start[r]:q_start[r + 1] are the last of request r's kv_len[r] tokens, as in
+        paged_attention_q8. A block that a call begins takes the scale that its tokens need; one
+        that goes on keeps its own, or takes a larger one and has its codes rounded again."""
+        if self._rec is None:
+            r = self._fast.kv_write_q8(self, k, v, k_cache, v_cache, k_scale, v_scale, block_table,
+                                       kv_len, q_start, stream)
+            if r is not None:
+                return r
+        a = self._rows_q8(k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, q_start)
+        self._call("tri_kv_write_quant", _dll.tri_kv_write_quant, C.byref(a),
+                   _stream_ptr(stream, self._dev))
+        return k_cache, v_cache, k_scale, v_scale
+
+    def kv_read_q8(self, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, q_start, T: int,
+                   dtype=torch.bfloat16, k=None, v=None, stream=None):
+        """The values of an 8-bit cache as rows k, v [T, nk, hd] (tri_kv_read_quant): rows
+        q_start[r]:q_start[r + 1] are the last of request r's kv_len[r] tokens (all of them where
+        q_start is the lengths' running sum); zeros for a token whose page is not in the pool.
+        Rows of no request keep what k and v held (those made here are not initialised)."""
+        if self._rec is None:
+            r = self._fast.kv_read_q8(self, k_cache, v_cache, k_scale, v_scale, block_table, kv_len,
+                                      q_start, T, dtype, k, v, stream)
+            if r is not None:
+                return r
+        dev = self._dev
+        _, _, nk, hd = _dims(k_cache, "k_cache", 4, dev)
+        shape = (_whole(int(T), "T", 64), nk, hd)
+        if shape[0] < 0:
+            raise ValueError(f"T: {T} is negative")
+        dtype_code(dtype)
+        k = self._made(k, k_cache, stream, shape, dtype)
+        v = self._made(v, k_cache, stream, shape, dtype)
+        _like(k, "k", shape, dtype, dev)
+        a = self._rows_q8(k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, q_start)
+        self._call("tri_kv_read_quant", _dll.tri_kv_read_quant, C.byref(a), _stream_ptr(stream, dev))
+        return k, v
+
+    def paged_attention_q8(self, q, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, q_start,
+                           scale: Optional[float] = None, window: int = 0, max_kv: int = 0,
+                           out=None, stream=None) -> torch.Tensor:
+        """paged_attention over the 8-bit cache of kv_write_q8 (tri_paged_attention_quant): q and
+        out [T, nq, hd] in bfloat16 or float32, arguments and rows as there."""
+        if self._rec is None:
+            r = self._fast.paged_attention_q8(self, q, k_cache, v_cache, k_scale, v_scale,
+                                              block_table, kv_len, q_start, scale, window, max_kv,
+                                              out, stream)
+            if r is not None:
+                return r
+        dev = self._dev
+        T, nq, hd = _dims(q, "q", 3, dev)
+        o = self._made(out, q, stream, (T, nq, hd))
+        _like(o, "out", q.shape, q.dtype, dev)
+        R, cols, rs = _table(block_table, "block_table", dev)
+        kv, q8 = _kv_q8(k_cache, v_cache, k_scale, v_scale, dev)
+        if kv.hd != hd:
+            raise ValueError(f"k_cache: expected heads of {hd}, got {kv.hd}")
+        a = L.AttentionArgs(dtype_code(q.dtype), _whole(nq, "q"), T, R, cols, q.data_ptr(),
+                            _tokens(q, "q", nq, hd), o.data_ptr(), _tokens(o, "out", nq, hd),
+                            block_table.data_ptr(), rs, _int32(kv_len, "kv_len", R, dev),
+                            _int32(q_start, "q_start", R + 1, dev),
+                            hd ** -0.5 if scale is None else scale, _whole(window, "window"),
+                            _whole(max_kv, "max_kv", 64), None, 0, kv)
+        need = _dll.tri_paged_attention_quant_workspace(C.byref(a))
+        if need:
+            a._workspace = self._made(None, q, stream, need, torch.uint8)
+            a.workspace, a.workspace_bytes = a._workspace.data_ptr(), need
+        self._call("tri_paged_attention_quant", _dll.tri_paged_attention_quant, C.byref(a), C.byref(q8),
                    _stream_ptr(stream, dev))
         return o
 

@@ -20,6 +20,8 @@ OP_RMSNORM, OP_RES_RMSNORM, OP_ROPE_QK, OP_SWIGLU, OP_CHAIN, OP_QK_NORM_ROPE = 1
 OP_CHAIN_LAYERS = 7
 OP_SILU, OP_ADD, OP_MASKED_FILL, OP_EMBEDDING = 8, 9, 10, 11
 OP_KV_SLOTS, OP_KV_WRITE, OP_PAGED_ATTENTION = 12, 13, 14
+OP_KV_WRITE_Q8, OP_KV_READ_Q8, OP_PAGED_ATTENTION_Q8 = 15, 16, 17
+INT8, E4M3 = 0, 1
 MAX_REQUESTS, MAX_PAGE, MAX_KV_SPLITS = 4096, 65536, 64
 MAX_LAYERS = 1024
 AUTO_INSTALL = 1
@@ -132,8 +134,26 @@ class AttentionArgs(C.Structure):
                 ("kv", KvCache)]
 
 
+class KvQ8(C.Structure):
+    _fields_ = [("code", C.c_int32), ("block", C.c_int32),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_ps", C.c_int64), ("k_bs", C.c_int64), ("k_hs", C.c_int64),
+                ("v_ps", C.c_int64), ("v_bs", C.c_int64), ("v_hs", C.c_int64)]
+
+
+class KvRowsArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("R", C.c_int32), ("T", C.c_int64),
+                ("k", C.c_void_p), ("k_ts", C.c_int64),
+                ("v", C.c_void_p), ("v_ts", C.c_int64),
+                ("table", C.c_void_p), ("table_rs", C.c_int64),
+                ("kv_len", C.c_void_p), ("q_start", C.c_void_p),
+                ("cols", C.c_int32), ("reserved", C.c_int32),
+                ("kv", KvCache), ("q8", KvQ8)]
+
+
 assert C.sizeof(KvCache) == 80 and C.sizeof(KvSlotsArgs) == 112
 assert C.sizeof(AttentionArgs) == 200
+assert C.sizeof(KvQ8) == 72 and C.sizeof(KvRowsArgs) == 240
 assert C.sizeof(Selection) == 120 and C.sizeof(ChainArgs) == 240 and C.sizeof(RopeExt) == 48
 assert C.sizeof(VersionInfo) == 144 and C.sizeof(ResidentInfo) == 16
 
@@ -165,6 +185,10 @@ SIGNATURES = {
                                _P]),
     "tri_paged_attention": (C.c_int, [_P, C.POINTER(AttentionArgs), _P]),
     "tri_paged_attention_workspace": (_I64, [C.POINTER(AttentionArgs)]),
+    "tri_kv_write_quant": (C.c_int, [_P, C.POINTER(KvRowsArgs), _P]),
+    "tri_kv_read_quant": (C.c_int, [_P, C.POINTER(KvRowsArgs), _P]),
+    "tri_paged_attention_quant": (C.c_int, [_P, C.POINTER(AttentionArgs), C.POINTER(KvQ8), _P]),
+    "tri_paged_attention_quant_workspace": (_I64, [C.POINTER(AttentionArgs)]),
     "tri_decode_chain": (C.c_int, [_P, C.POINTER(ChainArgs), _P]),
     "tri_decode_chain_layers": (C.c_int, [_P, C.POINTER(ChainArgs), _U32, _P]),
     "tri_graph_build_layers": (C.c_int, [_P, C.POINTER(ChainArgs), _U32, C.POINTER(C.c_void_p)]),

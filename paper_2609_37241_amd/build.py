@@ -43,7 +43,8 @@ DEVICE_FLAGS = ["-O3", "-std=c++17", "-ffp-contract=off",
                 "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 HIP_FLAGS = [f"--offload-arch={ARCH}", *DEVICE_FLAGS, "-fPIC", "-I", INCLUDE, "-I", CSRC]
 HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-I", INCLUDE, "-I", CSRC]
-HOST_SOURCES = ["api.cpp", "paged.cpp", "cache.cpp", "policy.cpp", "jit.cpp", "tune.cpp", "resident.cpp"]
+HOST_SOURCES = ["api.cpp", "paged.cpp", "paged_q8.cpp", "cache.cpp", "policy.cpp", "jit.cpp", "tune.cpp",
+                "resident.cpp"]
 JIT_PRELUDE = os.path.join(BUILD, "jit_prelude.cpp")
 HIP_BACKEND = "backend_hip.cpp"
 

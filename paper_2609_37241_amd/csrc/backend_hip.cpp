@@ -26,6 +26,7 @@ const void *empty_kernel();
 const void *elt_kernel(int32_t variant, uint32_t dtype, int32_t op);
 const void *emb_kernel(int32_t variant, uint32_t dtype);
 const void *paged_kernel(int32_t variant, uint32_t dtype, int32_t sub);
+const void *paged_q8_kernel(int32_t variant, uint32_t dtype, int32_t sub);
 const void *rn_kernel_resident(int32_t variant, uint32_t dtype, int32_t res);
 const void *rope_kernel_resident(int32_t variant, uint32_t dtype);
 const void *sw_kernel_resident(int32_t variant, uint32_t dtype);
@@ -65,6 +66,8 @@ int be_resolve(int32_t kvariant, uint32_t dtype, int32_t ksub, void **fn) {
     sym = emb_kernel(kvariant, dtype);
   else if (kvariant >= KV_SLOTS && kvariant <= PA_PAIR)
     sym = paged_kernel(kvariant, dtype, ksub);
+  else if (kvariant >= Q8W_ANY && kvariant <= PA8_PAIR)
+    sym = paged_q8_kernel(kvariant, dtype, ksub);
   else if (kvariant == EMPTY)
     sym = empty_kernel();
   if (!sym) return TRI_E_RUNTIME;

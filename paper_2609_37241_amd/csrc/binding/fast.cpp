@@ -22,6 +22,7 @@
 #include <c10/core/StreamGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
@@ -471,12 +472,11 @@ bool block_table(PyObject *o, int dev, int32_t **p, int64_t *R, int64_t *cols, i
   return *rs >= 0;
 }
 
-// The cache of k and v [n_pages, page, nk, hd] of `like`'s type; a dimension
+// The cache of k and v [n_pages, page, nk, hd] of type `st`; a dimension
 // of one reports what a packed cache has.
-bool kv_cache(PyObject *ko, PyObject *vo, int dev, const at::Tensor &like, tri_kv_cache *c) {
+bool kv_cache(PyObject *ko, PyObject *vo, int dev, at::ScalarType st, tri_kv_cache *c) {
   const at::Tensor *k = plain(ko, dev), *v = plain(vo, dev);
-  if (!k || !v || k->dim() != 4 || k->scalar_type() != like.scalar_type() || !same(*v, *k))
-    return false;
+  if (!k || !v || k->dim() != 4 || k->scalar_type() != st || !same(*v, *k)) return false;
   const int64_t n = k->size(0), page = k->size(1), nk = k->size(2), hd = k->size(3);
   if (n > INT32_MAX || page > INT32_MAX || nk > INT32_MAX || hd > INT32_MAX) return false;
   const auto view = [&](const at::Tensor &t, int64_t *ps, int64_t *ss, int64_t *hs) {
@@ -588,7 +588,7 @@ PyObject *kv_write(Handle *h, PyObject *owner, PyObject *const *a) {
   void *s;
   if (!k || !v || k->dim() != 3 || dtype_of(*k) < 0 || !same(*v, *k) ||
       !integers(a[2], h->dev, at::kLong, k->size(0), false, &slots) ||
-      !kv_cache(a[3], a[4], h->dev, *k, &c) || c.nk != k->size(1) || c.hd != k->size(2) ||
+      !kv_cache(a[3], a[4], h->dev, k->scalar_type(), &c) || c.nk != k->size(1) || c.hd != k->size(2) ||
       !stream_of(h, a[5], &s))
     Py_RETURN_NONE;
   const int64_t T = k->size(0), ks = tokens(*k), vs = tokens(*v);
@@ -601,16 +601,120 @@ PyObject *kv_write(Handle *h, PyObject *owner, PyObject *const *a) {
   return PyTuple_Pack(2, a[3], a[4]);
 }
 
+// The cache of 8-bit codes and its scales at a[0 .. 3]: k_cache, v_cache, k_scale, v_scale.
+bool kv_q8(PyObject *const *a, int dev, tri_kv_cache *c, tri_kv_q8 *q) {
+  const at::Tensor *k = plain(a[0], dev), *ks = plain(a[2], dev), *vs = plain(a[3], dev);
+  if (!k || !ks || !vs) return false;
+  const at::ScalarType st = k->scalar_type();
+  if ((st != at::kChar && st != at::kFloat8_e4m3fn) || !kv_cache(a[0], a[1], dev, st, c)) return false;
+  if (ks->dim() != 3 || ks->scalar_type() != at::kFloat || !same(*vs, *ks)) return false;
+  const int64_t n = ks->size(0), blocks = ks->size(1), nk = ks->size(2);
+  if (n != c->n_pages || nk != c->nk || blocks < 1 || c->page % blocks) return false;
+  q->code = st == at::kChar ? TRI_INT8 : TRI_E4M3;
+  q->block = int32_t(c->page / blocks);
+  const auto view = [&](const at::Tensor &t, float **p, int64_t *ps, int64_t *bs, int64_t *hs) {
+    *p = static_cast<float *>(t.data_ptr());
+    *hs = nk > 1 ? t.stride(2) : 1;
+    *bs = blocks > 1 ? t.stride(1) : nk * *hs;
+    *ps = n > 1 ? t.stride(0) : blocks * std::max(*bs, nk * *hs);
+  };
+  view(*ks, &q->k_scale, &q->k_ps, &q->k_bs, &q->k_hs);
+  view(*vs, &q->v_scale, &q->v_ps, &q->v_bs, &q->v_hs);
+  return true;
+}
+
+// Rows k, v of a call over an 8-bit cache whose codes and scales, table, lengths and starts are
+// a[0 .. 6].
+bool rows_q8(const at::Tensor &k, const at::Tensor &v, PyObject *const *a, int dev,
+             tri_kv_rows_args *x) {
+  int64_t R, cols;
+  int32_t *tp, *kv, *starts;
+  const at::Tensor *table;
+  if (!block_table(a[4], dev, &tp, &R, &cols, &x->table_rs, &table) ||
+      !integers(a[5], dev, at::kInt, R, false, &kv) ||
+      !integers(a[6], dev, at::kInt, R + 1, false, &starts) || x->kv.nk != k.size(1) ||
+      x->kv.hd != k.size(2))
+    return false;
+  x->dtype = dtype_of(k);
+  x->R = int32_t(R);
+  x->T = k.size(0);
+  x->k = k.data_ptr();
+  x->k_ts = tokens(k);
+  x->v = v.data_ptr();
+  x->v_ts = tokens(v);
+  x->table = tp;
+  x->kv_len = kv;
+  x->q_start = starts;
+  x->cols = int32_t(cols);
+  return x->k_ts >= 0 && x->v_ts >= 0;
+}
+
+// kv_write_q8(owner, k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, q_start,
+// stream)
+PyObject *kv_write_q8(Handle *h, PyObject *owner, PyObject *const *a) {
+  const at::Tensor *k = plain(a[0], h->dev), *v = plain(a[1], h->dev);
+  tri_kv_rows_args x{};
+  void *s;
+  if (!k || !v || k->dim() != 3 || dtype_of(*k) < 0 || !same(*v, *k) ||
+      !kv_q8(a + 2, h->dev, &x.kv, &x.q8) || !rows_q8(*k, *v, a + 2, h->dev, &x) ||
+      !stream_of(h, a[9], &s))
+    Py_RETURN_NONE;
+  if (!issue(owner, "tri_kv_write_quant", [&] { return tri_kv_write_quant(h->cache, &x, s); }))
+    return nullptr;
+  return PyTuple_Pack(4, a[2], a[3], a[4], a[5]);
+}
+
+// kv_read_q8(owner, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, q_start, T, dtype, k, v,
+// stream)
+PyObject *kv_read_q8(Handle *h, PyObject *owner, PyObject *const *a) {
+  tri_kv_rows_args x{};
+  int64_t T;
+  void *s;
+  if (!kv_q8(a, h->dev, &x.kv, &x.q8) || !integer(a[7], &T) || T < 0 || !THPDtype_Check(a[8]) ||
+      !stream_of(h, a[11], &s))
+    Py_RETURN_NONE;
+  const at::ScalarType st = reinterpret_cast<THPDtype *>(a[8])->scalar_type;
+  if (st != at::kFloat && st != at::kBFloat16) Py_RETURN_NONE;
+  Out o[2];
+  for (int i = 0; i < 2; ++i) {
+    if (a[9 + i] == Py_None) continue;
+    const at::Tensor *t = plain(a[9 + i], h->dev);
+    if (!t || t->dim() != 3 || t->scalar_type() != st || t->size(0) != T || t->size(1) != x.kv.nk ||
+        t->size(2) != x.kv.hd)
+      Py_RETURN_NONE;
+    o[i].t = *t;
+    o[i].given = a[9 + i];
+  }
+  {
+    MakingOn on(h, a[11], s);
+    NoGil g;
+    for (Out &y : o)
+      if (!y.given)
+        y.t = at::empty({T, x.kv.nk, x.kv.hd},
+                        at::TensorOptions().dtype(st).device(at::kCUDA, c10::DeviceIndex(h->dev)));
+  }
+  if (!rows_q8(o[0].t, o[1].t, a, h->dev, &x)) Py_RETURN_NONE;
+  if (!issue(owner, "tri_kv_read_quant", [&] { return tri_kv_read_quant(h->cache, &x, s); }))
+    return nullptr;
+  return pair(o[0].result(), o[1].result());
+}
+
 // paged_attention(owner, q, k_cache, v_cache, block_table, kv_len, q_start,
-// scale, window, max_kv, out, stream)
-PyObject *paged_attention(Handle *h, PyObject *owner, PyObject *const *a) {
-  const at::Tensor *q = plain(a[0], h->dev), *table;
+// scale, window, max_kv, out, stream), and paged_attention_q8 with k_scale and v_scale after
+// v_cache.
+template <bool Q8>
+PyObject *paged_attention(Handle *h, PyObject *owner, PyObject *const *args) {
+  const at::Tensor *q = plain(args[0], h->dev), *table;
+  PyObject *const *a = args + (Q8 ? 2 : 0);   // (block_table and what follows at a[3])
   tri_attention_args x{};
+  tri_kv_q8 q8{};
   int64_t R, cols, window;
   int32_t *tp, *kv, *starts;
   void *s;
   if (!q || q->dim() != 3 || dtype_of(*q) < 0 || q->size(1) > INT32_MAX ||
-      !kv_cache(a[1], a[2], h->dev, *q, &x.kv) || x.kv.hd != q->size(2) ||
+      !(Q8 ? kv_q8(args + 1, h->dev, &x.kv, &q8)
+           : kv_cache(args[1], args[2], h->dev, q->scalar_type(), &x.kv)) ||
+      x.kv.hd != q->size(2) ||
       !block_table(a[3], h->dev, &tp, &R, &cols, &x.table_rs, &table) ||
       !integers(a[4], h->dev, at::kInt, R, false, &kv) ||
       !integers(a[5], h->dev, at::kInt, R + 1, false, &starts) ||
@@ -639,15 +743,18 @@ PyObject *paged_attention(Handle *h, PyObject *owner, PyObject *const *a) {
   x.q_start = starts;
   x.window = int32_t(window);
   at::Tensor work;
-  if (const int64_t need = tri_paged_attention_workspace(&x)) {
+  if (const int64_t need = Q8 ? tri_paged_attention_quant_workspace(&x)
+                              : tri_paged_attention_workspace(&x)) {
     MakingOn on(h, a[10], s);
     NoGil g;
     work = at::empty({need}, q->options().dtype(at::kByte));
     x.workspace = work.data_ptr();
     x.workspace_bytes = need;
   }
-  if (!issue(owner, "tri_paged_attention",
-             [&] { return tri_paged_attention(h->cache, &x, s); }))
+  if (!issue(owner, Q8 ? "tri_paged_attention_quant" : "tri_paged_attention", [&] {
+        return Q8 ? tri_paged_attention_quant(h->cache, &x, &q8, s)
+                  : tri_paged_attention(h->cache, &x, s);
+      }))
     return nullptr;
   return y.result();
 }
@@ -704,7 +811,10 @@ PyMethodDef g_methods[] = {
     {"rope", fn<rope, 10>(), METH_FASTCALL, nullptr},
     {"kv_slots", fn<kv_slots, 13>(), METH_FASTCALL, nullptr},
     {"kv_write", fn<kv_write, 6>(), METH_FASTCALL, nullptr},
-    {"paged_attention", fn<paged_attention, 11>(), METH_FASTCALL, nullptr},
+    {"paged_attention", fn<paged_attention<false>, 11>(), METH_FASTCALL, nullptr},
+    {"kv_write_q8", fn<kv_write_q8, 10>(), METH_FASTCALL, nullptr},
+    {"kv_read_q8", fn<kv_read_q8, 12>(), METH_FASTCALL, nullptr},
+    {"paged_attention_q8", fn<paged_attention<true>, 13>(), METH_FASTCALL, nullptr},
     {"chain", fn<chain, 2>(), METH_FASTCALL, nullptr},
     {"layers", fn<layers, 2>(), METH_FASTCALL, nullptr},
     {"close", close, METH_NOARGS, nullptr},

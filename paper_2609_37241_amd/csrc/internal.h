@@ -25,6 +25,8 @@ enum Variant : int32_t {
   KV_SLOTS = 80, KVW_ANY = 82, KVW_VEC = 83,
   PA_ANY = 90, PA_ROWS = 91, PA_TILE = 92, PA_JOIN = 93, PA_PAIR = 94,
   EMPTY = 99,
+  Q8W_ANY = 100, Q8W_VEC = 101, Q8R_ANY = 102, Q8R_VEC = 103,
+  PA8_ANY = 104, PA8_ROWS = 105, PA8_TILE = 106, PA8_PAIR = 107,
 };
 
 // Token buckets up to this one are "decode sized": RoPE head slices, one
@@ -65,6 +67,7 @@ constexpr int64_t kKeysMax = kPosLimit - 4096;
 // k3: rotary dim | variant bits << 16 | scaling << 24 | original_max_pos << 32
 // k4: factor bits | low_freq_factor bits << 32;  k5: high_freq_factor bits
 // Attention: k3 = form << 16 | split << 24 (AttnForm; 1: keys split and joined).
+// 8-bit cache: k3 also has code << 32 (tri_code).
 // Fields an op does not use are zero.
 struct Key {
   uint64_t k0, k1, k2, k3, k4, k5;
@@ -86,6 +89,7 @@ inline uint32_t key_nk(const Key &k) { return uint32_t((k.k2 >> 32) & 0xFFFF); }
 inline uint32_t key_rd(const Key &k) { return uint32_t(k.k3 & 0xFFFF); }
 inline uint32_t key_rope_bits(const Key &k) { return uint32_t((k.k3 >> 16) & 0xFF); }
 inline uint32_t key_scaling(const Key &k) { return uint32_t((k.k3 >> 24) & 0xFF); }
+inline uint32_t key_code(const Key &k) { return uint32_t(k.k3 >> 32); }   // tri_code
 inline uint32_t key_orig_max(const Key &k) { return uint32_t(k.k3 >> 32); }
 inline void key_words(const Key &k, uint64_t *w) {
   w[0] = k.k0;
@@ -166,7 +170,8 @@ Role elt_role(uint32_t dtype, int64_t W, unsigned flags, uint32_t bucket, int64_
 Role emb_role(uint32_t dtype, int64_t H, unsigned flags, int64_t T);
 
 // ---- the paged KV cache ----
-inline bool is_paged_op(uint32_t op) { return op >= TRI_OP_KV_SLOTS && op <= TRI_OP_PAGED_ATTENTION; }
+inline bool is_paged_op(uint32_t op) { return op >= TRI_OP_KV_SLOTS && op <= TRI_OP_PAGED_ATTENTION_Q8; }
+inline bool is_q8_op(uint32_t op) { return op >= TRI_OP_KV_WRITE_Q8 && op <= TRI_OP_PAGED_ATTENTION_Q8; }
 // How attention computes: any alignment and head size, a wavefront per row; or
 // on the matrix cores, tiles of few rows whose keys the wavefronts share out,
 // or of many rows that the wavefronts share out (in pairs: two groups of them
@@ -201,6 +206,15 @@ inline uint64_t attn_workspace(int64_t T, int32_t nq, int32_t hd, int32_t splits
 }
 uint32_t kv_slots_grid(int64_t T, int32_t R);
 uint32_t kv_write_grid(int64_t T, uint32_t row_items);
+// The 8-bit cache: the matrix forms take heads of whole 16-byte vectors of codes.
+inline bool attn_q8_matrix(bool aligned, int32_t hd) {
+  return aligned && hd % 16 == 0 && hd <= kAttnMatrixHd;
+}
+// As attn_plan, `aligned` with the codes.
+AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
+                      bool aligned, int64_t kv_max, uint64_t workspace);
+uint32_t q8_write_grid(int64_t T, int32_t R, int32_t nk, int32_t block);
+uint32_t q8_read_grid(int64_t T);
 // n / d by multiplication (kernargs.h).
 FastDiv fast_div_of(uint32_t d);
 
@@ -354,7 +368,7 @@ struct Version {
   uint64_t hits;
 };
 
-constexpr int kOps = 15;   // op ids 1..14
+constexpr int kOps = 18;   // op ids 1..17
 
 // Memo of first matches: a direct-mapped table of keys and the version
 // Algorithm 1's scan selected for them. First match depends only on the key

@@ -210,6 +210,37 @@ struct PagedArgs {
   FastDiv g_div;          // by g
 };
 
+// Where the scales of an 8-bit cache lie: elements from page to page, block to
+// block and head to head.
+struct ScaleView {
+  float *p;
+  int64_t ps, bs, hs;
+};
+
+// Rows of K and V into an 8-bit cache (Q8W_*), or out of it (Q8R_*).
+struct Q8RowsArgs {
+  void *k, *v;
+  PagedView ck, cv;
+  ScaleView sk, sv;
+  const int32_t *table, *kv_len, *q_start;
+  int64_t k_ts, v_ts, table_rs;
+  int32_t T, R, cols, n_pages;
+  int32_t page, nk, hd, block;
+  FastDiv div;            // by page
+  FastDiv block_div;      // by block
+  FastDiv nk_div;         // by nk
+};
+
+// Attention over an 8-bit cache (PA8_*). The maxima that its parts leave are already in
+// powers of two, so PA_JOIN takes `a` with a scale of 1.
+struct PagedQ8Args {
+  PagedArgs a;
+  ScaleView ks, vs;
+  float scale;            // |scale| log2 e
+  int32_t block;
+  FastDiv block_div;      // by block
+};
+
 // An argument block held in device memory for launches without kernel
 // arguments: the kernel's argument struct (zero beyond its size), the
 // launch's workgroup count and a tag that marks the slot as written
@@ -258,6 +289,10 @@ static_assert(sizeof(KvWriteArgs) == 152 && __builtin_offsetof(KvWriteArgs, row_
               "KvWriteArgs layout");
 static_assert(sizeof(PagedArgs) == 216 && __builtin_offsetof(PagedArgs, div) == 200,
               "PagedArgs layout");
+static_assert(sizeof(Q8RowsArgs) == 248 && __builtin_offsetof(Q8RowsArgs, T) == 192,
+              "Q8RowsArgs layout");
+static_assert(sizeof(PagedQ8Args) == 296 && __builtin_offsetof(PagedQ8Args, scale) == 280,
+              "PagedQ8Args layout");
 static_assert(sizeof(ResidentBlock) == 320 && __builtin_offsetof(ResidentBlock, grid) == 288 &&
                   __builtin_offsetof(ResidentBlock, tag) == 292,
               "ResidentBlock layout");

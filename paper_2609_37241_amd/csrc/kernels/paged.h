@@ -41,11 +41,13 @@ __device__ inline int32_t clamp_i32(int32_t v, int32_t lo, int32_t hi) {
   return v < lo ? lo : v > hi ? hi : v;
 }
 
-__device__ inline Request clamped(const PagedArgs &a, int32_t q0, int32_t q1, int32_t kv) {
+template <class A>
+__device__ inline Request clamped(const A &a, int32_t q0, int32_t q1, int32_t kv) {
   return {clamp_i32(q0, 0, a.T), clamp_i32(q1, 0, a.T), clamp_i32(kv, 0, a.cols * a.page)};
 }
 
-__device__ inline Request request_of(const PagedArgs &a, int32_t r) {
+template <class A>
+__device__ inline Request request_of(const A &a, int32_t r) {
   return clamped(a, a.q_start[r], a.q_start[r + 1], a.kv_len[r]);
 }
 

@@ -314,6 +314,22 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
   return p;
 }
 
+// ---- the paged KV cache in 8 bits ----
+// A wavefront for each block of tokens that a request's rows can touch (numbered as
+// q8_write's kernel says, T / block + 2 R of them), head, and K or V.
+uint32_t q8_write_grid(int64_t T, int32_t R, int32_t nk, int32_t block) {
+  return clamp_grid(cdiv((T / block + 2 * int64_t(R)) * nk * 2, 4));
+}
+
+// A wavefront a row.
+uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4)); }
+
+AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
+                      bool aligned, int64_t kv_max, uint64_t workspace) {
+  (void)aligned;
+  return attn_plan(dtype, T, R, nq, nk, hd, false, kv_max, workspace);
+}
+
 // Workgroups of a role variant for T tokens (I is the row width: the norm
 // row H, the SwiGLU width, the row width of an element-wise op, or the
 // embedding row width).
@@ -370,11 +386,15 @@ static bool paged_key_valid(const Key &k) {
   if (op == TRI_OP_KV_SLOTS)
     return key_dtype(k) == 0 && key_flags(k) == 0 && k.k2 == 0 && k.k3 == 0;
   if (hd < 1 || int32_t(hd) > kAttnHdMax || nk < 1 || int32_t(nk) > kHeadsMax) return false;
-  if (op == TRI_OP_KV_WRITE) return nq == 0 && k.k3 == 0;
+  const bool q8 = is_q8_op(op);
+  if (q8 && key_code(k) > TRI_E4M3) return false;
+  const uint64_t k3 = q8 ? k.k3 & 0xFFFFFFFFu : k.k3;
+  if (op == TRI_OP_KV_WRITE || op == TRI_OP_KV_WRITE_Q8 || op == TRI_OP_KV_READ_Q8)
+    return nq == 0 && k3 == 0;
   const uint32_t form = key_attn_form(k);
   if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
-  if (k.k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
-  const bool matrix = attn_matrix(key_dtype(k), key_flags(k) & kAlign, int32_t(hd));
+  if (k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
+  const bool matrix = !q8 && attn_matrix(key_dtype(k), key_flags(k) & kAlign, int32_t(hd));
   if (form == kAttnPair && (key_dtype(k) == TRI_F32 || hd > 128)) return false;
   return matrix ? form >= kAttnRows && form <= kAttnPair : form == kAttnAny;
 }
@@ -492,6 +512,25 @@ Plan plan_for_key(const Key &k) {
                                   : key_attn_form(k) == kAttnPair ? PA_PAIR
                                                                   : PA_ANY;
       if (p.variant != PA_ANY) p.ksub[0] = attn_hdp(int32_t(key_hd(k)));
+      p.n_launches = 1;
+      if (key_attn_split(k)) p.kvariant[p.n_launches++] = PA_JOIN;
+      return p;
+    case TRI_OP_KV_WRITE_Q8:
+    case TRI_OP_KV_READ_Q8: {
+      const bool vec = (fl & kAlign) && key_hd(k) % vec_elems(dt) == 0;
+      p.variant = p.kvariant[0] = key_op(k) == TRI_OP_KV_WRITE_Q8 ? (vec ? Q8W_VEC : Q8W_ANY)
+                                                                  : (vec ? Q8R_VEC : Q8R_ANY);
+      p.ksub[0] = int32_t(key_code(k));
+      p.n_launches = 1;
+      return p;
+    }
+    case TRI_OP_PAGED_ATTENTION_Q8:
+      p.variant = p.kvariant[0] = key_attn_form(k) == kAttnRows   ? PA8_ROWS
+                                  : key_attn_form(k) == kAttnTile ? PA8_TILE
+                                  : key_attn_form(k) == kAttnPair ? PA8_PAIR
+                                                                  : PA8_ANY;
+      p.ksub[0] = int32_t(key_code(k));
+      if (p.variant != PA8_ANY) p.ksub[0] |= attn_hdp(int32_t(key_hd(k)));
       p.n_launches = 1;
       if (key_attn_split(k)) p.kvariant[p.n_launches++] = PA_JOIN;
       return p;
