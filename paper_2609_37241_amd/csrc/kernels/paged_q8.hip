@@ -320,9 +320,18 @@ const void *rows_kernel(int32_t variant) {
 }
 }  // namespace
 
-// sub: the code (tri_code) in bit 0, for the matrix forms the head size held above it.
+const void *attn_q8_rows(uint32_t dtype, int32_t code, int32_t hdp);
+const void *attn_q8_tile_bf16(bool pair, int32_t code, int32_t hdp);
+const void *attn_q8_tile_f32(int32_t code, int32_t hdp);
+
+// sub: the code (tri_code) in bit 0; for the matrix forms the head size held from bit 6 on.
 const void *paged_q8_kernel(int32_t variant, uint32_t dtype, int32_t sub) {
   const bool e4m3 = (sub & 1) == TRI_E4M3;
+  const int32_t code = sub & 1, hdp = sub & ~63;
+  if (variant == PA8_ROWS) return attn_q8_rows(dtype, code, hdp);
+  if (variant == PA8_TILE && dtype == TRI_F32) return attn_q8_tile_f32(code, hdp);
+  if (variant == PA8_TILE || variant == PA8_PAIR)
+    return attn_q8_tile_bf16(variant == PA8_PAIR, code, hdp);
   if (dtype == TRI_F32)
     return e4m3 ? rows_kernel<kF32, kE4M3>(variant) : rows_kernel<kF32, kInt8>(variant);
   return e4m3 ? rows_kernel<kBF16, kE4M3>(variant) : rows_kernel<kBF16, kInt8>(variant);

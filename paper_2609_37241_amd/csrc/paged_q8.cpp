@@ -87,7 +87,8 @@ tri_status tri_paged_attention_quant(tri_cache *c, const tri_attention_args *p, 
   if (!plan.grid[0]) return finish_early(c, op, TRI_E_UNSUPPORTED);
   Key k = make_key(op, uint32_t(a.dtype), a.T, attn_aligned(a, 1) ? kAlign : 0u, 0, 0, 0,
                    uint64_t(a.kv.hd), uint64_t(a.nq), uint64_t(a.kv.nk));
-  k.k3 = (uint64_t(plan.form) << 16) | (uint64_t(plan.splits > 1) << 24) | key_code(*q8);
+  k.k3 = (uint64_t(plan.form) << 16) | (uint64_t(plan.splits > 1) << 24) |
+         key_code(*q8);
   const PagedQ8Args args{attn_args(a, plan, 1.0f, attn_outgrows(a, 1)),
                          {q8->k_scale, q8->k_ps, q8->k_bs, q8->k_hs},
                          {q8->v_scale, q8->v_ps, q8->v_bs, q8->v_hs},

@@ -324,10 +324,50 @@ uint32_t q8_write_grid(int64_t T, int32_t R, int32_t nk, int32_t block) {
 // A wavefront a row.
 uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4)); }
 
+// Form and splits as attn_plan.
 AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                       bool aligned, int64_t kv_max, uint64_t workspace) {
-  (void)aligned;
-  return attn_plan(dtype, T, R, nq, nk, hd, false, kv_max, workspace);
+  AttnPlan p{};
+  const int64_t rows = T * nq, g = nq / nk, f32 = dtype == TRI_F32;
+  int64_t have = cdiv(rows, 4), want = 512, run = 256, tiles = 0;
+  p.form = kAttnAny;
+  p.block = kBlock;
+  if (attn_q8_matrix(aligned, hd)) {
+    const int64_t rpr = cdiv(T, R) * g, tiles16 = cdiv(T * g, 16) * nk;
+    const bool few = rpr <= 16 || (tiles16 <= 64 && kv_max <= 4096);
+    p.form = few ? kAttnRows : kAttnTile;
+    const int64_t m = few ? 16 : 128;
+    tiles = T * g / m + R;
+    const int64_t full = cdiv(T * g, m), busy = R < T ? R : T;
+    have = (full > busy ? full : busy) * nk;
+    want = few ? 1024 : 256;
+    run = few ? 1024 : 512;
+    const bool equal = T % R == 0;
+    const int64_t expected = (equal ? R * cdiv(T / R * g, 128) : full + busy / 2) * nk;
+    const int64_t most = !equal ? kUnits * 9 / 8 : R > 1 ? kUnits - 1 : kUnits;
+    if (!few && !f32 && hd <= 128 && full * nk <= kUnits && expected <= most) {
+      p.form = kAttnPair;
+      p.block = 2 * kBlock;
+    }
+    if (few) p.block = uint32_t(64 * rows_waves(attn_hdp(hd)));
+  }
+  const auto splits = [&](int64_t wgs, int64_t keys) {
+    const int64_t x = wgs / have, most = cdiv(kv_max, keys);
+    return x < most ? x : most;
+  };
+  int64_t s = splits(want, run);
+  if (p.form == kAttnRows && kv_max > 512 && splits(256, 512) > s) s = splits(256, 512);
+  if (s > TRI_MAX_KV_SPLITS) s = TRI_MAX_KV_SPLITS;
+  while (s > 1 && attn_workspace(T, nq, hd, int32_t(s)) > workspace) --s;
+  p.splits = s < 1 ? 1 : int32_t(s);
+  p.tiles = int32_t(tiles);
+  const int64_t grid = tiles * nk * p.splits;
+  if (p.form == kAttnAny)
+    p.grid[0] = clamp_grid(cdiv(rows * p.splits, 4));
+  else if (grid * p.block < int64_t(1) << 32)   // the work-items a launch can have
+    p.grid[0] = uint32_t(grid);
+  p.grid[1] = p.splits < 2 ? 0 : clamp_grid(p.splits > kJoinWave ? rows : cdiv(rows, 4));
+  return p;
 }
 
 // Workgroups of a role variant for T tokens (I is the row width: the norm
@@ -394,7 +434,9 @@ static bool paged_key_valid(const Key &k) {
   const uint32_t form = key_attn_form(k);
   if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
   if (k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
-  const bool matrix = !q8 && attn_matrix(key_dtype(k), key_flags(k) & kAlign, int32_t(hd));
+  const bool aligned = key_flags(k) & kAlign;
+  const bool matrix = q8 ? attn_q8_matrix(aligned, int32_t(hd))
+                         : attn_matrix(key_dtype(k), aligned, int32_t(hd));
   if (form == kAttnPair && (key_dtype(k) == TRI_F32 || hd > 128)) return false;
   return matrix ? form >= kAttnRows && form <= kAttnPair : form == kAttnAny;
 }

@@ -579,3 +579,117 @@ def test_attention_at_the_last_position(cache, dtype, code, n, hd, window):
     same(p, after)
     gk, gv = cache.kv_read_q8(p["kc"], p["vc"], p["ks"], p["vs"], p["table"], p["kv_len"], p["q_start"], n, DT[dtype])
     read_check(short | {c: p[c] for c in ("kc", "vc", "ks", "vs")}, gk, gv, dtype)
+
+
+# ---- tiles of many rows: every case of these is served by them ------------------------------
+TILE_HEADS = [("bf16", 8, 1, 128), ("bf16", 5, 1, 80), ("bf16", 16, 1, 64), ("bf16", 6, 1, 256),
+              ("bf16", 10, 2, 96), ("bf16", 33, 3, 48), ("f32", 20, 1, 64), ("f32", 20, 1, 80),
+              ("f32", 32, 1, 128), ("f32", 21, 1, 256)]
+
+
+def tile_problem(dtype, code, lens, nq, nk, hd, page=16, block=8, **kw):
+    """A problem whose table is wide: more keys than tiles of few rows serve."""
+    p = problem(dtype, code, lens, nq, nk, hd, page, block, **kw)
+    wide = torch.full((len(lens), 4200 // page + 1), -1, dtype=torch.int32, device=DEV)
+    wide[:, :p["table"].shape[1]] = p["table"]
+    return dict(p, table=wide)
+
+
+def tile_check(cache, p, dtype, window=0, **kw):
+    """The result of the form that many rows take: with few tiles and heads of up to 128 in
+    bf16 two groups of wavefronts share the keys, else one has them. Rows of nobody make the
+    tiles too many for the first; both are compared with the oracle."""
+    want = oracle(p, window)
+    got = attend(cache, p, window=window, **kw)
+    assert cache.last_selection().variant in (P.PA8_TILE, P.PA8_PAIR)
+    check(got, want, dtype)
+    T, nq, hd = p["q"].shape
+    nk = p["kc"].shape[2]
+    if dtype == "bf16" and hd <= 128 and cache.last_selection().variant == P.PA8_PAIR:
+        more = 300 * 128 * nk // nq
+        q = torch.cat([p["q"], torch.zeros((more, nq, hd), dtype=p["q"].dtype, device=DEV)])
+        got = attend(cache, dict(p, q=q), window=window)
+        assert cache.last_selection().variant == P.PA8_TILE
+        assert (got[T:] == 7.0).all()
+        check(got[:T], want, dtype)
+
+
+@pytest.mark.parametrize("batch", list(TILE_BATCHES))
+@pytest.mark.parametrize("dtype,nq,nk,hd", TILE_HEADS)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("block", [8, 1])
+def test_tiles_heads_and_lengths(cache, block, code, dtype, nq, nk, hd, batch):
+    tile_check(cache, tile_problem(dtype, code, TILE_BATCHES[batch], nq, nk, hd, block=block, seed=hd), dtype)
+
+
+@pytest.mark.parametrize("layout", ["slot", "head", "pair"])
+@pytest.mark.parametrize("page,block", [(3, 3), (16, 16), (24, 12), (64, 64), (100, 50), (100, 25), (128, 4)])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_tiles_pages_blocks_and_layouts(cache, dtype, code, page, block, layout):
+    p = tile_problem(dtype, code, [(300, 129), (65, 40), (200, 30)], 16, 1, 64, page, block, layout=layout, pad=3,
+                     seed=page)
+    tile_check(cache, p, dtype)
+
+
+@pytest.mark.parametrize("window", [1, 15, 64, 100, 1000])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("block", [16, 2])
+def test_tiles_window(cache, dtype, code, block, window):
+    p = tile_problem(dtype, code, [(700, 150), (90, 64), (10, 20)], 8, 1, 128, block=block)
+    tile_check(cache, p, dtype, window)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_tiles_split_keys(cache, dtype, code, hd):
+    """Long contexts before a chunk: split, joined, and the same bits every time."""
+    p = problem(dtype, code, [(4300, 40), (2000, 50), (0, 0)], 16, 2, hd, 16, 16, seed=hd, pad=1)
+    want = oracle(p)
+    got = attend(cache, p)
+    assert cache.last_selection().variant in (P.PA8_TILE, P.PA8_PAIR)
+    assert cache.last_selection().n_launches == 2
+    check(got, want, dtype)
+    for _ in range(3):
+        assert torch.equal(got, attend(cache, p))
+    check(attend(cache, p, window=700), oracle(p, 700), dtype)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("hd", [64, 256])
+def test_tiles_nan_in_hidden_places(cache, dtype, code, hd):
+    lens = [(300, 137), (220, 120)]
+    p = tile_problem(dtype, code, lens, 16, 2, hd, block=1)
+    nan = float("nan")
+    for i, (r, back) in enumerate([(0, 1), (0, 5), (0, 100), (1, 3), (1, 80)]):
+        x = lens[r][0] - back
+        pid = int(p["table"][r, x // 16])
+        if code == "e4m3":
+            p["vc"][pid, x % 16, i % 2, 3 * i] = torch.tensor(nan, device=DEV).to(CODE[code])
+        if i == 2:
+            p["ks"][pid, x % 16, 0] = nan
+        if i in (1, 4):
+            p["vs"][pid, x % 16, 1] = nan
+    tile_check(cache, p, dtype)
+    tile_check(cache, p, dtype, window=90)
+    p["q"][3, 1] = nan
+    p["q"][50, 9, 5] = float("inf")
+    tile_check(cache, p, dtype)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_tiles_bad_pages_and_scores(cache, dtype, code):
+    p = tile_problem(dtype, code, [(300, 129), (200, 60)], 16, 2, 64)
+    p["table"][0, 2], p["table"][0, 5], p["table"][1, :] = p["kc"].shape[0], -7, 2 ** 31 - 1
+    tile_check(cache, p, dtype)
+    p = tile_problem(dtype, code, [(300, 129), (200, 60)], 16, 2, 64, peak=100.0)
+    tile_check(cache, p, dtype)
+    for scale in (0.0, -0.3):
+        p = tile_problem(dtype, code, [(300, 129), (200, 60)], 16, 2, 64)
+        p["scale"] = scale
+        tile_check(cache, p, dtype)
+    tile_check(cache, p, dtype, out=p["q"].clone().fill_(7.0))
