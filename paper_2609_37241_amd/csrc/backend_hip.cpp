@@ -66,7 +66,7 @@ int be_resolve(int32_t kvariant, uint32_t dtype, int32_t ksub, void **fn) {
     sym = emb_kernel(kvariant, dtype);
   else if (kvariant >= KV_SLOTS && kvariant <= PA_PAIR)
     sym = paged_kernel(kvariant, dtype, ksub);
-  else if (kvariant >= Q8W_ANY && kvariant <= PA8_PAIR)
+  else if (kvariant >= Q8W_ANY && kvariant <= PA8_JOIN)
     sym = paged_q8_kernel(kvariant, dtype, ksub);
   else if (kvariant == EMPTY)
     sym = empty_kernel();

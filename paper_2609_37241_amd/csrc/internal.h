@@ -26,7 +26,7 @@ enum Variant : int32_t {
   PA_ANY = 90, PA_ROWS = 91, PA_TILE = 92, PA_JOIN = 93, PA_PAIR = 94,
   EMPTY = 99,
   Q8W_ANY = 100, Q8W_VEC = 101, Q8R_ANY = 102, Q8R_VEC = 103,
-  PA8_ANY = 104, PA8_ROWS = 105, PA8_TILE = 106, PA8_PAIR = 107,
+  PA8_ANY = 104, PA8_ROWS = 105, PA8_TILE = 106, PA8_PAIR = 107, PA8_JOIN = 108,
 };
 
 // Token buckets up to this one are "decode sized": RoPE head slices, one
@@ -194,6 +194,9 @@ struct AttnPlan {
   uint32_t grid[2];      // the attention launch (0: more than a launch can have), and the
                          // join's when splits > 1
   uint32_t block;        // work-items of the first's workgroups
+  // few rows over an 8-bit cache: log2 of the K heads of a tile, of the keys of a step that
+  // workgroups share out
+  int32_t heads, step_shift;
 };
 // `aligned`: every address and stride of q, out and the cache is a multiple of
 // 16 bytes. kv_max: the most keys a row can see. workspace: bytes available.
@@ -210,9 +213,11 @@ uint32_t kv_write_grid(int64_t T, uint32_t row_items);
 inline bool attn_q8_matrix(bool aligned, int32_t hd) {
   return aligned && hd % 16 == 0 && hd <= kAttnMatrixHd;
 }
-// As attn_plan, `aligned` with the codes.
+// As attn_plan, `aligned` with the codes; keys_max: the most keys the table holds for a request.
 AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
-                      bool aligned, int64_t kv_max, uint64_t workspace);
+                      bool aligned, int64_t kv_max, int64_t keys_max, uint64_t workspace);
+// Whether four wavefronts join a row of PA8_ROWS' parts: rows too few to fill the units.
+inline bool q8_join_four(int64_t T, int32_t nq) { return T * nq < 1024; }
 uint32_t q8_write_grid(int64_t T, int32_t R, int32_t nk, int32_t block);
 uint32_t q8_read_grid(int64_t T);
 // n / d by multiplication (kernargs.h).

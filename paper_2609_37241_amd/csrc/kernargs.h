@@ -231,6 +231,7 @@ struct Q8RowsArgs {
   FastDiv nk_div;         // by nk
 };
 
+constexpr int32_t kQ8Splits = 128;   // parts of a tile of few rows over an 8-bit cache, at most
 // Attention over an 8-bit cache (PA8_*). The maxima that its parts leave are already in
 // powers of two, so PA_JOIN takes `a` with a scale of 1.
 struct PagedQ8Args {
@@ -239,6 +240,10 @@ struct PagedQ8Args {
   float scale;            // |scale| log2 e
   int32_t block;
   FastDiv block_div;      // by block
+  int32_t runs;           // PA8_ROWS: its workgroups
+  int32_t step_shift;     // steps of 2^step_shift keys are what it shares out
+  int32_t four;           // PA8_JOIN: 1: four wavefronts join a row, else one
+  int32_t reserved;
 };
 
 // An argument block held in device memory for launches without kernel
@@ -291,7 +296,7 @@ static_assert(sizeof(PagedArgs) == 216 && __builtin_offsetof(PagedArgs, div) == 
               "PagedArgs layout");
 static_assert(sizeof(Q8RowsArgs) == 248 && __builtin_offsetof(Q8RowsArgs, T) == 192,
               "Q8RowsArgs layout");
-static_assert(sizeof(PagedQ8Args) == 296 && __builtin_offsetof(PagedQ8Args, scale) == 280,
+static_assert(sizeof(PagedQ8Args) == 312 && __builtin_offsetof(PagedQ8Args, scale) == 280,
               "PagedQ8Args layout");
 static_assert(sizeof(ResidentBlock) == 320 && __builtin_offsetof(ResidentBlock, grid) == 288 &&
                   __builtin_offsetof(ResidentBlock, tag) == 292,

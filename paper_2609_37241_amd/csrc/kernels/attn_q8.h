@@ -22,6 +22,9 @@
 namespace tri {
 namespace dev {
 
+// Whether PA8_ROWS reads codes past the caches (nontemporally).
+constexpr bool kStreamCodes = true;
+
 // Eight codes as bf16 (exact): v_cvt_scalef32_pk_bf16_fp8 of two, or a conversion to float32 of
 // each, whose upper half it is.
 template <int CT>
@@ -176,18 +179,36 @@ __device__ inline NanKeys nan_keys(int32_t key, bool inside, const int32_t *tabl
 }
 
 // ---- PA8_ROWS -----------------------------------------------------------------------------------
-// Few rows per request (decode), as PA_ROWS: a tile is 16 rows, the wavefronts share out
-// its keys, 64 at a time each with its own softmax, joined in LDS at the end. HBM-bound:
-// K and V come in whole rows and pass as codes through a part of LDS that is the wavefront's
-// own, where a lane's 16 codes of K are two products' operands, and the transposing read of
-// bytes gives it 8 keys of one element of V. A lane fetches the two scales of one
-// of the 64 keys; the others read them from LDS.
-template <int DT, int HDP>
+// Few rows per request (decode), as PA_ROWS: the wavefronts share out a tile's keys,
+// each with its own softmax, joined in LDS at the end. HBM-bound: K and V come in whole rows
+// and pass as codes through a part of LDS that is the wavefront's own, where a lane's 16
+// codes of K are two products' operands, and the transposing read of bytes gives it 8 keys of one
+// element of V.
+//
+// Products of 16 rows would leave most of them empty where few query heads share a K head.
+// So a tile is 16 / HG rows of each of HG neighbouring K heads, and a step of a wavefront 64 / HG
+// keys of each: 64 rows of K, head by head, against all 16 columns. A column takes the
+// scores of its own head's rows and gives the others' weights of 0, so the products are as many
+// per byte as with one head, the exponentials 1 / HG, and what is read in a slot is HG
+// heads long (64 requests of 8192 keys, 4 of 8 heads: FIGURES).
+// A NaN code of V would meet other heads' weights of 0: a unit whose sums hold one where
+// the weights are finite is done again with such codes cleared.
+//
+// A workgroup fills a compute unit (its registers), so what it does not overlap by itself
+// nothing does: its start, the first loads and the join took 4.3 us of each of several
+// workgroups a unit. So there is at most one a unit, and each takes as many steps: the
+// steps of all tiles, numbered from the requests' lengths by every workgroup for itself, are
+// cut into equal runs, which may end inside a tile; the parts of such a tile leave partial sums. A
+// workgroup is a step ahead in loading K and V, two in looking up pages, also from
+// one tile to the next.
+template <int DT, int HDP, int HG>
 struct Rows8Shape {
   static constexpr int ES = Elt<DT>::ES;
   static constexpr int NW = rows_waves(HDP);              // wavefronts
-  static constexpr int KB = 64;         // keys of a step
-  static constexpr int MB = KB / 16;
+  static constexpr int TM = 16 / HG;                      // rows of a K head in a tile
+  static constexpr int KB = 64;                           // rows of K of a step
+  static constexpr int KH = KB / HG;                      // its keys
+  static constexpr int MB = KB / 16, MH = MB / HG;        // 16 rows of K: all, a head's
   static constexpr int QP = DT == kF32 ? 3 : 1;           // parts of a query
   static constexpr int WP = DT == kF32 ? 3 : 2;           // and of a weight
   static constexpr int NS = HDP / 64;                     // 16-byte vectors of a lane's K
@@ -201,88 +222,266 @@ struct Rows8Shape {
   static constexpr int WAVE_LDS = KB * LS > 16 * OS * 4 ? KB * LS : 16 * OS * 4;
 };
 
-template <int DT, int CT, int HDP>
+// The steps that all tiles take, `step` keys each, numbered request by request, tile by
+// tile, and that once for each HG heads: the host's choice of `step` keeps their number
+// below 2^31. Up to 64 requests are held by a lane each, more in LDS.
+template <int TM>
+struct Numbering {
+  const PagedQ8Args &a8;
+  int32_t *sums;              // [R] of LDS
+  Request rq;                 // the lane's request
+  int32_t first, all;         // steps before it, of all (for one HG heads)
+  int32_t per;                // of a workgroup
+
+  // Steps of each of a request's tiles, whose rows see at most 15 keys more than the window.
+  __device__ int32_t steps_of(const Request &x) const {
+    const int32_t w = a8.a.window, keys = w > 0 && w < 0x7FFFFF00 && w + 15 < x.kv ? w + 15 : x.kv;
+    const int32_t n = int32_t((uint32_t(keys) + (1u << a8.step_shift) - 1) >> a8.step_shift);
+    return n > 0 ? n : 1;
+  }
+  // Tiles of its n g rows of a K head.
+  __device__ int32_t tiles_of(const Request &x) const {
+    const int32_t n = x.q1 - x.q0;
+    return n > 0 ? (n * a8.a.g + TM - 1) / TM : 0;
+  }
+
+  // The whole workgroup of NW wavefronts; `heads`: how often all steps are taken, `runs`:
+  // workgroups to share them.
+  template <int NW>
+  __device__ void number(int32_t *wave_sums, int32_t heads, int32_t runs) {
+    const PagedArgs &a = a8.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // over the first `lanes` lanes: sums with those of the lanes before, the largest
+    const int lanes = a.R < 64 ? a.R : 64;
+    const auto scan = [&](int32_t x) {
+      for (int d = 1; d < lanes; d *= 2) {
+        const int32_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+      }
+      return x;
+    };
+    const auto largest = [&](int32_t x) {
+      for (int d = 1; d < lanes; d *= 2) {
+        const int32_t y = __shfl_xor(x, d);
+        x = y > x ? y : x;
+      }
+      return __builtin_amdgcn_readfirstlane(x);
+    };
+    int32_t most = 0;   // steps of the longest tile
+    if (a.R <= 64) {
+      rq = request_of(a, lane < a.R ? lane : 0);
+      const int32_t steps = steps_of(rq), mine = lane < a.R ? tiles_of(rq) * steps : 0;
+      const int32_t sum = scan(mine);
+      first = sum - mine;
+      all = __builtin_amdgcn_readlane(sum, a.R - 1);
+      if (a.splits > 1) most = largest(steps);
+    } else {
+      // consecutive requests a work-item, then the sums of what was before
+      const int32_t each = (a.R + 64 * NW - 1) / (64 * NW), r0 = int32_t(threadIdx.x) * each;
+      int32_t mine = 0;
+      for (int32_t r = r0; r < r0 + each && r < a.R; ++r) {
+        const Request x = request_of(a, r);
+        const int32_t n = steps_of(x);
+        most = n > most ? n : most;
+        mine += tiles_of(x) * n;
+      }
+      const int32_t sum = scan(mine);
+      most = largest(most);
+      if (lane == 63) {
+        wave_sums[wave] = sum;
+        wave_sums[NW + wave] = most;
+      }
+      __syncthreads();
+      int32_t before = sum - mine;
+      all = 0;
+      for (int w = 0; w < NW; ++w) {
+        before += w < wave ? wave_sums[w] : 0;
+        all += wave_sums[w];
+        most = wave_sums[NW + w] > most ? wave_sums[NW + w] : most;
+      }
+      for (int32_t r = r0; r < r0 + each && r < a.R; ++r) {
+        sums[r] = before;
+        const Request x = request_of(a, r);
+        before += tiles_of(x) * steps_of(x);
+      }
+      __syncthreads();
+      all = __builtin_amdgcn_readfirstlane(all);
+      most = __builtin_amdgcn_readfirstlane(most);
+    }
+    per = int32_t((uint32_t(all) * uint32_t(heads) + uint32_t(runs) - 1) / uint32_t(runs));
+    // a tile of n steps meets at most (n - 2) / per + 2 runs
+    if (a.splits > 1) {
+      const int32_t least = (most + a.splits - 2) / (a.splits - 1);
+      per = per < least ? least : per;
+    }
+    if (per < 1) per = 1;
+  }
+
+  // The request of step `in` of all.
+  __device__ int32_t find(int32_t in) const {
+    if (a8.a.R > 64)
+      return __builtin_amdgcn_readfirstlane(
+          last_request(a8.a.R, [&](int32_t y) { return sums[y] <= in; }));
+    const uint64_t hit = __ballot(int32_t(threadIdx.x & 63) < a8.a.R && first <= in);
+    return 63 - __builtin_clzll(hit);
+  }
+  // Steps before request r.
+  __device__ int32_t before(int32_t r) const {
+    return a8.a.R > 64 ? __builtin_amdgcn_readfirstlane(sums[r]) : __builtin_amdgcn_readlane(first, r);
+  }
+  __device__ Request request(int32_t r) const {
+    if (a8.a.R > 64) return request_of(a8.a, r);
+    return {__builtin_amdgcn_readlane(rq.q0, r), __builtin_amdgcn_readlane(rq.q1, r),
+            __builtin_amdgcn_readlane(rq.kv, r)};
+  }
+};
+
+// What a workgroup does in one go: keys [b, e) of a tile's HG K heads from kh on, the tile's
+// rows from row0 on of request r's.
+struct Unit {
+  int32_t r;                  // -1: none
+  int32_t row0, b, e, steps;
+  uint32_t kh;
+  int32_t part;               // which part of the tile, -1: all of it
+};
+
+// The keys that a tile of `rows` rows sees some of, and the positions of its first and last row.
+struct Span {
+  int32_t rows, p0, p1, lo, hi;
+};
+template <int TM>
+__device__ inline Span span_of(const PagedArgs &a, const Request &x, int32_t row0) {
+  Span s;
+  const int32_t all = (x.q1 - x.q0) * a.g, base = x.kv - (x.q1 - x.q0);
+  s.rows = all - row0 < TM ? all - row0 : TM;
+  s.p0 = base + int32_t(fast_div(uint32_t(row0), a.g_div));
+  s.p1 = base + int32_t(fast_div(uint32_t(row0 + s.rows - 1), a.g_div));
+  s.lo = s.p0 < 0 ? 0 : first_key(s.p0, a.window);
+  s.hi = s.p1 + 1 > s.lo ? s.p1 + 1 : s.lo;
+  return s;
+}
+
+// The unit at step *at of all, which ends at `end` (the workgroup's run) or with the tile; *at
+// is behind it then. Without partial sums tiles are whole, and those that begin in the run are
+// its workgroup's.
+template <int HG>
+__device__ inline Unit unit_at(const Numbering<16 / HG> &nb, int32_t *at, int32_t end, int32_t wave_keys) {
+  constexpr int TM = 16 / HG;
+  const PagedArgs &a = nb.a8.a;
+  Unit u;
+  u.r = -1;
+  while (*at < end) {
+    const uint32_t heads = uint32_t(*at) / uint32_t(nb.all);
+    const int32_t in = *at - int32_t(heads) * nb.all, r = nb.find(in), before = nb.before(r);
+    const Request x = nb.request(r);
+    const int32_t steps = nb.steps_of(x);
+    const int32_t tile = int32_t(uint32_t(in - before) / uint32_t(steps));
+    const int32_t s0 = in - before - tile * steps, begin = *at - s0;
+    int32_t to = begin + steps;
+    if (a.splits < 2 && s0 > 0) {
+      *at = to;
+      continue;
+    }
+    u.part = -1;
+    if (a.splits > 1) {
+      if (s0 > 0 || to > end) u.part = int32_t(blockIdx.x) - int32_t(uint32_t(begin) / uint32_t(nb.per));
+      to = to < end ? to : end;
+    }
+    u.r = r;
+    u.kh = heads * HG;
+    u.row0 = tile * TM;
+    const Span s = span_of<TM>(a, x, u.row0);
+    const int64_t from = s.lo + (int64_t(s0) << nb.a8.step_shift);
+    const int64_t till = from + (int64_t(to - *at) << nb.a8.step_shift);
+    u.b = int32_t(from < s.hi ? from : s.hi);
+    u.e = int32_t(till < s.hi ? till : s.hi);
+    u.steps = u.e > u.b ? (u.e - u.b + wave_keys - 1) / wave_keys : 1;
+    *at = to;
+    break;
+  }
+  return u;
+}
+
+template <int DT, int CT, int HDP, int HG>
 __device__ void body_pa8_rows(const PagedQ8Args &a8) {
-  typedef Rows8Shape<DT, HDP> S;
-  constexpr int ES = S::ES, KB = S::KB, MB = S::MB, NS = S::NS, ND = S::ND, NW = S::NW;
-  constexpr int QP = S::QP, WP = S::WP;
+  typedef Rows8Shape<DT, HDP, HG> S;
+  constexpr int ES = S::ES, KB = S::KB, KH = S::KH, MB = S::MB, MH = S::MH, NS = S::NS, ND = S::ND;
+  constexpr int NW = S::NW, TM = S::TM, QP = S::QP, WP = S::WP;
   const PagedArgs &a = a8.a;
   __shared__ __attribute__((aligned(16))) char lds[NW * S::WAVE_LDS];
   __shared__ __attribute__((aligned(16))) float scales[NW][2][KB];   // s c of K, s of V
   __shared__ float wave_m[NW][16], wave_l[NW][16];
+  __shared__ int32_t sums[TRI_MAX_REQUESTS], wave_sums[2 * NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, quarter = lane >> 4;
-  const uint32_t kh = blockIdx.x % uint32_t(a.nk), rest = blockIdx.x / uint32_t(a.nk);
-  const int32_t split = int32_t(rest % uint32_t(a.splits));
-  const Tile t = find_tile<16>(a, int32_t(rest / uint32_t(a.splits)));
-  if (t.r < 0) return;
-  const int32_t lo = t.p0 < 0 ? 0 : first_key(t.p0, a.window), hi = t.p1 + 1;
-  int32_t b, e;
-  split_keys(lo, hi, a.splits, split, &b, &e);
-  // what the lane's query sees; rows behind the tile's last do as that one
-  int32_t token, head;
-  row_of(a, t, n < t.rows ? n : t.rows - 1, int32_t(kh), &token, &head);
-  const int32_t my_p = t.rq.kv - (t.rq.q1 - token);
-  const int32_t my_lo = my_p < 0 ? 0 : first_key(my_p, a.window), my_hi = my_p + 1;
-  // keys that all rows see
-  const int32_t all_lo = t.p1 < 0 ? 0 : first_key(t.p1, a.window), all_hi = t.p0 + 1;
-
-  // product i of K takes elements 64 (i / 2) + 16 quarter + 8 (i % 2) .. of a row
-  u32x4 q[2 * NS][QP];
-  {
-    const char *p = static_cast<const char *>(a.q) +
-                    (int64_t(token) * a.q_ts + int64_t(head) * a.hd) * ES;
-#pragma unroll
-    for (int i = 0; i < 2 * NS; ++i) {
-      const int d = 64 * (i / 2) + 16 * quarter + 8 * (i % 2);
-      load_query<DT, QP>(p + d * ES, d < a.hd, a.flip, q[i]);
-    }
-  }
-  const int32_t *table = a.table + int64_t(t.r) * a.table_rs;
-  const char *kp = static_cast<const char *>(a.k.p) + int64_t(kh) * a.k.hs;
-  const char *vp = static_cast<const char *>(a.v.p) + int64_t(kh) * a.v.hs;
+  const int hn = n / TM;                                   // the column's head
+  const int lane_key = lane % KH, lane_head = lane / KH;   // the lane's row of K
   char *vl = lds + wave * S::WAVE_LDS;
+  Numbering<TM> nb{a8, sums, {}, 0, 0, 0};
+  nb.template number<NW>(wave_sums, a.nk / HG, int32_t(gridDim.x));
+  const int64_t all = int64_t(nb.all) * (a.nk / HG), run = int64_t(blockIdx.x) * nb.per;
+  const int32_t begin = int32_t(run < all ? run : all);
+  const int32_t end = int32_t(run + nb.per < all ? run + nb.per : all);
+  bool clean = false, again = false;   // NaN codes are cleared; there were some
+start:
+  int32_t at = begin;
+  // what is computed, what is loaded (a step ahead), what is looked up (two)
+  Unit now = unit_at<HG>(nb, &at, end, NW * KH);
+  if (now.r < 0) return;
+  Unit ahead = now, far = now;
+  int32_t now_step = 0, ahead_step = 0, far_step = 0;
+  // the step after: of the next unit after a unit's last (behind all units: the last's again)
+  const auto advance = [&](Unit &x, int32_t &step) {
+    if (++step < x.steps) return;
+    const Unit y = unit_at<HG>(nb, &at, end, NW * KH);
+    if (y.r >= 0) {
+      x = y;
+      step = 0;
+    } else {
+      x.r = -1;
+    }
+  };
 
-  f32x4 o[ND];
-#pragma unroll
-  for (int i = 0; i < ND; ++i) o[i] = f32x4{0, 0, 0, 0};
-  float m = kNegInf, l = 0.0f;
-
-  // the page of key k0 + lane (beyond the end: the last key's)
-  const auto look_up = [&](int32_t k0) {
-    const int32_t key = k0 + lane;
-    return table[fast_div(uint32_t(key < e ? key : e - 1), a.div)];
+  // the page of the lane's key in a step (beyond the end: the last key's)
+  const auto look_up = [&](const Unit &x, int32_t step) {
+    int32_t key = x.b + (step * NW + wave) * KH + lane_key;
+    key = key < x.e ? key : x.e - 1;
+    const int32_t r = x.r < 0 ? 0 : x.r;
+    return a.table[r * a.table_rs + fast_div(uint32_t(key < 0 ? 0 : key), a.div)];
   };
   // where the lane's key lies (the pool's first page for one that is not
   // there), handed to the lanes that load its row; behind the head's end a lane loads
   // the first vector and clears it on the way to LDS
   const int srow = lane / S::CH, sbyte = (lane % S::CH) * 16;
-  const bool one_layout = a.k.ps == a.v.ps && a.k.ss == a.v.ss;
+  const bool one_layout = a.k.ps == a.v.ps && a.k.ss == a.v.ss && a.k.hs == a.v.hs;
   const bool padded = a.hd < HDP, inside = sbyte < a.hd;
   const int lbyte = inside ? sbyte : 0;
   int64_t ko, vo;
-  uint64_t seen = 0;      // bit i: key k0 + i is there
-  float ksc, vsc;         // the lane's key's scales
-  const auto rows_of = [&](int32_t k0, int32_t page) {
-    const int32_t mine = k0 + lane;
-    const KeyPlace x = place_of(uint32_t(mine < e ? mine : e - 1), page, a8);
-    const bool ok = mine < e && x.id >= 0;
+  uint64_t seen = 0;      // bit i: row i of the step is there
+  float ksc, vsc;         // the lane's row's scales
+  const auto rows_of = [&](const Unit &x, int32_t step, int32_t page) {
+    int32_t key = x.b + (step * NW + wave) * KH + lane_key;
+    const bool in = key < x.e;
+    key = in ? key : x.e - 1;
+    const KeyPlace y = place_of(uint32_t(key < 0 ? 0 : key), page, a8);
+    const bool ok = in && y.id >= 0;
     seen = __ballot(ok);
-    const int64_t id = ok ? x.id : 0;
-    ko = id * a.k.ps + int64_t(x.slot) * a.k.ss;
+    const int64_t id = ok ? y.id : 0;
+    const uint32_t h = x.kh + uint32_t(lane_head);
+    ko = id * a.k.ps + int64_t(y.slot) * a.k.ss + int64_t(h) * a.k.hs;
     vo = ko;
-    if (!one_layout) vo = id * a.v.ps + int64_t(x.slot) * a.v.ss;
-    ksc = *scale_at(a8.ks, id, x.block, kh);
-    vsc = *scale_at(a8.vs, id, x.block, kh);   // (looked at in the next step only)
+    if (!one_layout) vo = id * a.v.ps + int64_t(y.slot) * a.v.ss + int64_t(h) * a.v.hs;
+    ksc = *scale_at(a8.ks, id, y.block, h);
+    vsc = *scale_at(a8.vs, id, y.block, h);   // (looked at in the next step only)
   };
   u32x4 k[S::NP], v[S::NP];
-  const auto load = [&](auto nt, u32x4(&x)[S::NP], const char *p, int64_t at) {
+  const auto load = [&](u32x4(&x)[S::NP], const void *c, int64_t at) {
+    const char *p = static_cast<const char *>(c) + lbyte;
     int64_t r[S::NP];
 #pragma unroll
     for (int i = 0; i < S::NP; ++i) r[i] = __shfl(at, srow + S::RP * i);
 #pragma unroll
-    for (int i = 0; i < S::NP; ++i)
-      x[i] = ld16<nt.value>(reinterpret_cast<const u32x4 *>(p + r[i] + lbyte));
+    for (int i = 0; i < S::NP; ++i) x[i] = ld16<kStreamCodes>(reinterpret_cast<const u32x4 *>(p + r[i]));
   };
   const auto to_lds = [&](u32x4(&x)[S::NP]) {
     if (padded)
@@ -294,204 +493,269 @@ __device__ void body_pa8_rows(const PagedQ8Args &a8) {
       *reinterpret_cast<u32x4 *>(vl + (srow + S::RP * i) * S::LS + sbyte) = x[i];
   };
 
-  int32_t odd_b = 0, odd_e = 0;   // from the first to the last step with NaN that was cleared
-  const auto steps = [&](auto nt) {
-    int32_t k0 = b + wave * KB;
-    rows_of(k0, look_up(k0));
-    load(nt, k, kp, ko);
-    // (loads return in order: before those of V, which need not be there for it)
-    int32_t page = look_up(k0 + NW * KB);
-    load(nt, v, vp, vo);
-    // (the last step loads for one more, of keys that are not there: with a branch around
-    // them the compiler waits for all loads at every step)
-    for (; k0 < e; k0 += NW * KB) {
-      const uint64_t there = seen;
-      const int32_t k1 = k0 + KB < e ? k0 + KB : e;
-      const bool mixed = k0 < all_lo || k1 > all_hi;   // some row sees not all of them
-      const bool partial = mixed || there != ~uint64_t(0);
-      bool odd = false;
-      float vs = (there >> lane) & 1 ? vsc : 0.0f;
-      if (mixed && vs != vs) {
-        odd = true;
-        vs = 0.0f;
+  int32_t page = look_up(far, far_step);
+  advance(far, far_step);
+  rows_of(ahead, ahead_step, page);
+  load(k, a.k.p, ko);
+  // (loads return in order: before those of V, which need not be there for it)
+  page = look_up(far, far_step);
+  load(v, a.v.p, vo);
+  ahead = far;
+  ahead_step = far_step;
+  if (far.r >= 0) advance(far, far_step);
+
+  // product i of K takes elements 64 (i / 2) + 16 quarter + 8 (i % 2) .. of a row
+  u32x4 q[2 * NS][QP];
+  f32x4 o[ND];
+  float m, l;
+  int32_t my_lo, my_hi, all_lo, all_hi, odd_b, odd_e;
+  // (behind the last unit loads are of keys that are not there: with a branch around
+  // them the compiler waits for all loads at every step)
+  for (;;) {
+    if (now_step == 0) {
+      // what the lane's query sees (rows behind the tile's last do as that one), and
+      // what all rows see
+      const Request rq = nb.request(now.r);
+      const Span sp = span_of<TM>(a, rq, now.row0);
+      const int c = n % TM;
+      const uint32_t x = uint32_t(now.row0 + (c < sp.rows ? c : sp.rows - 1));
+      const uint32_t tok = fast_div(x, a.g_div);
+      const int32_t token = rq.q0 + int32_t(tok);
+      const int32_t head = (int32_t(now.kh) + hn) * a.g + int32_t(x - tok * uint32_t(a.g));
+      const int32_t my_p = rq.kv - (rq.q1 - token);
+      my_lo = my_p < 0 ? 0 : first_key(my_p, a.window);
+      my_hi = my_p + 1;
+      all_lo = sp.p1 < 0 ? 0 : first_key(sp.p1, a.window);
+      all_hi = sp.p0 + 1;
+      const char *p = static_cast<const char *>(a.q) +
+                      (int64_t(token) * a.q_ts + int64_t(head) * a.hd) * ES;
+#pragma unroll
+      for (int i = 0; i < 2 * NS; ++i) {
+        const int d = 64 * (i / 2) + 16 * quarter + 8 * (i % 2);
+        load_query<DT, QP>(p + d * ES, d < a.hd, a.flip, q[i]);
       }
-      scales[wave][0][lane] = ksc * a8.scale;
-      scales[wave][1][lane] = vs;
-      to_lds(k);
-      rows_of(k0 + NW * KB, page);
-      load(nt, k, kp, ko);
-      page = look_up(k0 + 2 * NW * KB);
-      // S^T
-      f32x4 st[MB];
 #pragma unroll
-      for (int j = 0; j < MB; ++j) {
-        st[j] = f32x4{0, 0, 0, 0};
+      for (int i = 0; i < ND; ++i) o[i] = f32x4{0, 0, 0, 0};
+      m = kNegInf;
+      l = 0.0f;
+      odd_b = odd_e = 0;
+    }
+    const int32_t k0 = now.b + (now_step * NW + wave) * KH;
+    const uint64_t there = seen;
+    const int32_t k1 = k0 + KH < now.e ? k0 + KH : now.e;
+    const bool mixed = clean || k0 < all_lo || k1 > all_hi;   // some row sees not all of them
+    const bool partial = mixed || there != ~uint64_t(0);
+    bool odd = false;
+    float vs = (there >> lane) & 1 ? vsc : 0.0f;
+    if (mixed && vs != vs) {
+      odd = true;
+      vs = 0.0f;
+    }
+    scales[wave][0][lane] = ksc * a8.scale;
+    scales[wave][1][lane] = vs;
+    to_lds(k);
+    rows_of(ahead, ahead_step, page);
+    load(k, a.k.p, ko);
+    page = look_up(far, far_step);
+    // S^T
+    f32x4 st[MB];
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const u32x4 x = *reinterpret_cast<const u32x4 *>(vl + (16 * j + n) * S::LS + quarter * 16 +
-                                                           64 * s);
+    for (int j = 0; j < MB; ++j) {
+      st[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const bf16x8 y = codes_bf16<CT>(u32x2{x[2 * i], x[2 * i + 1]});
+      for (int s = 0; s < NS; ++s) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(vl + (16 * j + n) * S::LS + quarter * 16 +
+                                                         64 * s);
 #pragma unroll
-            for (int c = QP - 1; c >= 0; --c)   // (the small parts first)
-              st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  y, __builtin_bit_cast(bf16x8, q[2 * s + i][c]), st[j], 0, 0, 0);
-          }
-        }
-      }
-      // V in K's place; codes that are not there are zero, so that no weight of 0 meets a NaN
-      if (CT == kE4M3 && partial) {
+        for (int i = 0; i < 2; ++i) {
+          const bf16x8 y = codes_bf16<CT>(u32x2{x[2 * i], x[2 * i + 1]});
 #pragma unroll
-        for (int i = 0; i < S::NP; ++i) {
-          if (!((there >> (srow + S::RP * i)) & 1)) v[i] = u32x4{0, 0, 0, 0};
-          if (mixed) odd |= clear_nan_codes<CT>(v[i]);
-        }
-      }
-      if (mixed && __ballot(odd)) {
-        if (odd_b == odd_e) odd_b = k0;
-        odd_e = k1;
-      }
-      to_lds(v);
-      load(nt, v, vp, vo);
-      // softmax: the lane's keys are k0 + 16 j + 4 quarter + i
-#pragma unroll
-      for (int j = 0; j < MB; ++j)
-        st[j] *= *reinterpret_cast<const f32x4 *>(&scales[wave][0][16 * j + 4 * quarter]);
-      if (partial) {
-        const uint64_t see = in_range(there, k0, my_lo, my_hi) >> (4 * quarter);
-#pragma unroll
-        for (int j = 0; j < MB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            st[j][i] = (uint32_t(see >> (32 * (j / 2))) >> (16 * (j % 2) + i)) & 1 ? st[j][i] : kNegInf;
-      }
-      float top = kNegInf;
-#pragma unroll
-      for (int j = 0; j < MB; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, st[j][i]);
-      top = max_16_32(top);
-      const float mn = fmaxf(m, top);
-      const float ms = mn == kNegInf ? 0.0f : mn;
-      const float alpha = exp2_hw(m - ms);
-      m = mn;
-      l *= alpha;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) o[d] *= alpha;
-#pragma unroll
-      for (int g = 0; g < KB / 32; ++g) {
-        // weights of keys 32 g + (0, 16) + 4 quarter + i, and products
-        u32x4 p[WP];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          f32x4 w = st[2 * g + j];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[i] = exp2_hw(w[i] - ms);
-            l += w[i];
-          }
-          w *= *reinterpret_cast<const f32x4 *>(&scales[wave][1][32 * g + 16 * j + 4 * quarter]);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t x[WP];
-            bf16_parts<WP>(w[2 * i], w[2 * i + 1], x);
-#pragma unroll
-            for (int c = 0; c < WP; ++c) p[c][2 * j + i] = x[c];
-          }
-        }
-        // O^T: 8 rows of a quarter's, in the weights' order
-        const int row = 32 * g + 4 * quarter + ((n >> 1) & 3) + 16 * (n >> 3);
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const bf16x8 y = codes_bf16<CT>(lds_transpose8(vl + row * S::LS + 16 * d + 8 * (n & 1)));
-#pragma unroll
-          for (int c = WP - 1; c >= 0; --c)
-            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, __builtin_bit_cast(bf16x8, p[c]), o[d], 0, 0,
-                                                           0);
+          for (int c = QP - 1; c >= 0; --c)   // (the small parts first)
+            st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                y, __builtin_bit_cast(bf16x8, q[2 * s + i][c]), st[j], 0, 0, 0);
         }
       }
     }
-  };
-  // K and V that stay in no cache are read past them. (Two loops: in one, the compiler waits
-  // for all loads wherever the two kinds meet.)
-  if (b + wave * KB < e) {
-    if (a.stream)
-      steps(std::true_type());
-    else
-      steps(std::false_type());
-  }
-
-  l = sum_16_32(l);
-  for (int32_t x0 = odd_b; x0 < odd_e; x0 += NW * KB) {   // (the wavefront's own steps)
-    const NanKeys k = nan_keys<CT>(x0 + lane, x0 + lane < e, table, vp, kh, a8);
-    for (uint64_t keys = k.odd; keys; keys &= keys - 1) {
-      const int i = __builtin_ctzll(keys);
-      const char *x = vp + __shfl(k.at, i);
-      const bool sees = x0 + i >= my_lo && x0 + i < my_hi;
+    // V in K's place. Codes that are not there become zero, so that no weight of 0 meets a
+    // NaN (in LDS: changed on their way they would take as many registers again)
+    to_lds(v);
+    if (CT == kE4M3 && partial) {
+#pragma unroll 1
+      for (int i = 0; i < S::NP; ++i) {
+        u32x4 *p = reinterpret_cast<u32x4 *>(vl + (srow + S::RP * i) * S::LS + sbyte);
+        u32x4 x = {0, 0, 0, 0};
+        if ((there >> (srow + S::RP * i)) & 1) x = *p;
+        if (mixed) odd |= clear_nan_codes<CT>(x);
+        *p = x;
+      }
+    }
+    if (mixed && __ballot(odd)) {
+      if (odd_b == odd_e) odd_b = k0;
+      odd_e = k1;
+    }
+    load(v, a.v.p, vo);
+    // softmax over the column's own head: the lane's keys are k0 + 16 j + 4 quarter + i, j < MH
+    f32x4 sc[MH];
+#pragma unroll
+    for (int j = 0; j < MH; ++j) {
+      sc[j] = st[j];
+#pragma unroll
+      for (int h = 1; h < HG; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[j][i] = hn == h ? st[h * MH + j][i] : sc[j][i];
+      sc[j] *= *reinterpret_cast<const f32x4 *>(&scales[wave][0][KH * hn + 16 * j + 4 * quarter]);
+    }
+    if (partial) {
+      const uint64_t see = in_range(there >> (KH * hn), k0, my_lo, my_hi) >> (4 * quarter);
+#pragma unroll
+      for (int j = 0; j < MH; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sc[j][i] = (uint32_t(see >> (32 * (j / 2))) >> (16 * (j % 2) + i)) & 1 ? sc[j][i] : kNegInf;
+    }
+    float top = kNegInf;
+#pragma unroll
+    for (int j = 0; j < MH; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[j][i]);
+    top = max_16_32(top);
+    const float mn = fmaxf(m, top);
+    const float ms = mn == kNegInf ? 0.0f : mn;
+    const float alpha = exp2_hw(m - ms);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] *= alpha;
+    uint32_t p[MH][2][WP];   // the weights' parts
+#pragma unroll
+    for (int j = 0; j < MH; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[j][i] = exp2_hw(sc[j][i] - ms);
+        l += sc[j][i];
+      }
+      sc[j] *= *reinterpret_cast<const f32x4 *>(&scales[wave][1][KH * hn + 16 * j + 4 * quarter]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) bf16_parts<WP>(sc[j][2 * i], sc[j][2 * i + 1], p[j][i]);
+    }
+    // O^T, 32 rows of V at a time: 8 of a quarter's in the order of S^T
+#pragma unroll
+    for (int g = 0; g < KB / 32; ++g) {
+      u32x4 w[WP];
+#pragma unroll
+      for (int c = 0; c < WP; ++c)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int y = 2 * g + j;
+            w[c][2 * j + i] = HG == 1 || hn == y / MH ? p[y % MH][i][c] : 0u;
+          }
+      const int row = 32 * g + 4 * quarter + ((n >> 1) & 3) + 16 * (n >> 3);
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
-        float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
-        add_nan<CT>(x, sees, (k.whole >> i) & 1, 16 * d + 4 * quarter, a.hd, z);
-        o[d] = f32x4{z[0], z[1], z[2], z[3]};
+        const bf16x8 y = codes_bf16<CT>(lds_transpose8(vl + row * S::LS + 16 * d + 8 * (n & 1)));
+#pragma unroll
+        for (int c = WP - 1; c >= 0; --c)
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, __builtin_bit_cast(bf16x8, w[c]), o[d], 0, 0,
+                                                         0);
       }
     }
-  }
 
-  // join the wavefronts
-  if (quarter == 0) {
-    wave_m[wave][n] = m;
-    wave_l[wave][n] = l;
-  }
-  float *ol = reinterpret_cast<float *>(vl);
+    if (now_step + 1 == now.steps) {
+      l = sum_16_32(l);
+      if (CT == kE4M3 && HG > 1 && !clean && __ballot(holds_not_finite<ND>(o, 4, l))) again = true;
+      for (int32_t x0 = odd_b; x0 < odd_e; x0 += NW * KH) {   // (the wavefront's own steps)
+        const uint32_t h = now.kh + uint32_t(lane_head);
+        const char *vp = static_cast<const char *>(a.v.p) + int64_t(h) * a.v.hs;
+        const NanKeys x = nan_keys<CT>(x0 + lane_key, x0 + lane_key < now.e,
+                                       a.table + now.r * a.table_rs, vp, h, a8);
+        for (uint64_t keys = x.odd; keys; keys &= keys - 1) {
+          const int i = __builtin_ctzll(keys);
+          const int32_t key = x0 + i % KH;
+          const char *c = static_cast<const char *>(a.v.p) +
+                          int64_t(now.kh + uint32_t(i / KH)) * a.v.hs + __shfl(x.at, i);
+          const bool sees = hn == i / KH && key >= my_lo && key < my_hi;
 #pragma unroll
-  for (int d = 0; d < ND; ++d)
-    *reinterpret_cast<f32x4 *>(ol + n * S::OS + 16 * d + 4 * quarter) = o[d];
-  __syncthreads();
-  constexpr int PR = NW * 4;   // work-items of a row
-  const int row = threadIdx.x / PR, part = threadIdx.x % PR;
-  if (row >= t.rows) return;
-  float top = kNegInf;
+          for (int d = 0; d < ND; ++d) {
+            float z[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
+            add_nan<CT>(c, sees, (x.whole >> i) & 1, 16 * d + 4 * quarter, a.hd, z);
+            o[d] = f32x4{z[0], z[1], z[2], z[3]};
+          }
+        }
+      }
+      // join the wavefronts
+      if (quarter == 0) {
+        wave_m[wave][n] = m;
+        wave_l[wave][n] = l;
+      }
+      float *ol = reinterpret_cast<float *>(vl);
 #pragma unroll
-  for (int w = 0; w < NW; ++w)
-    if (wave_l[w][row] != 0.0f) top = fmaxf(top, wave_m[w][row]);
-  const float ts = top == kNegInf ? 0.0f : top;
-  float f[NW], sum = 0.0f;
+      for (int d = 0; d < ND; ++d)
+        *reinterpret_cast<f32x4 *>(ol + n * S::OS + 16 * d + 4 * quarter) = o[d];
+      __syncthreads();
+      constexpr int PR = NW * 4;   // work-items of a row
+      const int row = threadIdx.x / PR, share = threadIdx.x % PR;
+      const Request rq = nb.request(now.r);
+      if (row % TM < span_of<TM>(a, rq, now.row0).rows) {
+        float top = kNegInf;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    f[w] = 0.0f;
-    if (wave_l[w][row] != 0.0f) {
-      f[w] = exp2_hw(wave_m[w][row] - ts);
-      sum += f[w] * wave_l[w][row];
+        for (int w = 0; w < NW; ++w)
+          if (wave_l[w][row] != 0.0f) top = fmaxf(top, wave_m[w][row]);
+        const float ts = top == kNegInf ? 0.0f : top;
+        float f[NW], sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          f[w] = 0.0f;
+          if (wave_l[w][row] != 0.0f) {
+            f[w] = exp2_hw(wave_m[w][row] - ts);
+            sum += f[w] * wave_l[w][row];
+          }
+        }
+        const uint32_t x = uint32_t(now.row0 + row % TM), tok = fast_div(x, a.g_div);
+        const int32_t to = rq.q0 + int32_t(tok);
+        const int32_t oh = (int32_t(now.kh) + row / TM) * a.g + int32_t(x - tok * uint32_t(a.g));
+        const int64_t slot = (int64_t(to) * a.nq + oh) * a.splits + now.part;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int c = 0; c < (HDP + 4 * PR - 1) / (4 * PR); ++c) {
+          const int d = 4 * PR * c + 4 * share;
+          if (d >= a.hd) break;
+          f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int w = 0; w < NW; ++w) {
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(
+                reinterpret_cast<const float *>(lds + w * S::WAVE_LDS) + row * S::OS + d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], y[i], acc[i]);
+          }
+          if (now.part >= 0) {
+            *reinterpret_cast<f32x4 *>(a.part + slot * a.hd + d) = acc;
+          } else {
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = sum == 0.0f ? 0.0f : acc[i] * inv;
+            store4<DT>(a, to, oh, d, y);
+          }
+        }
+        if (now.part >= 0 && share == 0) {
+          a.ml[2 * slot] = top;
+          a.ml[2 * slot + 1] = sum;
+        }
+      }
+      // (the barrier: the sums are read)
+      if (ahead.r < 0) {
+        if (CT == kInt8 || HG == 1 || clean || !__syncthreads_or(again)) return;
+        clean = true;
+        goto start;
+      }
+      __syncthreads();
     }
-  }
-  row_of(a, t, row, int32_t(kh), &token, &head);
-  const int64_t at = (int64_t(token) * a.nq + head) * a.splits + split;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-  for (int c = 0; c < (HDP + 4 * PR - 1) / (4 * PR); ++c) {
-    const int d = 4 * PR * c + 4 * part;
-    if (d >= a.hd) break;
-    f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(
-          reinterpret_cast<const float *>(lds + w * S::WAVE_LDS) + row * S::OS + d);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], x[i], acc[i]);
-    }
-    if (a.splits > 1) {
-      *reinterpret_cast<f32x4 *>(a.part + at * a.hd + d) = acc;
-    } else {
-      float y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = sum == 0.0f ? 0.0f : acc[i] * inv;
-      store4<DT>(a, token, head, d, y);
-    }
-  }
-  if (a.splits > 1 && part == 0) {
-    a.ml[2 * at] = top;
-    a.ml[2 * at + 1] = sum;
+    now = ahead;
+    now_step = ahead_step;
+    ahead = far;
+    ahead_step = far_step;
+    if (far.r >= 0) advance(far, far_step);
   }
 }
 

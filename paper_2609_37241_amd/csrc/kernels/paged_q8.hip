@@ -1,7 +1,8 @@
 // The paged KV cache in 8 bits: rows into it (Q8W_*) and out of it (Q8R_*),
 // attention at any alignment and head size (PA8_ANY).
 #include "../internal.h"
-#include "paged_q8.h"
+#include "attn_q8.h"
+#include "join.h"
 
 namespace tri {
 using namespace dev;
@@ -301,6 +302,28 @@ __global__ __launch_bounds__(256) void k_pa8_any(PagedQ8Args a8) {
   }
 }
 
+// ---- PA8_JOIN: the parts of the tiles that PA8_ROWS cut (join.h) -----------------------------
+template <int DT, int HG>
+__global__ __launch_bounds__(256) void k_pa8_join(PagedQ8Args a8) {
+  constexpr int TM = 16 / HG;
+  const PagedArgs &a = a8.a;
+  __shared__ int32_t sums[TRI_MAX_REQUESTS], wave_sums[8];
+  Numbering<TM> nb{a8, sums, {}, 0, 0, 0};
+  nb.template number<4>(wave_sums, a.nk / HG, a8.runs);
+  const auto parts_of = [&](int32_t t, int32_t h) {
+    const int32_t r = __builtin_amdgcn_readfirstlane(
+        last_request(a.R, [&](int32_t x) { return a.q_start[x] <= t; }));
+    if (r < 0) return 0;
+    const Request rq = nb.request(r);
+    const int32_t kh = int32_t(fast_div(uint32_t(h), a.g_div));
+    const int32_t tile = ((t - rq.q0) * a.g + h - kh * a.g) / TM, steps = nb.steps_of(rq);
+    const uint32_t begin = uint32_t(nb.all * (kh / HG) + nb.before(r) + tile * steps);
+    const uint32_t per = uint32_t(nb.per);
+    return int32_t((begin + uint32_t(steps) - 1) / per - begin / per) + 1;
+  };
+  join_rows<DT, 4, kQ8Splits / 64>(a, a8.four != 0, parts_of);
+}
+
 namespace {
 template <class F>
 const void *sym(F *f) {
@@ -320,15 +343,24 @@ const void *rows_kernel(int32_t variant) {
 }
 }  // namespace
 
-const void *attn_q8_rows(uint32_t dtype, int32_t code, int32_t hdp);
+const void *attn_q8_rows(uint32_t dtype, int32_t code, int32_t hdp, int32_t heads);
 const void *attn_q8_tile_bf16(bool pair, int32_t code, int32_t hdp);
 const void *attn_q8_tile_f32(int32_t code, int32_t hdp);
 
-// sub: the code (tri_code) in bit 0; for the matrix forms the head size held from bit 6 on.
+template <int DT>
+static const void *join_kernel(int32_t heads) {
+  return heads == 4 ? sym(&k_pa8_join<DT, 4>) : heads == 2 ? sym(&k_pa8_join<DT, 2>) : sym(&k_pa8_join<DT, 1>);
+}
+
+// sub: the code (tri_code) in bit 0; for the matrix forms the head size held from bit 6 on,
+// for few rows the logarithm of the K heads of a tile in bits 1 and 2.
 const void *paged_q8_kernel(int32_t variant, uint32_t dtype, int32_t sub) {
   const bool e4m3 = (sub & 1) == TRI_E4M3;
   const int32_t code = sub & 1, hdp = sub & ~63;
-  if (variant == PA8_ROWS) return attn_q8_rows(dtype, code, hdp);
+  const int32_t heads = 1 << ((sub >> 1) & 3);
+  if (variant == PA8_JOIN)
+    return dtype == TRI_F32 ? join_kernel<kF32>(heads) : join_kernel<kBF16>(heads);
+  if (variant == PA8_ROWS) return attn_q8_rows(dtype, code, hdp, heads);
   if (variant == PA8_TILE && dtype == TRI_F32) return attn_q8_tile_f32(code, hdp);
   if (variant == PA8_TILE || variant == PA8_PAIR)
     return attn_q8_tile_bf16(variant == PA8_PAIR, code, hdp);

@@ -58,7 +58,7 @@ tri_status rows_q8(tri_cache *c, uint32_t op, const tri_kv_rows_args *p, void *s
 
 AttnPlan plan_of(const tri_attention_args &a, uint64_t workspace) {
   return attn_q8_plan(uint32_t(a.dtype), a.T, a.R, a.nq, a.kv.nk, a.kv.hd, attn_aligned(a, 1),
-                      attn_keys(a), workspace);
+                      attn_keys(a), int64_t(a.cols) * a.kv.page, workspace);
 }
 
 }  // namespace
@@ -88,11 +88,13 @@ tri_status tri_paged_attention_quant(tri_cache *c, const tri_attention_args *p, 
   Key k = make_key(op, uint32_t(a.dtype), a.T, attn_aligned(a, 1) ? kAlign : 0u, 0, 0, 0,
                    uint64_t(a.kv.hd), uint64_t(a.nq), uint64_t(a.kv.nk));
   k.k3 = (uint64_t(plan.form) << 16) | (uint64_t(plan.splits > 1) << 24) |
-         key_code(*q8);
+         (uint64_t(plan.heads) << 25) | key_code(*q8);
   const PagedQ8Args args{attn_args(a, plan, 1.0f, attn_outgrows(a, 1)),
                          {q8->k_scale, q8->k_ps, q8->k_bs, q8->k_hs},
                          {q8->v_scale, q8->v_ps, q8->v_bs, q8->v_hs},
-                         weight_scale(a.scale), q8->block, fast_div_of(uint32_t(q8->block))};
+                         weight_scale(a.scale), q8->block, fast_div_of(uint32_t(q8->block)),
+                         int32_t(plan.grid[0]),
+                         plan.step_shift, q8_join_four(a.T, a.nq), 0};
   return run_paged(c, op, k, a.T, plan.grid, plan.splits > 1 ? 2 : 1, plan.block, &args, sizeof args,
                    stream);
 }

@@ -324,49 +324,73 @@ uint32_t q8_write_grid(int64_t T, int32_t R, int32_t nk, int32_t block) {
 // A wavefront a row.
 uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4)); }
 
-// Form and splits as attn_plan.
+// Forms as attn_plan, but that float32 queries take tiles of many rows as bf16 ones do (three
+// products for one, not sixteen). Splits of those as attn_plan, too.
+//
+// PA8_ROWS takes as many K heads a tile, up to four, as its 16 rows have room for, and shares
+// its steps out to a workgroup a compute unit by itself, so the host sets only the most parts
+// that a tile may have: all that the join takes, within 128 MiB of partial sums; none where a
+// workgroup would take 16 tiles or more, or no request has over 1024 keys. Those take one head a
+// tile: as many workgroups as there are, of a step or two (one request of 500, 32 heads: FIGURES
+// us, with four heads and a join 19).
 AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
-                      bool aligned, int64_t kv_max, uint64_t workspace) {
+                      bool aligned, int64_t kv_max, int64_t keys_max, uint64_t workspace) {
   AttnPlan p{};
   const int64_t rows = T * nq, g = nq / nk, f32 = dtype == TRI_F32;
-  int64_t have = cdiv(rows, 4), want = 512, run = 256, tiles = 0;
+  const int64_t rpr = cdiv(T, R) * g, busy = R < T ? R : T;
+  int64_t have = cdiv(rows, 4), want = 512, run = 256, s = 0;
+  bool four = false;
   p.form = kAttnAny;
   p.block = kBlock;
   if (attn_q8_matrix(aligned, hd)) {
-    const int64_t rpr = cdiv(T, R) * g, tiles16 = cdiv(T * g, 16) * nk;
-    const bool few = rpr <= 16 || (tiles16 <= 64 && kv_max <= 4096);
+    const bool few = rpr <= 16 || (cdiv(T * g, 16) * nk <= 64 && kv_max <= 4096);
     p.form = few ? kAttnRows : kAttnTile;
-    const int64_t m = few ? 16 : 128;
-    tiles = T * g / m + R;
-    const int64_t full = cdiv(T * g, m), busy = R < T ? R : T;
-    have = (full > busy ? full : busy) * nk;
-    want = few ? 1024 : 256;
-    run = few ? 1024 : 512;
-    const bool equal = T % R == 0;
-    const int64_t expected = (equal ? R * cdiv(T / R * g, 128) : full + busy / 2) * nk;
-    const int64_t most = !equal ? kUnits * 9 / 8 : R > 1 ? kUnits - 1 : kUnits;
-    if (!few && !f32 && hd <= 128 && full * nk <= kUnits && expected <= most) {
-      p.form = kAttnPair;
-      p.block = 2 * kBlock;
-    }
-    if (few) p.block = uint32_t(64 * rows_waves(attn_hdp(hd)));
   }
-  const auto splits = [&](int64_t wgs, int64_t keys) {
-    const int64_t x = wgs / have, most = cdiv(kv_max, keys);
-    return x < most ? x : most;
-  };
-  int64_t s = splits(want, run);
-  if (p.form == kAttnRows && kv_max > 512 && splits(256, 512) > s) s = splits(256, 512);
-  if (s > TRI_MAX_KV_SPLITS) s = TRI_MAX_KV_SPLITS;
-  while (s > 1 && attn_workspace(T, nq, hd, int32_t(s)) > workspace) --s;
+  if (p.form == kAttnRows) {
+    const bool small = kv_max <= 1024;
+    while (p.heads < 2 && !small && nk % (2 << p.heads) == 0 && rpr <= 8 >> p.heads) ++p.heads;
+    const int64_t tm = 16 >> p.heads, full = cdiv(T * g, tm), groups = nk >> p.heads;
+    const int64_t tiles = T * g / tm + R;
+    have = (full > busy ? full : busy) * groups;
+    const uint64_t part = attn_workspace(T, nq, hd, 2) / 2;
+    if (!small && have < 16 * kUnits) s = int64_t((uint64_t(1) << 27) / part);
+    if (s > kQ8Splits) s = kQ8Splits;
+    if (s > int64_t(workspace / part)) s = int64_t(workspace / part);
+    four = q8_join_four(T, nq);
+    p.block = uint32_t(64 * rows_waves(attn_hdp(hd)));
+    p.step_shift = (hd > 128 ? 8 : 9) - p.heads;
+    const int64_t steps = tiles * groups * cdiv(kv_max, int64_t(1) << p.step_shift);
+    p.grid[0] = uint32_t(steps < kUnits ? steps : kUnits);
+    // steps are counted in 31 bits, for lengths up to the table's
+    while (tiles * groups * cdiv(keys_max, int64_t(1) << p.step_shift) >= int64_t(1) << 31) ++p.step_shift;
+  } else {
+    if (p.form == kAttnTile) {
+      const int64_t full = cdiv(T * g, 128);
+      have = (full > busy ? full : busy) * nk;
+      want = 256;
+      run = 512;
+      const bool equal = T % R == 0;
+      const int64_t expected = (equal ? R * cdiv(T / R * g, 128) : full + busy / 2) * nk;
+      const int64_t most = !equal ? kUnits * 9 / 8 : R > 1 ? kUnits - 1 : kUnits;
+      if (!f32 && hd <= 128 && full * nk <= kUnits && expected <= most) {
+        p.form = kAttnPair;
+        p.block = 2 * kBlock;
+      }
+      p.tiles = int32_t(T * g / 128 + R);
+    }
+    const int64_t x = want / have, most = cdiv(kv_max, run);
+    s = x < most ? x : most;
+    if (s > TRI_MAX_KV_SPLITS) s = TRI_MAX_KV_SPLITS;
+    while (s > 1 && attn_workspace(T, nq, hd, int32_t(s)) > workspace) --s;
+    four = s > kJoinWave;
+    const int64_t grid = int64_t(p.tiles) * nk * (s > 1 ? s : 1);
+    if (p.form == kAttnAny)
+      p.grid[0] = clamp_grid(cdiv(rows * (s > 1 ? s : 1), 4));
+    else if (grid * p.block < int64_t(1) << 32)   // the work-items a launch can have
+      p.grid[0] = uint32_t(grid);
+  }
   p.splits = s < 1 ? 1 : int32_t(s);
-  p.tiles = int32_t(tiles);
-  const int64_t grid = tiles * nk * p.splits;
-  if (p.form == kAttnAny)
-    p.grid[0] = clamp_grid(cdiv(rows * p.splits, 4));
-  else if (grid * p.block < int64_t(1) << 32)   // the work-items a launch can have
-    p.grid[0] = uint32_t(grid);
-  p.grid[1] = p.splits < 2 ? 0 : clamp_grid(p.splits > kJoinWave ? rows : cdiv(rows, 4));
+  p.grid[1] = p.splits < 2 ? 0 : clamp_grid(four ? rows : cdiv(rows, 4));
   return p;
 }
 
@@ -433,7 +457,7 @@ static bool paged_key_valid(const Key &k) {
     return nq == 0 && k3 == 0;
   const uint32_t form = key_attn_form(k);
   if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
-  if (k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(1) << 24))) return false;
+  if (k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(q8 ? 7 : 1) << 24))) return false;
   const bool aligned = key_flags(k) & kAlign;
   const bool matrix = q8 ? attn_q8_matrix(aligned, int32_t(hd))
                          : attn_matrix(key_dtype(k), aligned, int32_t(hd));
@@ -573,8 +597,12 @@ Plan plan_for_key(const Key &k) {
                                                                   : PA8_ANY;
       p.ksub[0] = int32_t(key_code(k));
       if (p.variant != PA8_ANY) p.ksub[0] |= attn_hdp(int32_t(key_hd(k)));
+      p.ksub[0] |= int32_t(k.k3 >> 25 & 3) << 1;
       p.n_launches = 1;
-      if (key_attn_split(k)) p.kvariant[p.n_launches++] = PA_JOIN;
+      if (key_attn_split(k)) {
+        p.ksub[1] = p.ksub[0];
+        p.kvariant[p.n_launches++] = p.variant == PA8_ROWS ? PA8_JOIN : PA_JOIN;
+      }
       return p;
     case TRI_OP_SWIGLU: {
       const Role r = sw_role(dt, key_I(k), fl, call_bytes(k) > kStreamBytes, 1);
