@@ -449,7 +449,7 @@ start:
     const int32_t r = x.r < 0 ? 0 : x.r;
     return a.table[r * a.table_rs + fast_div(uint32_t(key < 0 ? 0 : key), a.div)];
   };
-  // where the lane's key lies (the pool's first page for one that is not
+  // where the lane's key lies (in the pool's first page for one that is not
   // there), handed to the lanes that load its row; behind the head's end a lane loads
   // the first vector and clears it on the way to LDS
   const int srow = lane / S::CH, sbyte = (lane % S::CH) * 16;
@@ -698,19 +698,19 @@ start:
       const int row = threadIdx.x / PR, share = threadIdx.x % PR;
       const Request rq = nb.request(now.r);
       if (row % TM < span_of<TM>(a, rq, now.row0).rows) {
-        float top = kNegInf;
-#pragma unroll
-        for (int w = 0; w < NW; ++w)
-          if (wave_l[w][row] != 0.0f) top = fmaxf(top, wave_m[w][row]);
-        const float ts = top == kNegInf ? 0.0f : top;
-        float f[NW], sum = 0.0f;
+        // (all at once: with branches these reads took 2 us one after the other)
+        float f[NW], wl[NW], top = kNegInf, sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          f[w] = 0.0f;
-          if (wave_l[w][row] != 0.0f) {
-            f[w] = exp2_hw(wave_m[w][row] - ts);
-            sum += f[w] * wave_l[w][row];
-          }
+          wl[w] = wave_l[w][row];
+          f[w] = wl[w] != 0.0f ? wave_m[w][row] : kNegInf;
+          top = fmaxf(top, f[w]);
+        }
+        const float ts = top == kNegInf ? 0.0f : top;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          f[w] = wl[w] != 0.0f ? exp2_hw(f[w] - ts) : 0.0f;
+          sum += wl[w] != 0.0f ? f[w] * wl[w] : 0.0f;
         }
         const uint32_t x = uint32_t(now.row0 + row % TM), tok = fast_div(x, a.g_div);
         const int32_t to = rq.q0 + int32_t(tok);
