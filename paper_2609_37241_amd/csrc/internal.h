@@ -67,7 +67,8 @@ constexpr int64_t kKeysMax = kPosLimit - 4096;
 // k3: rotary dim | variant bits << 16 | scaling << 24 | original_max_pos << 32
 // k4: factor bits | low_freq_factor bits << 32;  k5: high_freq_factor bits
 // Attention: k3 = form << 16 | split << 24 (AttnForm; 1: keys split and joined).
-// 8-bit cache: k3 also has code << 32 (tri_code).
+// 8-bit cache: k3 also has code << 32 (tri_code), of attention the logarithm of the K heads of
+// a tile << 25, of the write its team << 16.
 // Fields an op does not use are zero.
 struct Key {
   uint64_t k0, k1, k2, k3, k4, k5;
@@ -218,7 +219,13 @@ AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t 
                       bool aligned, int64_t kv_max, int64_t keys_max, uint64_t workspace);
 // Whether four wavefronts join a row of PA8_ROWS' parts: rows too few to fill the units.
 inline bool q8_join_four(int64_t T, int32_t nq) { return T * nq < 1024; }
-uint32_t q8_write_grid(int64_t T, int32_t R, int32_t nk, int32_t block);
+// Lanes of a team that quantises a block's rows of a head, `vecs` vectors: 0: 16, 1: 64, 2: 256.
+inline uint32_t q8_write_team(int64_t vecs) { return vecs <= 128 ? 0 : vecs <= 512 ? 1 : 2; }
+// Heads that a team of 16 lanes takes one after the other.
+uint32_t q8_write_inner(int64_t units, int32_t nk);
+uint32_t q8_write_grid(int64_t units, int32_t nk, uint32_t team, uint32_t inner);
+// Rows that a wavefront gives back: several where there are many.
+inline int32_t q8_read_rows(int64_t T) { return T < 16384 ? 1 : 4; }
 uint32_t q8_read_grid(int64_t T);
 // n / d by multiplication (kernargs.h).
 FastDiv fast_div_of(uint32_t d);

@@ -228,7 +228,10 @@ struct Q8RowsArgs {
   int32_t page, nk, hd, block;
   FastDiv div;            // by page
   FastDiv block_div;      // by block
-  FastDiv nk_div;         // by nk
+  FastDiv per_div;        // by per
+  int32_t per;            // work-items of a row of a head
+  int32_t units, by_row;  // Q8W_*: how blocks are numbered; Q8R_*: rows of a wavefront
+  uint32_t inner;         // Q8W_*: heads that a team takes one after the other
 };
 
 constexpr int32_t kQ8Splits = 128;   // parts of a tile of few rows over an 8-bit cache, at most
@@ -294,7 +297,7 @@ static_assert(sizeof(KvWriteArgs) == 152 && __builtin_offsetof(KvWriteArgs, row_
               "KvWriteArgs layout");
 static_assert(sizeof(PagedArgs) == 216 && __builtin_offsetof(PagedArgs, div) == 200,
               "PagedArgs layout");
-static_assert(sizeof(Q8RowsArgs) == 248 && __builtin_offsetof(Q8RowsArgs, T) == 192,
+static_assert(sizeof(Q8RowsArgs) == 264 && __builtin_offsetof(Q8RowsArgs, T) == 192,
               "Q8RowsArgs layout");
 static_assert(sizeof(PagedQ8Args) == 312 && __builtin_offsetof(PagedQ8Args, scale) == 280,
               "PagedQ8Args layout");

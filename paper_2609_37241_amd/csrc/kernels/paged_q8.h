@@ -58,30 +58,33 @@ __device__ inline Rounder rounder(float s) {
   return {s, 1.0f / s, (__float_as_uint(s) & 0x7FFFFFu) == 0};
 }
 
-// The whole number nearest to x / s, ties to even, as the low byte of the result:
-// 1.5 2^23 added, a float32's last place is 1, so the fused product is rounded to a
-// whole number n, off from the quotient's by one at most, where that is within 2^-16 of
-// the middle of two. What n leaves of x, x - n s, is exact (a multiple of the
+// Four codes; all 0 with a scale of NaN. Whole numbers are the nearest to x / s, ties to even:
+// 1.5 2^23 added, a float32's last place is 1, so the fused product is rounded to a whole
+// number n, whose low byte is the sum's, off from the quotient's by one at most, where that is
+// within 2^-16 of the middle of two. What n leaves of x, x - n s, is exact (a multiple of the
 // smaller of both operands' last places, and no longer than s), so its distance to
-// s / 2 says which of the two is nearer, and a tie is one.
-__device__ inline uint32_t round_i8(float x, const Rounder &r) {
-  constexpr float kMagic = 12582912.0f;
-  float t = fmaf(x, r.inv, kMagic);
-  const float n = t - kMagic, left = fmaf(-n, r.s, x), far = fabsf(left), h = 0.5f * r.s;
-  const bool odd = __float_as_uint(t) & 1u;
-  if (far > h || (far == h && odd)) t += left > 0.0f ? 1.0f : -1.0f;
-  return __float_as_uint(t) & 0xFFu;
-}
-
-// Four codes; all 0 with a scale of NaN.
+// s / 2 says which of the two is nearer, and a tie is one; few are that near.
 template <int CT>
 __device__ inline uint32_t to_codes4(const float *x, const Rounder &r) {
   if (r.s != r.s) return 0;
   if constexpr (CT == kInt8) {
-    uint32_t c = 0;
+    constexpr float kMagic = 12582912.0f;
+    float t[4], left[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c |= round_i8(x[i], r) << (8 * i);
-    return c;
+    for (int i = 0; i < 4; ++i) {
+      t[i] = fmaf(x[i], r.inv, kMagic);
+      left[i] = fmaf(-(t[i] - kMagic), r.s, x[i]);
+    }
+    const float h = 0.5f * r.s;
+    if (fmaxf(fmaxf(fabsf(left[0]), fabsf(left[1])), fmaxf(fabsf(left[2]), fabsf(left[3]))) >= h) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float far = fabsf(left[i]);
+        if (far > h || (far == h && (__float_as_uint(t[i]) & 1u))) t[i] += left[i] > 0.0f ? 1.0f : -1.0f;
+      }
+    }
+    return __builtin_amdgcn_perm(__float_as_uint(t[1]), __float_as_uint(t[0]), 0x0C0C0400) |
+           __builtin_amdgcn_perm(__float_as_uint(t[3]), __float_as_uint(t[2]), 0x04000C0C);
   } else {
     float y[4];
 #pragma unroll
@@ -91,26 +94,41 @@ __device__ inline uint32_t to_codes4(const float *x, const Rounder &r) {
   }
 }
 
-// Codes of scale `was` as codes of `now` > was: the nearest to c was / now. c was is
-// exact in 64 bits, and so is which whole number (int8) their quotient is nearest to: a
-// quotient of 31 by 24 bits is a tie or more than 2^-56 of it off.
+// Codes of scale `was` as codes of `now` > was: the nearest to c was / now. A float32 product
+// with the quotient is off by 2^-15 at most, so it tells which whole number is nearest, but within
+// 2^-12 of the middle of two; e4m3's powers of two have exact products. Else 64 bits: c was is
+// exact in them, and a quotient of 31 by 24 bits is a tie or more than 2^-56 of it off.
 template <int CT>
 __device__ inline uint32_t recode4(uint32_t c, float was, float now) {
-  float f[4];
+  float f[4], y[4];
   codes4<CT>(c, f);
-  uint32_t out = 0;
-  if constexpr (CT == kInt8) {
+  const float ratio = was / now;
+  bool plain = CT == kInt8 || ((__float_as_uint(was) | __float_as_uint(now)) & 0x7FFFFFu) == 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      out |= (uint32_t(int32_t(rint(double(f[i]) * double(was) / double(now)))) & 0xFFu) << (8 * i);
-  } else {
-    float y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = float(double(f[i]) * double(was) / double(now));
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    out = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true));
+  for (int i = 0; i < 4; ++i) {
+    y[i] = f[i] * ratio;
+    if constexpr (CT == kInt8) {
+      const float n = rintf(y[i]);
+      plain = plain && fabsf(y[i] - n) < 0.5f - 0x1p-12f;
+      y[i] = n;
+    }
   }
-  return out;
+  if (!plain) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const double q = double(f[i]) * double(was) / double(now);
+      y[i] = CT == kInt8 ? float(rint(q)) : float(q);
+    }
+  }
+  if constexpr (CT == kInt8) {
+    uint32_t out = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out |= (uint32_t(int32_t(y[i])) & 0xFFu) << (8 * i);
+    return out;
+  } else {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true));
+  }
 }
 
 // Where a block's scale lies: page, block of the page, head.

@@ -7,197 +7,306 @@
 namespace tri {
 using namespace dev;
 
-// ---- Q8W_* ------------------------------------------------------------------------------------
-// A wavefront quantises the tokens that a call adds to one block, of one head of K or V:
-// it takes the largest magnitude, makes the scale, and reads the rows again for their
-// codes. Blocks are numbered through the requests without knowing their lengths on the
-// host: those of r start at floor(q_start[r] / B) + 2 r, which leaves each request
-// room for the floor((n - 2) / B) + 2 blocks that n tokens can touch. The
-// wavefront has its block's scale to itself: no atomics, the same bits every time.
 namespace {
 
-// The block that wavefront `unit` of the numbering writes.
-struct Touched {
-  int64_t id;              // page, -1: nothing to do
-  uint32_t block;          // of the page
-  int32_t slot, held;      // first slot of the block; tokens that it holds already
-  int32_t first, last;     // rows of k and v
+// The requests of a call: up to 64 held by a lane each, looked up all at once.
+struct Requests {
+  int32_t q0, q1, kv;
 };
-
-__device__ inline Touched touched(const Q8RowsArgs &a, int64_t unit) {
-  Touched t;
-  t.id = -1;
-  const int32_t r = __builtin_amdgcn_readfirstlane(last_request(a.R, [&](int32_t x) {
-    return int64_t(fast_div(uint32_t(clamp_i32(a.q_start[x], 0, a.T)), a.block_div)) + 2 * int64_t(x) <=
-           unit;
-  }));
-  if (r < 0) return t;
-  const Request rq = request_of(a, r);
-  const int32_t n = rq.q1 - rq.q0, base = rq.kv - n, lo = base < 0 ? 0 : base;
-  if (n <= 0) return t;
-  const int64_t j = unit - (int64_t(fast_div(uint32_t(rq.q0), a.block_div)) + 2 * int64_t(r));
-  const int64_t begin = (int64_t(fast_div(uint32_t(lo), a.block_div)) + j) * a.block;
-  if (begin >= rq.kv) return t;
-  const uint32_t col = fast_div(uint32_t(begin), a.div);
-  const int32_t id = a.table[r * a.table_rs + col];
-  if (uint32_t(id) >= uint32_t(a.n_pages)) return t;
-  t.slot = int32_t(uint32_t(begin) - col * uint32_t(a.page));
-  t.block = fast_div(uint32_t(t.slot), a.block_div);
-  const int32_t from = begin < lo ? lo : int32_t(begin);
-  const int32_t to = rq.kv - begin > a.block ? int32_t(begin) + a.block : rq.kv;
-  t.held = from - int32_t(begin);
-  t.first = from - base + rq.q0;
-  t.last = to - base + rq.q0;
-  t.id = id;
-  return t;
+__device__ inline Requests requests(const Q8RowsArgs &a) {
+  const int lane = threadIdx.x & 63, x = lane < a.R ? lane : 0;
+  if (a.R > 64) return {0, 0, 0};
+  return {a.q_start[x], a.q_start[x + 1], a.kv_len[x]};
 }
 
-// Four elements of a row, or one.
-template <int DT, bool VEC>
-__device__ inline void load4(const char *p, float *x) {
-  if constexpr (!VEC) {
-    x[0] = Elt<DT>::ld(p, 0);
-    x[1] = x[2] = x[3] = 0.0f;
-  } else if constexpr (DT == kF32) {
-    Elt<kF32>::unpack(*reinterpret_cast<const u32x4 *>(p), x);
+// The last request r with first(r, q_start[r] in [0, T]) at or before what is looked for (first()
+// tells), -1 if none.
+template <class F>
+__device__ inline int32_t find_request(const Q8RowsArgs &a, const Requests &h, Request *rq, F &&first) {
+  const int lane = threadIdx.x & 63;
+  if (a.R <= 64) {
+    const uint64_t hit = __ballot(lane < a.R && first(lane, clamp_i32(h.q0, 0, a.T)));
+    if (!hit) return -1;
+    const int r = 63 - __builtin_clzll(hit);
+    *rq = clamped(a, __builtin_amdgcn_readlane(h.q0, r), __builtin_amdgcn_readlane(h.q1, r),
+                  __builtin_amdgcn_readlane(h.kv, r));
+    return r;
+  }
+  const int32_t r = __builtin_amdgcn_readfirstlane(
+      last_request(a.R, [&](int32_t x) { return first(x, clamp_i32(a.q_start[x], 0, a.T)); }));
+  if (r >= 0) *rq = request_of(a, r);
+  return r;
+}
+
+// A vector of a row (an element: in its first place, as float32), and its N elements.
+template <int DT, int N>
+__device__ inline u32x4 load_row(const char *p) {
+  if constexpr (N == 1)
+    return u32x4{__float_as_uint(Elt<DT>::ld(p, 0)), 0, 0, 0};
+  else
+    return *reinterpret_cast<const u32x4 *>(p);
+}
+template <int DT, int N>
+__device__ inline void elements(const u32x4 &v, float *x) {
+  if constexpr (N == 1)
+    x[0] = __uint_as_float(v[0]);
+  else
+    Elt<DT>::unpack(v, x);
+}
+
+// N codes as they lie in a register (or two).
+
+template <int N>
+struct CodesOf {
+  uint32_t w[(N + 3) / 4];
+};
+template <int N>
+__device__ inline CodesOf<N> load_codes(const char *p) {
+  CodesOf<N> c;
+  if constexpr (N == 1) {
+    c.w[0] = *reinterpret_cast<const uint8_t *>(p);
+  } else if constexpr (N == 4) {
+    c.w[0] = *reinterpret_cast<const uint32_t *>(p);
   } else {
     const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x[2 * i] = __uint_as_float(v[i] << 16);
-      x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
-    }
+    c.w[0] = v[0];
+    c.w[1] = v[1];
   }
+  return c;
 }
-
-template <bool VEC>
-__device__ inline uint32_t load_codes(const char *p) {
-  if constexpr (VEC)
-    return *reinterpret_cast<const uint32_t *>(p);
+template <int N>
+__device__ inline void store_codes(char *p, const CodesOf<N> &c) {
+  if constexpr (N == 1)
+    *reinterpret_cast<uint8_t *>(p) = uint8_t(c.w[0]);
+  else if constexpr (N == 4)
+    *reinterpret_cast<uint32_t *>(p) = c.w[0];
   else
-    return *reinterpret_cast<const uint8_t *>(p);
-}
-
-template <bool VEC>
-__device__ inline void store_codes(char *p, uint32_t c) {
-  if constexpr (VEC)
-    *reinterpret_cast<uint32_t *>(p) = c;
-  else
-    *reinterpret_cast<uint8_t *>(p) = uint8_t(c);
+    *reinterpret_cast<u32x2 *>(p) = u32x2{c.w[0], c.w[1]};
 }
 
 }  // namespace
 
-template <int DT, int CT, bool VEC>
-__global__ __launch_bounds__(256) void k_q8_write(Q8RowsArgs a) {
-  constexpr int N = VEC ? 4 : 1;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t parts = 2 * uint32_t(a.nk);
-  const int64_t items = (int64_t(fast_div(uint32_t(a.T), a.block_div)) + 2 * int64_t(a.R)) * parts;
-  const int per = a.hd / N;   // work-items of a row
-  for (int64_t it = int64_t(blockIdx.x) * 4 + wave; it < items; it += int64_t(gridDim.x) * 4) {
-    const int64_t unit = it / parts;
-    const uint32_t part = uint32_t(it - unit * parts);
-    const bool is_v = part >= uint32_t(a.nk);
-    const uint32_t h = is_v ? part - uint32_t(a.nk) : part;
-    const Touched t = touched(a, unit);
-    if (t.id < 0) continue;
-    const int64_t ts = is_v ? a.v_ts : a.k_ts;
-    const char *x = static_cast<const char *>(is_v ? a.v : a.k) +
-                    (t.first * ts + int64_t(h) * a.hd) * Elt<DT>::ES;
-    const PagedView &view = is_v ? a.cv : a.ck;
-    char *c = static_cast<char *>(view.p) + t.id * view.ps + int64_t(t.slot) * view.ss +
-              int64_t(h) * view.hs;
-    float *scale = scale_at(is_v ? a.sv : a.sk, t.id, t.block, h);
-    const float was = *scale;
-    // the largest magnitude: as whole numbers, so that infinities and NaN are above all
-    const int n = (t.last - t.first) * per;
-    uint32_t most = 0;
-    for (int i = lane; i < n; i += 64) {
-      const int row = i / per, e = (i - row * per) * N;
-      float f[4];
-      load4<DT, VEC>(x + (row * ts + e) * Elt<DT>::ES, f);
+// ---- Q8W_* ------------------------------------------------------------------------------------
+// A team of L lanes (16, a wavefront, or a workgroup) quantises the tokens that a call adds to one
+// block, of one head of K or V: it holds them, 8 vectors a lane (an element a lane, Q8W_ANY),
+// takes the largest magnitude, makes the scale and stores the codes; what it cannot hold
+// it reads twice. A block belongs to one team alone: no atomics, the same bits every
+// time. Blocks are numbered through the requests without knowing their lengths on the
+// host: n tokens touch at most floor((n - 2) / B) + 2 blocks, and at most n, so those of r
+// start at floor(q_start[r] / B) + 2 r, or (a.by_row, the fewer) at q_start[r].
+template <int DT, int CT, bool VEC, int L>
+__global__ __launch_bounds__(256, L == 16 ? 4 : 5) void k_q8_write(Q8RowsArgs a) {
+  constexpr int N = VEC ? Elt<DT>::V : 1, HOLD = 8;
+  __shared__ uint32_t team_most[L == 256 ? 4 : 1];
+  const int tid = threadIdx.x % L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Requests held = requests(a);
+  // teams of a wavefront take neighbouring heads of one block, a.inner times (what finds the
+  // block costs as much as a few vectors)
+  constexpr int TW = L < 64 ? 64 / L : 1;
+  const uint32_t inner = L == 16 ? a.inner : 1;
+  const uint32_t parts = 2 * uint32_t(a.nk), groups = (parts + TW * inner - 1) / (TW * inner);
+  const int64_t items = int64_t(a.units) * groups;
+  const int64_t first = L == 256 ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + wave;
+  const int64_t stride = int64_t(gridDim.x) * (L == 256 ? 1 : 4);
+  for (int64_t it = first; it < items; it += stride) {
+    const uint32_t unit = uint32_t(it / groups);
+    const uint32_t part0 = uint32_t(it - int64_t(unit) * groups) * TW * inner;
+    Request rq;
+    const int32_t r = find_request(a, held, &rq, [&](int32_t x, int32_t q0) {
+      return a.by_row ? uint32_t(q0) <= unit
+                      : int64_t(fast_div(uint32_t(q0), a.block_div)) + 2 * int64_t(x) <= int64_t(unit);
+    });
+    if (r < 0) continue;
+    const int32_t n = rq.q1 - rq.q0, base = rq.kv - n, lo = base < 0 ? 0 : base;
+    if (n <= 0) continue;
+    const int64_t j = a.by_row ? int64_t(unit) - rq.q0
+                               : unit - (int64_t(fast_div(uint32_t(rq.q0), a.block_div)) + 2 * int64_t(r));
+    const int64_t begin = (int64_t(fast_div(uint32_t(lo), a.block_div)) + j) * a.block;
+    if (begin >= rq.kv) continue;
+    const uint32_t col = fast_div(uint32_t(begin), a.div);
+    const int32_t id = a.table[r * a.table_rs + col];
+    // tokens that the block holds, and the rows that it gets
+    const int32_t from = begin < lo ? lo : int32_t(begin);
+    const int32_t to = rq.kv - begin > a.block ? int32_t(begin) + a.block : rq.kv;
+    const int32_t old = from - int32_t(begin), row0 = from - base + rq.q0;
+    const int32_t items_new = (to - from) * a.per;   // work-items
+    const uint32_t slot = uint32_t(begin) - col * uint32_t(a.page);
+    const bool there = uint32_t(id) < uint32_t(a.n_pages);
+    if (!there) continue;
+    for (uint32_t in = 0; in < inner; ++in) {
+      uint32_t part = part0 + in * TW;
+      if (part >= parts) break;
+      if constexpr (TW > 1) part += (threadIdx.x & 63) / L;
+      const bool active = part < parts;
+      const bool is_v = part >= uint32_t(a.nk);
+      const uint32_t h = is_v ? part - uint32_t(a.nk) : part;
+      const int64_t ts = is_v ? a.v_ts : a.k_ts;
+      const char *x = static_cast<const char *>(is_v ? a.v : a.k) +
+                      (row0 * ts + int64_t(h) * a.hd) * Elt<DT>::ES;
+      const auto row_of = [&](int i, int *e) {
+        asm volatile("" : "+v"(i));   // (or every place lives on from the load to the store)
+        const int row = int(fast_div(uint32_t(i), a.per_div));
+        *e = (i - row * a.per) * N;
+        return row;
+      };
+      // the largest magnitude: as whole numbers, so that infinities and NaN are above all
+      u32x4 f[HOLD];
+      uint32_t most = 0;
+      const auto take = [&](const u32x4 &v) {
+        float y[N];
+        elements<DT, N>(v, y);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t b = __float_as_uint(f[j]) & 0x7FFFFFFFu;
+        for (int c = 0; c < N; ++c) {
+          const uint32_t b = __float_as_uint(y[c]) & 0x7FFFFFFFu;
+          most = b > most ? b : most;
+        }
+      };
+      const auto load = [&](int i) {
+        int e;
+        const int row = row_of(i, &e);
+        return load_row<DT, N>(x + (row * ts + e) * Elt<DT>::ES);
+      };
+#pragma unroll
+      for (int k = 0; k < HOLD; ++k) {
+        f[k] = u32x4{0, 0, 0, 0};
+        if (L * k >= items_new) continue;   // (for all lanes)
+        if (active && tid + L * k < items_new) f[k] = load(tid + L * k);
+      }
+      const PagedView &view = is_v ? a.cv : a.ck;
+      char *c = static_cast<char *>(view.p) + id * view.ps + int64_t(slot) * view.ss +
+                int64_t(h) * view.hs;
+      float *scale = scale_at(is_v ? a.sv : a.sk, id, fast_div(slot, a.block_div), h);
+      const float was = active ? *scale : 0.0f;
+#pragma unroll
+      for (int k = 0; k < HOLD; ++k)
+        if (L * k < items_new) take(f[k]);
+      for (int i = tid + L * HOLD; active && i < items_new; i += L) take(load(i));
+#pragma unroll
+      for (int d = (L < 64 ? L : 64) / 2; d; d >>= 1) {
+        const uint32_t b = __shfl_xor(most, d);
         most = b > most ? b : most;
       }
-    }
+      if constexpr (L == 256) {
+        __syncthreads();   // (the last item's are read)
+        if ((threadIdx.x & 63) == 0) team_most[wave] = most;
+        __syncthreads();
 #pragma unroll
-    for (int d = 32; d; d >>= 1) {
-      const uint32_t b = __shfl_xor(most, d);
-      most = b > most ? b : most;
-    }
-    const float need = scale_for<CT>(most);
-    // (a scale of NaN stays one)
-    const float now = t.held == 0 || need != need || need > was ? need : was;
-    if (t.held > 0 && now > was) {
-      for (int i = lane; i < t.held * per; i += 64) {
-        const int row = i / per, e = (i - row * per) * N;
-        char *p = c + row * view.ss + e;
-        store_codes<VEC>(p, recode4<CT>(load_codes<VEC>(p), was, now));
+        for (int w = 0; w < 4; ++w) most = team_most[w] > most ? team_most[w] : most;
       }
-    }
-    if (lane == 0) *scale = now;
-    const Rounder r = rounder(now);
-    for (int i = lane; i < n; i += 64) {
-      const int row = i / per, e = (i - row * per) * N;
-      float f[4];
-      load4<DT, VEC>(x + (row * ts + e) * Elt<DT>::ES, f);
-      store_codes<VEC>(c + (t.held + row) * view.ss + e, to_codes4<CT>(f, r));
+      if (!active) continue;
+      // (else the elements live on as float32, in twice the registers)
+#pragma unroll
+      for (int k = 0; k < HOLD; ++k) asm volatile("" : "+v"(f[k]));
+      const float need = scale_for<CT>(most);
+      // (a scale of NaN stays one)
+      const float now = old == 0 || need != need || need > was ? need : was;
+      if (old > 0 && now > was) {
+        const int last = old * a.per;
+#pragma unroll 1
+        for (int i0 = tid; i0 < last; i0 += 2 * L) {
+          char *p[2];
+          CodesOf<N> y[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            int e;
+            const int i = i0 + L * u < last ? i0 + L * u : i0, row = row_of(i, &e);
+            p[u] = c + row * view.ss + e;
+            y[u] = load_codes<N>(p[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if (i0 + L * u >= last) break;
+#pragma unroll
+            for (uint32_t &w : y[u].w) w = recode4<CT>(w, was, now);
+            store_codes<N>(p[u], y[u]);
+          }
+        }
+      }
+      if (tid == 0) *scale = now;
+      const Rounder rd = rounder(now);
+      const auto put = [&](int i, const u32x4 &v) {
+        int e;
+        const int row = row_of(i, &e);
+        float y[N];
+        elements<DT, N>(v, y);
+        CodesOf<N> z;
+#pragma unroll
+        for (int k = 0; k < (N + 3) / 4; ++k) {
+          float four[4];
+#pragma unroll
+          for (int m = 0; m < 4; ++m) four[m] = 4 * k + m < N ? y[4 * k + m] : 0.0f;
+          z.w[k] = to_codes4<CT>(four, rd);
+        }
+        store_codes<N>(c + (old + row) * view.ss + e, z);
+      };
+#pragma unroll
+      for (int k = 0; k < HOLD; ++k)
+        if (L * k < items_new && tid + L * k < items_new) put(tid + L * k, f[k]);
+      for (int i = tid + L * HOLD; i < items_new; i += L) put(i, load(i));
     }
   }
 }
 
 // ---- Q8R_* ------------------------------------------------------------------------------------
-// A wavefront gives one row of K and V back, four elements a work-item.
+// A wavefront gives a.units neighbouring rows of K and V back, a vector a work-item (an
+// element, Q8R_ANY), four of them in flight.
 template <int DT, int CT, bool VEC>
 __global__ __launch_bounds__(256) void k_q8_read(Q8RowsArgs a) {
-  constexpr int N = VEC ? 4 : 1;
+  constexpr int N = VEC ? Elt<DT>::V : 1, U = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int64_t row = int64_t(blockIdx.x) * 4 + wave; row < a.T; row += int64_t(gridDim.x) * 4) {
-    const int32_t r = __builtin_amdgcn_readfirstlane(
-        last_request(a.R, [&](int32_t x) { return a.q_start[x] <= row; }));
-    if (r < 0) continue;
-    const Request rq = request_of(a, r);
-    if (row < rq.q0 || row >= rq.q1) continue;
-    const int32_t p = rq.kv - (rq.q1 - int32_t(row));
-    int64_t id = -1;
-    uint32_t slot = 0;
-    if (p >= 0) {
-      const uint32_t col = fast_div(uint32_t(p), a.div);
-      const int32_t x = a.table[r * a.table_rs + col];
-      id = uint32_t(x) < uint32_t(a.n_pages) ? x : -1;
-      slot = uint32_t(p) - col * uint32_t(a.page);
-    }
-    const uint32_t block = fast_div(slot, a.block_div);
-    const int per = a.hd / N, half = a.nk * per;
-    for (int i = lane; i < 2 * half; i += 64) {
-      const bool is_v = i >= half;
-      const int j = is_v ? i - half : i, h = j / per, e = (j - h * per) * N;
-      const PagedView &view = is_v ? a.cv : a.ck;
-      float f[4] = {};
-      if (id >= 0) {
-        const char *c = static_cast<const char *>(view.p) + id * view.ps + int64_t(slot) * view.ss +
-                        int64_t(h) * view.hs + e;
-        const float s = *scale_at(is_v ? a.sv : a.sk, id, block, uint32_t(h));
-        if constexpr (VEC) {
-          codes4<CT>(load_codes<VEC>(c), f);
+  const Requests held = requests(a);
+  const int half = a.nk * a.per;
+  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + wave) * a.units; row0 < a.T;
+       row0 += int64_t(gridDim.x) * 4 * a.units) {
+    Request rq = {0, 0, 0};
+    int32_t r = -1;
+    for (int32_t row = int32_t(row0); row < row0 + a.units && row < a.T; ++row) {
+      if (r < 0 || row >= rq.q1)
+        r = find_request(a, held, &rq, [&](int32_t, int32_t q0) { return q0 <= row; });
+      if (r < 0 || row < rq.q0 || row >= rq.q1) continue;
+      const int32_t p = rq.kv - (rq.q1 - row);
+      int64_t id = -1;
+      uint32_t slot = 0;
+      if (p >= 0) {
+        const uint32_t col = fast_div(uint32_t(p), a.div);
+        const int32_t x = a.table[r * a.table_rs + col];
+        id = uint32_t(x) < uint32_t(a.n_pages) ? x : -1;
+        slot = uint32_t(p) - col * uint32_t(a.page);
+      }
+      const uint32_t block = fast_div(slot, a.block_div);
+      const int64_t at = id < 0 ? 0 : id;
+      for (int i0 = lane; i0 < 2 * half; i0 += 64 * U) {
+        CodesOf<N> c[U];
+        float s[U];
+        int64_t to[U];
+        bool is_v[U];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) f[k] *= s;
-        } else {
-          f[0] = code1<CT>(uint8_t(load_codes<VEC>(c))) * s;
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + 64 * u < 2 * half ? i0 + 64 * u : i0;
+          is_v[u] = i >= half;
+          const int j = is_v[u] ? i - half : i, h = int(fast_div(uint32_t(j), a.per_div));
+          const int e = (j - h * a.per) * N;
+          const PagedView &view = is_v[u] ? a.cv : a.ck;
+          c[u] = load_codes<N>(static_cast<const char *>(view.p) + at * view.ps +
+                               int64_t(slot) * view.ss + int64_t(h) * view.hs + e);
+          s[u] = *scale_at(is_v[u] ? a.sv : a.sk, at, block, uint32_t(h));
+          to[u] = row * (is_v[u] ? a.v_ts : a.k_ts) + int64_t(h) * a.hd + e;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (i0 + 64 * u >= 2 * half) break;
+          float f[(N + 3) / 4 * 4];
+#pragma unroll
+          for (int k = 0; k < (N + 3) / 4; ++k) codes4<CT>(c[u].w[k], f + 4 * k);
+#pragma unroll
+          for (float &y : f) y = id < 0 ? 0.0f : y * s[u];
+          char *o = static_cast<char *>(is_v[u] ? a.v : a.k) + to[u] * Elt<DT>::ES;
+          if constexpr (VEC)
+            *reinterpret_cast<u32x4 *>(o) = Elt<DT>::pack(f);
+          else
+            Elt<DT>::st(o, 0, f[0]);
         }
       }
-      char *o = static_cast<char *>(is_v ? a.v : a.k) +
-                (row * (is_v ? a.v_ts : a.k_ts) + int64_t(h) * a.hd + e) * Elt<DT>::ES;
-      if constexpr (!VEC)
-        Elt<DT>::st(o, 0, f[0]);
-      else if constexpr (DT == kF32)
-        *reinterpret_cast<u32x4 *>(o) = Elt<kF32>::pack(f);
-      else
-        *reinterpret_cast<u32x2 *>(o) =
-            u32x2{Elt<kBF16>::pack2(f[0], f[1]), Elt<kBF16>::pack2(f[2], f[3])};
     }
   }
 }
@@ -331,10 +440,13 @@ const void *sym(F *f) {
 }
 
 template <int DT, int CT>
-const void *rows_kernel(int32_t variant) {
+const void *rows_kernel(int32_t variant, int32_t team) {
   switch (variant) {
-    case Q8W_ANY: return sym(&k_q8_write<DT, CT, false>);
-    case Q8W_VEC: return sym(&k_q8_write<DT, CT, true>);
+    case Q8W_ANY: return sym(&k_q8_write<DT, CT, false, 64>);
+    case Q8W_VEC:
+      return team == 2   ? sym(&k_q8_write<DT, CT, true, 256>)
+             : team == 1 ? sym(&k_q8_write<DT, CT, true, 64>)
+                         : sym(&k_q8_write<DT, CT, true, 16>);
     case Q8R_ANY: return sym(&k_q8_read<DT, CT, false>);
     case Q8R_VEC: return sym(&k_q8_read<DT, CT, true>);
     case PA8_ANY: return sym(&k_pa8_any<DT, CT>);
@@ -353,7 +465,8 @@ static const void *join_kernel(int32_t heads) {
 }
 
 // sub: the code (tri_code) in bit 0; for the matrix forms the head size held from bit 6 on,
-// for few rows the logarithm of the K heads of a tile in bits 1 and 2.
+// for few rows the logarithm of the K heads of a tile in bits 1 and 2; for the write there
+// the lanes of a team, 16, 64 or 256.
 const void *paged_q8_kernel(int32_t variant, uint32_t dtype, int32_t sub) {
   const bool e4m3 = (sub & 1) == TRI_E4M3;
   const int32_t code = sub & 1, hdp = sub & ~63;
@@ -365,8 +478,8 @@ const void *paged_q8_kernel(int32_t variant, uint32_t dtype, int32_t sub) {
   if (variant == PA8_TILE || variant == PA8_PAIR)
     return attn_q8_tile_bf16(variant == PA8_PAIR, code, hdp);
   if (dtype == TRI_F32)
-    return e4m3 ? rows_kernel<kF32, kE4M3>(variant) : rows_kernel<kF32, kInt8>(variant);
-  return e4m3 ? rows_kernel<kBF16, kE4M3>(variant) : rows_kernel<kBF16, kInt8>(variant);
+    return e4m3 ? rows_kernel<kF32, kE4M3>(variant, sub >> 1) : rows_kernel<kF32, kInt8>(variant, sub >> 1);
+  return e4m3 ? rows_kernel<kBF16, kE4M3>(variant, sub >> 1) : rows_kernel<kBF16, kInt8>(variant, sub >> 1);
 }
 
 }  // namespace tri

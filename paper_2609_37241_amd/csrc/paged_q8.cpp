@@ -42,17 +42,28 @@ tri_status rows_q8(tri_cache *c, uint32_t op, const tri_kv_rows_args *p, void *s
   const bool aligned = !(rows & 15u) && !(kv_bits(a.kv, 1) & (16 / es - 1));
   Key k = make_key(op, uint32_t(a.dtype), a.T, aligned ? kAlign : 0u, 0, 0, 0, uint64_t(a.kv.hd), 0,
                    uint64_t(a.kv.nk));
-  k.k3 = key_code(a.q8);
   const tri_kv_q8 &q = a.q8;
+  const bool vec = aligned && a.kv.hd % vec_elems(uint32_t(a.dtype)) == 0;
+  const int32_t per = a.kv.hd / int32_t(vec ? vec_elems(uint32_t(a.dtype)) : 1);
+  // blocks that the rows can touch, by the two ways to number them
+  const int64_t by_block = a.T / q.block + 2 * int64_t(a.R);
+  const bool by_row = a.T <= by_block;
+  const int64_t units = by_row ? a.T : by_block;
+  const bool write = op == TRI_OP_KV_WRITE_Q8;
+  // the rows that a block gets, were the requests equal
+  const int64_t rows_each = (a.T + a.R - 1) / a.R < q.block ? (a.T + a.R - 1) / a.R : q.block;
+  const uint32_t team = write && vec ? q8_write_team(rows_each * per) : 1;
+  const uint32_t inner = write && team == 0 ? q8_write_inner(units, a.kv.nk) : 1;
+  k.k3 = key_code(q) | (write && vec ? uint64_t(team) << 16 : 0);
   const Q8RowsArgs args{a.k, a.v, {a.kv.k, a.kv.k_ps, a.kv.k_ss, a.kv.k_hs},
                         {a.kv.v, a.kv.v_ps, a.kv.v_ss, a.kv.v_hs},
                         {q.k_scale, q.k_ps, q.k_bs, q.k_hs}, {q.v_scale, q.v_ps, q.v_bs, q.v_hs},
                         a.table, a.kv_len, a.q_start, a.k_ts, a.v_ts, a.table_rs, int32_t(a.T), a.R,
                         a.cols, a.kv.n_pages, a.kv.page, a.kv.nk, a.kv.hd, q.block,
                         fast_div_of(uint32_t(a.kv.page)), fast_div_of(uint32_t(q.block)),
-                        fast_div_of(uint32_t(a.kv.nk))};
-  const uint32_t grid = op == TRI_OP_KV_WRITE_Q8 ? q8_write_grid(a.T, a.R, a.kv.nk, q.block)
-                                                 : q8_read_grid(a.T);
+                        fast_div_of(uint32_t(per)), per,
+                        write ? int32_t(units) : q8_read_rows(a.T), by_row, inner};
+  const uint32_t grid = write ? q8_write_grid(units, a.kv.nk, team, inner) : q8_read_grid(a.T);
   return run_paged(c, op, k, a.T, &grid, 1, kBlock, &args, sizeof args, stream);
 }
 

@@ -315,14 +315,20 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
 }
 
 // ---- the paged KV cache in 8 bits ----
-// A wavefront for each block of tokens that a request's rows can touch (numbered as
-// q8_write's kernel says, T / block + 2 R of them), head, and K or V.
-uint32_t q8_write_grid(int64_t T, int32_t R, int32_t nk, int32_t block) {
-  return clamp_grid(cdiv((T / block + 2 * int64_t(R)) * nk * 2, 4));
+// As many as leave two wavefronts a SIMD unit, at most all.
+uint32_t q8_write_inner(int64_t units, int32_t nk) {
+  const int64_t groups = cdiv(2 * int64_t(nk), 4), x = units * groups / (8 * kUnits);
+  return uint32_t(x < 1 ? 1 : x < groups ? x : groups);
 }
 
-// A wavefront a row.
-uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4)); }
+// A team for each block of tokens that the rows can touch, `inner` heads, and K or V.
+uint32_t q8_write_grid(int64_t units, int32_t nk, uint32_t team, uint32_t inner) {
+  const int64_t parts = 2 * int64_t(nk);
+  if (team == 0) return clamp_grid(cdiv(units * cdiv(parts, 4 * int64_t(inner)), 4));
+  return clamp_grid(team == 2 ? units * parts : cdiv(units * parts, 4));
+}
+
+uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4 * int64_t(q8_read_rows(T)))); }
 
 // Forms as attn_plan, but that float32 queries take tiles of many rows as bf16 ones do (three
 // products for one, not sixteen). Splits of those as attn_plan, too.
@@ -453,8 +459,10 @@ static bool paged_key_valid(const Key &k) {
   const bool q8 = is_q8_op(op);
   if (q8 && key_code(k) > TRI_E4M3) return false;
   const uint64_t k3 = q8 ? k.k3 & 0xFFFFFFFFu : k.k3;
-  if (op == TRI_OP_KV_WRITE || op == TRI_OP_KV_WRITE_Q8 || op == TRI_OP_KV_READ_Q8)
-    return nq == 0 && k3 == 0;
+  const bool vec = (key_flags(k) & kAlign) && hd % vec_elems(key_dtype(k)) == 0;
+  if (op == TRI_OP_KV_WRITE_Q8)
+    return nq == 0 && (k3 & 0xFFFF) == 0 && k3 >> 16 <= (vec ? 2u : 0u);
+  if (op == TRI_OP_KV_WRITE || op == TRI_OP_KV_READ_Q8) return nq == 0 && k3 == 0;
   const uint32_t form = key_attn_form(k);
   if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
   if (k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(q8 ? 7 : 1) << 24))) return false;
@@ -586,7 +594,7 @@ Plan plan_for_key(const Key &k) {
       const bool vec = (fl & kAlign) && key_hd(k) % vec_elems(dt) == 0;
       p.variant = p.kvariant[0] = key_op(k) == TRI_OP_KV_WRITE_Q8 ? (vec ? Q8W_VEC : Q8W_ANY)
                                                                   : (vec ? Q8R_VEC : Q8R_ANY);
-      p.ksub[0] = int32_t(key_code(k));
+      p.ksub[0] = int32_t(key_code(k) | key_attn_form(k) << 1);
       p.n_launches = 1;
       return p;
     }
