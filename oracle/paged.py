@@ -204,10 +204,11 @@ KV_SLOTS, KVW_ANY, KVW_VEC = 80, 82, 83
 PA_ANY, PA_ROWS, PA_TILE, PA_JOIN, PA_PAIR = 90, 91, 92, 93, 94
 OP_KV_WRITE_Q8, OP_KV_READ_Q8, OP_PAGED_ATTENTION_Q8 = 15, 16, 17
 Q8W_ANY, Q8W_VEC, Q8R_ANY, Q8R_VEC = 100, 101, 102, 103
-PA8_ANY, PA8_ROWS, PA8_TILE, PA8_PAIR = 104, 105, 106, 107
+PA8_ANY, PA8_ROWS, PA8_TILE, PA8_PAIR, PA8_JOIN = 104, 105, 106, 107, 108
 GRID_CAP = 1 << 20
 MAX_SPLITS = 64
 JOIN_WAVE = 8          # splits one wavefront joins
+MAX_SPLITS_Q8 = 128    # of few rows over an 8-bit cache
 
 
 def _bucket(T):
@@ -279,4 +280,81 @@ def attention_selection(dtype, T, R, nq, nk, hd, aligned, kv_max, workspace):
     launches = [((PA_ANY, PA_ROWS, PA_TILE, PA_PAIR)[form], grids[0], block)]
     if s > 1:
         launches.append((PA_JOIN, grids[1], 256))
+    return key, launches
+
+
+def kv_rows_q8_selection(op, dtype, code, T, R, nk, hd, block, aligned):
+    """kv_write_q8 or kv_read_q8; aligned: rows at 16 bytes, slots at a vector's codes."""
+    v = 8 if dtype else 4
+    vec = aligned and hd % v == 0
+    key = [_k0(op, dtype, T, aligned), 0, hd | nk << 32, code << 32, 0, 0]
+    if op == OP_KV_READ_Q8:
+        rows = 1 if T < 16384 else 4
+        return tuple(key), [(Q8R_VEC if vec else Q8R_ANY, min(GRID_CAP, _cdiv(T, 4 * rows)), 256)]
+    units, parts = min(T, T // block + 2 * R), 2 * nk       # blocks that the rows can touch
+    team = 1                                                # a wavefront
+    if vec:
+        vecs = min(_cdiv(T, R), block) * (hd // v)
+        team = 0 if vecs <= 128 else 1 if vecs <= 512 else 2
+        key[3] |= team << 16
+    if team == 0:                                           # 16 lanes; heads one after the other
+        groups = _cdiv(parts, 4)
+        inner = max(1, min(groups, units * groups // 2048))
+        waves = units * _cdiv(parts, 4 * inner)
+    else:
+        waves = units * parts * (4 if team == 2 else 1)
+    return tuple(key), [(Q8W_VEC if vec else Q8W_ANY, min(GRID_CAP, _cdiv(waves, 4)), 256)]
+
+
+def attention_q8_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, keys_max, workspace):
+    """(form, splits, grids, work-items, log2 of a tile's K heads, log2 of a step's keys)."""
+    g, heads, shift = nq // nk, 0, 0
+    rows, rpr, busy = T * nq, _cdiv(T, R) * g, min(R, T)
+    fits = lambda s: s < 2 or attention_workspace(T, nq, hd, s) <= workspace  # noqa: E731
+    if not (aligned and hd % 16 == 0 and hd <= 256):
+        form, block = 0, 256
+        s = min(512 // _cdiv(rows, 4), _cdiv(kv_max, 256), MAX_SPLITS)
+    elif rpr <= 16 or (_cdiv(T * g, 16) * nk <= 64 and kv_max <= 4096):
+        form, block = 1, 256 if hd > 128 else 512
+        short = kv_max <= 1024
+        if not (short and busy * nk < 1024):
+            heads = max(x for x in range(3) if x == 0 or (nk % (1 << x) == 0 and rpr <= 16 >> x))
+        groups, m = nk >> heads, 16 >> heads
+        tiles = (T * g // m + R) * groups
+        s = 1
+        if not short and max(_cdiv(T * g, m), busy) * groups < 4096:
+            s = min(MAX_SPLITS_Q8, (1 << 27) // (rows * (hd + 2) * 4))
+        shift = (8 if hd > 128 else 9) - heads
+        first = min(256, tiles * _cdiv(kv_max, 1 << shift))
+        while tiles * _cdiv(keys_max, 1 << shift) >= 1 << 31:
+            shift += 1
+    else:
+        form, block, full = 2, 256, _cdiv(T * g, 128)
+        s = min(256 // (max(full, busy) * nk), _cdiv(kv_max, 512), MAX_SPLITS)
+        if T % R == 0:
+            few = R * _cdiv(T // R * g, 128) * nk < (256 if R > 1 else 257)
+        else:
+            few = (full + busy // 2) * nk <= 288
+        if dtype and hd <= 128 and few and full * nk <= 256:
+            form, block = 3, 512
+    while not fits(s):
+        s -= 1
+    s = max(1, s)
+    if form == 0:
+        first = min(GRID_CAP, _cdiv(rows * s, 4))
+    elif form > 1:
+        first = (T * g // 128 + R) * nk * s
+    four = rows < 1024 if form == 1 else s > JOIN_WAVE
+    join = min(GRID_CAP, rows if four else _cdiv(rows, 4))
+    return form, s, [first] + ([join] if s > 1 else []), block, heads, shift
+
+
+def attention_q8_selection(dtype, code, T, R, nq, nk, hd, aligned, kv_max, keys_max, workspace):
+    form, s, grids, block, heads, _ = attention_q8_plan(dtype, T, R, nq, nk, hd, aligned, kv_max,
+                                                        keys_max, workspace)
+    key = (_k0(OP_PAGED_ATTENTION_Q8, dtype, T, aligned), 0, hd | nq << 16 | nk << 32,
+           form << 16 | int(s > 1) << 24 | heads << 25 | code << 32, 0, 0)
+    launches = [((PA8_ANY, PA8_ROWS, PA8_TILE, PA8_PAIR)[form], grids[0], block)]
+    if s > 1:
+        launches.append((PA8_JOIN if form == 1 else PA_JOIN, grids[1], 256))
     return key, launches

@@ -22,9 +22,6 @@
 namespace tri {
 namespace dev {
 
-// Whether PA8_ROWS reads codes past the caches (nontemporally).
-constexpr bool kStreamCodes = true;
-
 // Eight codes as bf16 (exact): v_cvt_scalef32_pk_bf16_fp8 of two, or a conversion to float32 of
 // each, whose upper half it is.
 template <int CT>
@@ -481,7 +478,7 @@ start:
 #pragma unroll
     for (int i = 0; i < S::NP; ++i) r[i] = __shfl(at, srow + S::RP * i);
 #pragma unroll
-    for (int i = 0; i < S::NP; ++i) x[i] = ld16<kStreamCodes>(reinterpret_cast<const u32x4 *>(p + r[i]));
+    for (int i = 0; i < S::NP; ++i) x[i] = ld16<true>(reinterpret_cast<const u32x4 *>(p + r[i]));
   };
   const auto to_lds = [&](u32x4(&x)[S::NP]) {
     if (padded)

@@ -336,9 +336,11 @@ uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4 * int64_t(q8_read
 // PA8_ROWS takes as many K heads a tile, up to four, as its 16 rows have room for, and shares
 // its steps out to a workgroup a compute unit by itself, so the host sets only the most parts
 // that a tile may have: all that the join takes, within 128 MiB of partial sums; none where a
-// workgroup would take 16 tiles or more, or no request has over 1024 keys. Those take one head a
-// tile: as many workgroups as there are, of a step or two (one request of 500, 32 heads: FIGURES
-// us, with four heads and a join 19).
+// workgroup would take 16 tiles or more, or no request has over 1024 keys. Of such short ones a
+// tile takes one head while that leaves less than four tiles a compute unit (measured with one
+// and with up to four heads a tile, 32 query heads of 128: one request of 500 keys, 32 K heads
+// 12.0 and 18.1 us, the join with it; 64 of 500, 8 K heads 21.0 and 30.8; 128 of 500 39.6 and
+// 39.4, of 900 56.6 and 49.5; 400 of 500 115 and 69).
 AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                       bool aligned, int64_t kv_max, int64_t keys_max, uint64_t workspace) {
   AttnPlan p{};
@@ -354,7 +356,8 @@ AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t 
   }
   if (p.form == kAttnRows) {
     const bool small = kv_max <= 1024;
-    while (p.heads < 2 && !small && nk % (2 << p.heads) == 0 && rpr <= 8 >> p.heads) ++p.heads;
+    const bool one = small && busy * nk < 4 * kUnits;
+    while (p.heads < 2 && !one && nk % (2 << p.heads) == 0 && rpr <= 8 >> p.heads) ++p.heads;
     const int64_t tm = 16 >> p.heads, full = cdiv(T * g, tm), groups = nk >> p.heads;
     const int64_t tiles = T * g / tm + R;
     have = (full > busy ? full : busy) * groups;
@@ -466,6 +469,8 @@ static bool paged_key_valid(const Key &k) {
   const uint32_t form = key_attn_form(k);
   if (nq < 1 || int32_t(nq) > kHeadsMax || nq % nk) return false;
   if (k3 & ~((uint64_t(0xFF) << 16) | (uint64_t(q8 ? 7 : 1) << 24))) return false;
+  const uint32_t heads = uint32_t(k3 >> 25);   // log2 of the K heads of a tile
+  if (heads && (form != kAttnRows || heads > 2 || nk % (1u << heads))) return false;
   const bool aligned = key_flags(k) & kAlign;
   const bool matrix = q8 ? attn_q8_matrix(aligned, int32_t(hd))
                          : attn_matrix(key_dtype(k), aligned, int32_t(hd));
