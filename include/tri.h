@@ -104,6 +104,7 @@ enum { TRI_MAX_LAYERS = 1024 };   /* layers per tri_decode_chain_layers call */
 /* The paged KV cache: requests per call, slots per page, and workgroups that
  * share the keys of one tile of queries, at most. */
 enum { TRI_MAX_REQUESTS = 4096, TRI_MAX_PAGE = 65536, TRI_MAX_KV_SPLITS = 64 };
+/* (TRI_MAX_KV_SPLITS: parts of a tile's keys; over an 8-bit cache, few rows, 128) */
 
 enum {
   TRI_CACHE_AUTO_INSTALL = 1u,   /* on a miss: install, then launch */
@@ -135,7 +136,8 @@ typedef struct tri_launch_rec {
   int32_t variant;     /* kernel variant id (the install policy table)       */
   uint32_t grid_x;     /* workgroups                                          */
   uint32_t block_x;    /* work-items per workgroup: 256; 1024 for variant 19;
-                        * 512 for variant 91 with heads of up to 128, and 94  */
+                        * 512 for variants 91 and 105 with heads of up to 128,
+                        * 94 and 107                                           */
 } tri_launch_rec;
 
 /* Words of the packed guard key. */

@@ -289,17 +289,16 @@ def kv_rows_q8_selection(op, dtype, code, T, R, nk, hd, block, aligned):
     vec = aligned and hd % v == 0
     key = [_k0(op, dtype, T, aligned), 0, hd | nk << 32, code << 32, 0, 0]
     if op == OP_KV_READ_Q8:
-        rows = 1 if T < 16384 else 4
-        return tuple(key), [(Q8R_VEC if vec else Q8R_ANY, min(GRID_CAP, _cdiv(T, 4 * rows)), 256)]
+        return tuple(key), [(Q8R_VEC if vec else Q8R_ANY, min(GRID_CAP, _cdiv(T, 4)), 256)]
     units, parts = min(T, T // block + 2 * R), 2 * nk       # blocks that the rows can touch
     team = 1                                                # a wavefront
     if vec:
         vecs = min(_cdiv(T, R), block) * (hd // v)
-        team = 0 if vecs <= 128 else 1 if vecs <= 512 else 2
+        team = 0 if vecs < 128 else 1 if vecs <= 512 else 2
         key[3] |= team << 16
     if team == 0:                                           # 16 lanes; heads one after the other
         groups = _cdiv(parts, 4)
-        inner = max(1, min(groups, units * groups // 2048))
+        inner = max(1, min(groups, units * groups // 4096))
         waves = units * _cdiv(parts, 4 * inner)
     else:
         waves = units * parts * (4 if team == 2 else 1)
@@ -330,7 +329,7 @@ def attention_q8_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, keys_max, worksp
             shift += 1
     else:
         form, block, full = 2, 256, _cdiv(T * g, 128)
-        s = min(256 // (max(full, busy) * nk), _cdiv(kv_max, 512), MAX_SPLITS)
+        s = min(256 // (max(full, busy) * nk), _cdiv(kv_max, 512 if dtype else 256), MAX_SPLITS)
         if T % R == 0:
             few = R * _cdiv(T // R * g, 128) * nk < (256 if R > 1 else 257)
         else:
@@ -344,7 +343,7 @@ def attention_q8_plan(dtype, T, R, nq, nk, hd, aligned, kv_max, keys_max, worksp
         first = min(GRID_CAP, _cdiv(rows * s, 4))
     elif form > 1:
         first = (T * g // 128 + R) * nk * s
-    four = rows < 1024 if form == 1 else s > JOIN_WAVE
+    four = rows < 512 if form == 1 else s > JOIN_WAVE
     join = min(GRID_CAP, rows if four else _cdiv(rows, 4))
     return form, s, [first] + ([join] if s > 1 else []), block, heads, shift
 

@@ -217,15 +217,17 @@ inline bool attn_q8_matrix(bool aligned, int32_t hd) {
 // As attn_plan, `aligned` with the codes; keys_max: the most keys the table holds for a request.
 AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk, int32_t hd,
                       bool aligned, int64_t kv_max, int64_t keys_max, uint64_t workspace);
-// Whether four wavefronts join a row of PA8_ROWS' parts: rows too few to fill the units.
-inline bool q8_join_four(int64_t T, int32_t nq) { return T * nq < 1024; }
-// Lanes of a team that quantises a block's rows of a head, `vecs` vectors: 0: 16, 1: 64, 2: 256.
-inline uint32_t q8_write_team(int64_t vecs) { return vecs <= 128 ? 0 : vecs <= 512 ? 1 : 2; }
+// Whether four wavefronts join a row of PA8_ROWS' parts: rows too few to fill the units (32 rows
+// of 90 parts: 61 us with the attention before it, 67 with one wavefront a row; 256 rows
+// 19.6 and 19.7, 768 28.5 and 27.2, 2048 109 and 101).
+inline bool q8_join_four(int64_t T, int32_t nq) { return T * nq < 512; }
+// Lanes of a team that quantises a block's rows of a head, `vecs` vectors: 0: 16, 1: 64, 2: 256
+// (8192 rows of 8 + 8 heads of 128, teams of 16 / 64 / 256, us: 64 vectors 16.7 / 27.1 / 89.7,
+// 128 19.0 / 18.0 / 48, 256 20.5 / 14.7 / 28.1, 512 35.7 / 14.3 / 18.4, 1024 67 / 18.7 / 14.9).
+inline uint32_t q8_write_team(int64_t vecs) { return vecs < 128 ? 0 : vecs <= 512 ? 1 : 2; }
 // Heads that a team of 16 lanes takes one after the other.
 uint32_t q8_write_inner(int64_t units, int32_t nk);
 uint32_t q8_write_grid(int64_t units, int32_t nk, uint32_t team, uint32_t inner);
-// Rows that a wavefront gives back: several where there are many.
-inline int32_t q8_read_rows(int64_t T) { return T < 16384 ? 1 : 4; }
 uint32_t q8_read_grid(int64_t T);
 // n / d by multiplication (kernargs.h).
 FastDiv fast_div_of(uint32_t d);

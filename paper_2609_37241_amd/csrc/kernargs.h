@@ -230,7 +230,7 @@ struct Q8RowsArgs {
   FastDiv block_div;      // by block
   FastDiv per_div;        // by per
   int32_t per;            // work-items of a row of a head
-  int32_t units, by_row;  // Q8W_*: how blocks are numbered; Q8R_*: rows of a wavefront
+  int32_t units, by_row;  // Q8W_*: how blocks are numbered
   uint32_t inner;         // Q8W_*: heads that a team takes one after the other
 };
 
@@ -246,7 +246,7 @@ struct PagedQ8Args {
   int32_t runs;           // PA8_ROWS: its workgroups
   int32_t step_shift;     // steps of 2^step_shift keys are what it shares out
   int32_t four;           // PA8_JOIN: 1: four wavefronts join a row, else one
-  int32_t reserved;
+  int32_t most;           // PA8_ROWS: steps of all tiles of one set of heads, at most
 };
 
 // An argument block held in device memory for launches without kernel

@@ -177,8 +177,8 @@ __device__ inline NanKeys nan_keys(int32_t key, bool inside, const int32_t *tabl
 
 // ---- PA8_ROWS -----------------------------------------------------------------------------------
 // Few rows per request (decode), as PA_ROWS: the wavefronts share out a tile's keys,
-// each with its own softmax, joined in LDS at the end. HBM-bound: K and V come in whole rows
-// and pass as codes through a part of LDS that is the wavefront's own, where a lane's 16
+// each with its own softmax, joined in LDS at the end. HBM-bound: K and V come in whole rows,
+// past the caches (through them 115 us for the 101 below), and pass as codes through a part of LDS that is the wavefront's own, where a lane's 16
 // codes of K are two products' operands, and the transposing read of bytes gives it 8 keys of one
 // element of V.
 //
@@ -187,7 +187,8 @@ __device__ inline NanKeys nan_keys(int32_t key, bool inside, const int32_t *tabl
 // keys of each: 64 rows of K, head by head, against all 16 columns. A column takes the
 // scores of its own head's rows and gives the others' weights of 0, so the products are as many
 // per byte as with one head, the exponentials 1 / HG, and what is read in a slot is HG
-// heads long (64 requests of 8192 keys, 4 of 8 heads: FIGURES).
+// heads long (64 requests of up to 8192 keys, 32 and 8 heads of 128, one / two / four a tile: 117
+// / 111 / 101 us; all of 8192 213 / 205 / 188, 5.7 TB/s of codes; one of 131,072 68 / 62 / 62).
 // A NaN code of V would meet other heads' weights of 0: a unit whose sums hold one where
 // the weights are finite is done again with such codes cleared.
 //
@@ -221,7 +222,9 @@ struct Rows8Shape {
 
 // The steps that all tiles take, `step` keys each, numbered request by request, tile by
 // tile, and that once for each HG heads: the host's choice of `step` keeps their number
-// below 2^31. Up to 64 requests are held by a lane each, more in LDS.
+// below 2^31. Requests whose rows overlap (starts that fall) could take more than the rows allow:
+// sums stop at a8.most, and steps behind those that T rows and R requests can take are
+// taken by nobody. Up to 64 requests are held by a lane each, more in LDS.
 template <int TM>
 struct Numbering {
   const PagedQ8Args &a8;
@@ -250,12 +253,18 @@ struct Numbering {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // over the first `lanes` lanes: sums with those of the lanes before, the largest
     const int lanes = a.R < 64 ? a.R : 64;
+    const int32_t top = a8.most;
+    const auto add = [&](int32_t x, int64_t y) { return y < top - x ? int32_t(x + y) : top; };
     const auto scan = [&](int32_t x) {
       for (int d = 1; d < lanes; d *= 2) {
         const int32_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
+        if (lane >= d) x = add(x, y);
       }
       return x;
+    };
+    const auto before_lane = [&](int32_t sum) {
+      const int32_t x = __shfl_up(sum, 1);
+      return lane > 0 ? x : 0;
     };
     const auto largest = [&](int32_t x) {
       for (int d = 1; d < lanes; d *= 2) {
@@ -267,11 +276,11 @@ struct Numbering {
     int32_t most = 0;   // steps of the longest tile
     if (a.R <= 64) {
       rq = request_of(a, lane < a.R ? lane : 0);
-      const int32_t steps = steps_of(rq), mine = lane < a.R ? tiles_of(rq) * steps : 0;
-      const int32_t sum = scan(mine);
-      first = sum - mine;
+      const int32_t steps = steps_of(rq);
+      const int32_t sum = scan(lane < a.R ? add(0, int64_t(tiles_of(rq)) * steps) : 0);
+      first = before_lane(sum);
       all = __builtin_amdgcn_readlane(sum, a.R - 1);
-      if (a.splits > 1) most = largest(steps);
+      most = largest(steps);
     } else {
       // consecutive requests a work-item, then the sums of what was before
       const int32_t each = (a.R + 64 * NW - 1) / (64 * NW), r0 = int32_t(threadIdx.x) * each;
@@ -280,7 +289,7 @@ struct Numbering {
         const Request x = request_of(a, r);
         const int32_t n = steps_of(x);
         most = n > most ? n : most;
-        mine += tiles_of(x) * n;
+        mine = add(mine, int64_t(tiles_of(x)) * n);
       }
       const int32_t sum = scan(mine);
       most = largest(most);
@@ -289,22 +298,24 @@ struct Numbering {
         wave_sums[NW + wave] = most;
       }
       __syncthreads();
-      int32_t before = sum - mine;
+      int32_t before = before_lane(sum);
       all = 0;
       for (int w = 0; w < NW; ++w) {
-        before += w < wave ? wave_sums[w] : 0;
-        all += wave_sums[w];
+        before = add(before, w < wave ? wave_sums[w] : 0);
+        all = add(all, wave_sums[w]);
         most = wave_sums[NW + w] > most ? wave_sums[NW + w] : most;
       }
       for (int32_t r = r0; r < r0 + each && r < a.R; ++r) {
         sums[r] = before;
         const Request x = request_of(a, r);
-        before += tiles_of(x) * steps_of(x);
+        before = add(before, int64_t(tiles_of(x)) * steps_of(x));
       }
       __syncthreads();
       all = __builtin_amdgcn_readfirstlane(all);
       most = __builtin_amdgcn_readfirstlane(most);
     }
+    const int64_t room = (int64_t(a.T) * a.g / TM + a.R) * most;
+    all = room < all ? int32_t(room) : all;
     per = int32_t((uint32_t(all) * uint32_t(heads) + uint32_t(runs) - 1) / uint32_t(runs));
     // a tile of n steps meets at most (n - 2) / per + 2 runs
     if (a.splits > 1) {
@@ -764,6 +775,9 @@ start:
 // read from LDS in fours (one of each four, where neighbouring keys share it, gained 1.5 %
 // only: 2048 tokens behind 6144, 291 -> 287 us). The running maximum as in PA_TILE; bf16
 // weights are one part, rounded, float32 ones three.
+// Bound, as there, by each wavefront's chain of products, exponentials and LDS reads: those 2048
+// tokens, 32 and 8 heads of 128, 826 TFLOP/s in e4m3, 799 in int8 (from bf16 pages 845); a prompt's
+// last tile alone, 1024 keys of heads of 256, takes the 57 us of four such prompts.
 template <int DT, int HDP>
 struct Tile8Shape {
   static constexpr int ES = Elt<DT>::ES;

@@ -55,7 +55,6 @@ __device__ inline void elements(const u32x4 &v, float *x) {
 }
 
 // N codes as they lie in a register (or two).
-
 template <int N>
 struct CodesOf {
   uint32_t w[(N + 3) / 4];
@@ -91,7 +90,11 @@ __device__ inline void store_codes(char *p, const CodesOf<N> &c) {
 // block, of one head of K or V: it holds them, 8 vectors a lane (an element a lane, Q8W_ANY),
 // takes the largest magnitude, makes the scale and stores the codes; what it cannot hold
 // it reads twice. A block belongs to one team alone: no atomics, the same bits every
-// time. Blocks are numbered through the requests without knowing their lengths on the
+// time. Bound by memory where there are many rows (8192 of 8 + 8 heads of 128, a scale for 16
+// tokens: 14.4 us in e4m3, 7 TB/s, with the rows in the last-level cache; int8, whose exact quotient
+// takes more work, 16.2), by a chain of four loads (starts, table, scale and rows, codes of a
+// block that goes on) for single tokens (8 requests 6.3 us, a launch alone 2.4).
+// Blocks are numbered through the requests without knowing their lengths on the
 // host: n tokens touch at most floor((n - 2) / B) + 2 blocks, and at most n, so those of r
 // start at floor(q_start[r] / B) + 2 r, or (a.by_row, the fewer) at q_start[r].
 template <int DT, int CT, bool VEC, int L>
@@ -248,64 +251,60 @@ __global__ __launch_bounds__(256, L == 16 ? 4 : 5) void k_q8_write(Q8RowsArgs a)
 }
 
 // ---- Q8R_* ------------------------------------------------------------------------------------
-// A wavefront gives a.units neighbouring rows of K and V back, a vector a work-item (an
-// element, Q8R_ANY), four of them in flight.
+// A wavefront gives a row of K and V back, a vector a work-item (an element, Q8R_ANY), four of
+// them in flight. Bound by memory: 32 ragged caches of up to 4000 tokens, 8 heads of 128, 83.6 us
+// (4.9 TB/s, what a copy reaches); four rows a wavefront, one search for all, 86.9.
 template <int DT, int CT, bool VEC>
 __global__ __launch_bounds__(256) void k_q8_read(Q8RowsArgs a) {
   constexpr int N = VEC ? Elt<DT>::V : 1, U = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Requests held = requests(a);
   const int half = a.nk * a.per;
-  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + wave) * a.units; row0 < a.T;
-       row0 += int64_t(gridDim.x) * 4 * a.units) {
-    Request rq = {0, 0, 0};
-    int32_t r = -1;
-    for (int32_t row = int32_t(row0); row < row0 + a.units && row < a.T; ++row) {
-      if (r < 0 || row >= rq.q1)
-        r = find_request(a, held, &rq, [&](int32_t, int32_t q0) { return q0 <= row; });
-      if (r < 0 || row < rq.q0 || row >= rq.q1) continue;
-      const int32_t p = rq.kv - (rq.q1 - row);
-      int64_t id = -1;
-      uint32_t slot = 0;
-      if (p >= 0) {
-        const uint32_t col = fast_div(uint32_t(p), a.div);
-        const int32_t x = a.table[r * a.table_rs + col];
-        id = uint32_t(x) < uint32_t(a.n_pages) ? x : -1;
-        slot = uint32_t(p) - col * uint32_t(a.page);
+  for (int32_t row = int32_t(blockIdx.x) * 4 + wave; row < a.T; row += int32_t(gridDim.x) * 4) {
+    Request rq;
+    const int32_t r = find_request(a, held, &rq, [&](int32_t, int32_t q0) { return q0 <= row; });
+    if (r < 0 || row < rq.q0 || row >= rq.q1) continue;
+    const int32_t p = rq.kv - (rq.q1 - row);
+    int64_t id = -1;
+    uint32_t slot = 0;
+    if (p >= 0) {
+      const uint32_t col = fast_div(uint32_t(p), a.div);
+      const int32_t x = a.table[r * a.table_rs + col];
+      id = uint32_t(x) < uint32_t(a.n_pages) ? x : -1;
+      slot = uint32_t(p) - col * uint32_t(a.page);
+    }
+    const uint32_t block = fast_div(slot, a.block_div);
+    const int64_t at = id < 0 ? 0 : id;
+    for (int i0 = lane; i0 < 2 * half; i0 += 64 * U) {
+      CodesOf<N> c[U];
+      float s[U];
+      int64_t to[U];
+      bool is_v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + 64 * u < 2 * half ? i0 + 64 * u : i0;
+        is_v[u] = i >= half;
+        const int j = is_v[u] ? i - half : i, h = int(fast_div(uint32_t(j), a.per_div));
+        const int e = (j - h * a.per) * N;
+        const PagedView &view = is_v[u] ? a.cv : a.ck;
+        c[u] = load_codes<N>(static_cast<const char *>(view.p) + at * view.ps +
+                             int64_t(slot) * view.ss + int64_t(h) * view.hs + e);
+        s[u] = *scale_at(is_v[u] ? a.sv : a.sk, at, block, uint32_t(h));
+        to[u] = row * (is_v[u] ? a.v_ts : a.k_ts) + int64_t(h) * a.hd + e;
       }
-      const uint32_t block = fast_div(slot, a.block_div);
-      const int64_t at = id < 0 ? 0 : id;
-      for (int i0 = lane; i0 < 2 * half; i0 += 64 * U) {
-        CodesOf<N> c[U];
-        float s[U];
-        int64_t to[U];
-        bool is_v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int i = i0 + 64 * u < 2 * half ? i0 + 64 * u : i0;
-          is_v[u] = i >= half;
-          const int j = is_v[u] ? i - half : i, h = int(fast_div(uint32_t(j), a.per_div));
-          const int e = (j - h * a.per) * N;
-          const PagedView &view = is_v[u] ? a.cv : a.ck;
-          c[u] = load_codes<N>(static_cast<const char *>(view.p) + at * view.ps +
-                               int64_t(slot) * view.ss + int64_t(h) * view.hs + e);
-          s[u] = *scale_at(is_v[u] ? a.sv : a.sk, at, block, uint32_t(h));
-          to[u] = row * (is_v[u] ? a.v_ts : a.k_ts) + int64_t(h) * a.hd + e;
-        }
+      for (int u = 0; u < U; ++u) {
+        if (i0 + 64 * u >= 2 * half) break;
+        float f[(N + 3) / 4 * 4];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (i0 + 64 * u >= 2 * half) break;
-          float f[(N + 3) / 4 * 4];
+        for (int k = 0; k < (N + 3) / 4; ++k) codes4<CT>(c[u].w[k], f + 4 * k);
 #pragma unroll
-          for (int k = 0; k < (N + 3) / 4; ++k) codes4<CT>(c[u].w[k], f + 4 * k);
-#pragma unroll
-          for (float &y : f) y = id < 0 ? 0.0f : y * s[u];
-          char *o = static_cast<char *>(is_v[u] ? a.v : a.k) + to[u] * Elt<DT>::ES;
-          if constexpr (VEC)
-            *reinterpret_cast<u32x4 *>(o) = Elt<DT>::pack(f);
-          else
-            Elt<DT>::st(o, 0, f[0]);
-        }
+        for (float &y : f) y = id < 0 ? 0.0f : y * s[u];
+        char *o = static_cast<char *>(is_v[u] ? a.v : a.k) + to[u] * Elt<DT>::ES;
+        if constexpr (VEC)
+          *reinterpret_cast<u32x4 *>(o) = Elt<DT>::pack(f);
+        else
+          Elt<DT>::st(o, 0, f[0]);
       }
     }
   }
@@ -314,7 +313,9 @@ __global__ __launch_bounds__(256) void k_q8_read(Q8RowsArgs a) {
 // ---- PA8_ANY ----------------------------------------------------------------------------------
 // As PA_ANY: a wavefront per row, query head and split, a lane a key of 64 for the
 // scores, and elements l, l + 64, ... of the head for the sums. A key that is not
-// seen is never read. Scores are in powers of two from the start: (q.k s) c.
+// seen is never read. Scores are in powers of two from the start: (q.k s) c. Bound by its
+// loads, a byte of a row of K a lane (64 requests of up to 1000 keys, 32 and 8 heads of 100: 611 us,
+// PA_ANY over bf16 732).
 template <int DT, int CT>
 __global__ __launch_bounds__(256) void k_pa8_any(PagedQ8Args a8) {
   constexpr int ES = Elt<DT>::ES;
@@ -412,6 +413,8 @@ __global__ __launch_bounds__(256) void k_pa8_any(PagedQ8Args a8) {
 }
 
 // ---- PA8_JOIN: the parts of the tiles that PA8_ROWS cut (join.h) -----------------------------
+// How many a row has follows from the same numbering; a tile that one workgroup had is there
+// already. 32 rows of 90 parts 6.1 us, 2048 rows of one to eight 7.4: latency.
 template <int DT, int HG>
 __global__ __launch_bounds__(256) void k_pa8_join(PagedQ8Args a8) {
   constexpr int TM = 16 / HG;
@@ -428,7 +431,8 @@ __global__ __launch_bounds__(256) void k_pa8_join(PagedQ8Args a8) {
     const int32_t tile = ((t - rq.q0) * a.g + h - kh * a.g) / TM, steps = nb.steps_of(rq);
     const uint32_t begin = uint32_t(nb.all * (kh / HG) + nb.before(r) + tile * steps);
     const uint32_t per = uint32_t(nb.per);
-    return int32_t((begin + uint32_t(steps) - 1) / per - begin / per) + 1;
+    const int32_t parts = int32_t((begin + uint32_t(steps) - 1) / per - begin / per) + 1;
+    return parts < a.splits ? parts : a.splits;   // (a row in two requests: anything, but inside)
   };
   join_rows<DT, 4, kQ8Splits / 64>(a, a8.four != 0, parts_of);
 }

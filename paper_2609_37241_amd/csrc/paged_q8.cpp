@@ -62,7 +62,7 @@ tri_status rows_q8(tri_cache *c, uint32_t op, const tri_kv_rows_args *p, void *s
                         a.cols, a.kv.n_pages, a.kv.page, a.kv.nk, a.kv.hd, q.block,
                         fast_div_of(uint32_t(a.kv.page)), fast_div_of(uint32_t(q.block)),
                         fast_div_of(uint32_t(per)), per,
-                        write ? int32_t(units) : q8_read_rows(a.T), by_row, inner};
+                        int32_t(units), by_row, inner};
   const uint32_t grid = write ? q8_write_grid(units, a.kv.nk, team, inner) : q8_read_grid(a.T);
   return run_paged(c, op, k, a.T, &grid, 1, kBlock, &args, sizeof args, stream);
 }
@@ -105,7 +105,8 @@ tri_status tri_paged_attention_quant(tri_cache *c, const tri_attention_args *p, 
                          {q8->v_scale, q8->v_ps, q8->v_bs, q8->v_hs},
                          weight_scale(a.scale), q8->block, fast_div_of(uint32_t(q8->block)),
                          int32_t(plan.grid[0]),
-                         plan.step_shift, q8_join_four(a.T, a.nq), 0};
+                         plan.step_shift, q8_join_four(a.T, a.nq),
+                         int32_t(0x7FFFFFFF / (a.kv.nk >> plan.heads))};
   return run_paged(c, op, k, a.T, plan.grid, plan.splits > 1 ? 2 : 1, plan.block, &args, sizeof args,
                    stream);
 }

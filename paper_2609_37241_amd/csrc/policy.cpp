@@ -315,9 +315,11 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
 }
 
 // ---- the paged KV cache in 8 bits ----
-// As many as leave two wavefronts a SIMD unit, at most all.
+// As many as leave four wavefronts a SIMD unit, at most all (1 / 2 / 4, us: 8192 rows of 8 + 8 heads
+// of 128, a scale for four tokens 18.3 / 16.7 / 20.8, for each 37.3 / 31.6 / 28.4; 400 single rows
+// 7.0 / 8.3 / 11.8).
 uint32_t q8_write_inner(int64_t units, int32_t nk) {
-  const int64_t groups = cdiv(2 * int64_t(nk), 4), x = units * groups / (8 * kUnits);
+  const int64_t groups = cdiv(2 * int64_t(nk), 4), x = units * groups / (16 * kUnits);
   return uint32_t(x < 1 ? 1 : x < groups ? x : groups);
 }
 
@@ -328,10 +330,11 @@ uint32_t q8_write_grid(int64_t units, int32_t nk, uint32_t team, uint32_t inner)
   return clamp_grid(team == 2 ? units * parts : cdiv(units * parts, 4));
 }
 
-uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4 * int64_t(q8_read_rows(T)))); }
+uint32_t q8_read_grid(int64_t T) { return clamp_grid(cdiv(T, 4)); }
 
 // Forms as attn_plan, but that float32 queries take tiles of many rows as bf16 ones do (three
-// products for one, not sixteen). Splits of those as attn_plan, too.
+// products for one, not sixteen). Splits of those as attn_plan, too (float32: six chunks behind
+// up to 1500 tokens, 8 and 4 heads of 64, in runs of 128 / 256 / 512 keys 28.7 / 21.9 / 30.0 us).
 //
 // PA8_ROWS takes as many K heads a tile, up to four, as its 16 rows have room for, and shares
 // its steps out to a workgroup a compute unit by itself, so the host sets only the most parts
@@ -377,7 +380,7 @@ AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t 
       const int64_t full = cdiv(T * g, 128);
       have = (full > busy ? full : busy) * nk;
       want = 256;
-      run = 512;
+      run = f32 ? 256 : 512;
       const bool equal = T % R == 0;
       const int64_t expected = (equal ? R * cdiv(T / R * g, 128) : full + busy / 2) * nk;
       const int64_t most = !equal ? kUnits * 9 / 8 : R > 1 ? kUnits - 1 : kUnits;

@@ -199,6 +199,35 @@ def test_workspaces_of_any_size(cache, tri, part):
         assert (space[n:] == 255).all()
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("R", [3, 64, 301])
+@pytest.mark.parametrize("hd", [64, 20])
+def test_starts_that_fall(cache, code, R, hd):
+    """Requests whose rows overlap (a caller's mistake): what they leave is theirs, but no more
+    work is done than the rows allow and nothing else is written."""
+    T, page = 40, 16
+    p = problem("bf16", code, [(600, 1)] * R, 8, 2, hd, page, 8)
+    p["q_start"] = i32([0, T] * ((R + 1) // 2) + [0] * ((R + 1) % 2))
+    flat = torch.full((T + 8, 8, hd), 7.0, dtype=torch.bfloat16, device=DEV)
+    p["q"] = torch.randn((T, 8, hd), device=DEV).to(torch.bfloat16)
+    attend(cache, p, out=flat[4:-4])
+    attend(cache, p, max_kv=600, out=flat[4:-4])
+    assert (flat[:4] == 7.0).all() and (flat[-4:] == 7.0).all()
+    rows = torch.full((2, T + 8, 2, hd), 7.0, dtype=torch.bfloat16, device=DEV)
+    a = (p["kc"], p["vc"], p["ks"], p["vs"], p["table"], p["kv_len"], p["q_start"])
+    cache.kv_read_q8(*a, T, k=rows[0, 4:-4], v=rows[1, 4:-4])
+    torch.cuda.synchronize()
+    assert (rows[:, :4] == 7.0).all() and (rows[:, -4:] == 7.0).all()
+    spare = sorted(set(range(p["kc"].shape[0])) - set(p["table"].view(-1).tolist()))
+    before = [p[c][spare].view(torch.uint8).clone() for c in ("kc", "vc", "ks", "vs")]
+    cache.kv_write_q8(rows[0, 4:-4], rows[1, 4:-4], *a)
+    torch.cuda.synchronize()
+    assert spare and all(torch.equal(p[c][spare].view(torch.uint8), b)
+                         for c, b in zip(("kc", "vc", "ks", "vs"), before))
+    p = problem("bf16", code, [(600, 1)] * 3, 8, 2, hd, page, 8)
+    check(attend(cache, p), oracle(p), "bf16")
+
+
 # ---- routes -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("lens", [[(40, 1), (9, 1)], [(3000, 1)], [(300, 200)], [(1500, 33)]])
 @pytest.mark.parametrize("code", CODES)

@@ -267,7 +267,7 @@ def test_attention_argument_block(lib, fresh):
     assert C.c_float.from_buffer_copy(raw[192:196]).value == 1.0 and raw[196:198] == b"\x01\0"
     assert [word(216 + 8 * i, 8) for i in range(8)] == [at(7), 16, 4, 1, at(8), 16, 4, 1]
     assert abs(C.c_float.from_buffer_copy(raw[280:284]).value - 0.25 * 1.4426950408889634) < 1e-7
-    assert word(284) == 4 and [word(296 + 4 * i) for i in range(3)] == [grids[0], shift, 1]
+    assert word(284) == 4 and [word(296 + 4 * i) for i in range(4)] == [grids[0], shift, 1, (2 ** 31 - 1) // 2]
 
 
 def test_steps_stay_in_31_bits(lib, fresh):
