@@ -102,9 +102,9 @@ typedef enum tri_code { TRI_INT8 = 0, TRI_E4M3 = 1 } tri_code;
 enum { TRI_MAX_LAYERS = 1024 };   /* layers per tri_decode_chain_layers call */
 
 /* The paged KV cache: requests per call, slots per page, and workgroups that
- * share the keys of one tile of queries, at most. */
+ * share the keys of one tile of queries, at most (128 for tiles of few rows over
+ * the cache in 8 bits). */
 enum { TRI_MAX_REQUESTS = 4096, TRI_MAX_PAGE = 65536, TRI_MAX_KV_SPLITS = 64 };
-/* (TRI_MAX_KV_SPLITS: parts of a tile's keys; over an 8-bit cache, few rows, 128) */
 
 enum {
   TRI_CACHE_AUTO_INSTALL = 1u,   /* on a miss: install, then launch */
@@ -669,7 +669,7 @@ int64_t tri_paged_attention_workspace(const tri_attention_args *args);
 tri_status tri_kv_write_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
 
 /* The tokens' values code * scale, rounded once, into rows of k and v (which the call
- * writes; they must not overlap the cache). With kv_len = lengths and q_start their running
+ * writes; they must not overlap each other or the cache). With kv_len = lengths and q_start their running
  * sum: all tokens. Rows before q_start[0] and from q_start[R] on are left as they were. */
 tri_status tri_kv_read_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
 
