@@ -314,8 +314,8 @@ __global__ __launch_bounds__(256) void k_q8_read(Q8RowsArgs a) {
 // As PA_ANY: a wavefront per row, query head and split, a lane a key of 64 for the
 // scores, and elements l, l + 64, ... of the head for the sums. A key that is not
 // seen is never read. Scores are in powers of two from the start: (q.k s) c. Bound by its
-// loads, a byte of a row of K a lane (64 requests of up to 1000 keys, 32 and 8 heads of 100: 611 us,
-// PA_ANY over bf16 732).
+// loads, a byte of V a lane, one or four of K (64 requests of up to 1000 keys, 32 and 8 heads of
+// 100: 239 us; with a key's V at a time 594, bytes of K as well 612; PA_ANY over bf16 732).
 template <int DT, int CT>
 __global__ __launch_bounds__(256) void k_pa8_any(PagedQ8Args a8) {
   constexpr int ES = Elt<DT>::ES;
@@ -324,6 +324,9 @@ __global__ __launch_bounds__(256) void k_pa8_any(PagedQ8Args a8) {
   __shared__ float qs[4][512];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t items = int64_t(a.T) * a.nq * a.splits;
+  // whether four codes of K lie at a multiple of 4
+  const bool words = ((uint64_t(a.hd) | uint64_t(a.k.p) | uint64_t(a.k.ps) | uint64_t(a.k.ss) |
+                       uint64_t(a.k.hs)) & 3) == 0;
   for (int64_t it = int64_t(blockIdx.x) * 4 + wave; it < items; it += int64_t(gridDim.x) * 4) {
     const int64_t row = it / a.splits;
     const int32_t s = int32_t(it - row * a.splits);
@@ -361,6 +364,14 @@ __global__ __launch_bounds__(256) void k_pa8_any(PagedQ8Args a8) {
           vs = *scale_at(a8.vs, id, block, uint32_t(kh));
           float x[4] = {};   // four sums: shorter chains, smaller errors
           int d = 0;
+          if (words)
+#pragma unroll 4
+            for (; d < a.hd; d += 4) {
+              float c[4];
+              codes4<CT>(*reinterpret_cast<const uint32_t *>(k + d), c);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[i] = fmaf(qs[wave][d + i], c[i], x[i]);
+            }
           for (; d + 4 <= a.hd; d += 4)
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = fmaf(qs[wave][d + i], code1<CT>(k[d + i]), x[i]);
@@ -384,13 +395,28 @@ __global__ __launch_bounds__(256) void k_pa8_any(PagedQ8Args a8) {
       const float wv = w * vs;
 #pragma unroll
       for (int i = 0; i < NI; ++i) acc[i] *= alpha;
-      for (int j = 0; j < 64; ++j) {
-        if (!((seen >> j) & 1)) continue;
-        const float wj = __shfl(wv, j);
-        const uint8_t *v = vp + __shfl(vo, j);
+      // eight keys' loads in flight (of one that is not seen the pool's first slot, as 0)
+      for (int j = 0; j < 64; j += 8) {
+        if (!((seen >> j) & 0xFF)) continue;
+        float wj[8];
+        const uint8_t *v[8];
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-          if (lane + 64 * i < a.hd) acc[i] = fmaf(wj, code1<CT>(v[lane + 64 * i]), acc[i]);
+        for (int u = 0; u < 8; ++u) {
+          wj[u] = __shfl(wv, j + u);
+          const int64_t at = __shfl(vo, j + u);
+          v[u] = vp + (at < 0 ? 0 : at);
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if (64 * i >= a.hd) break;
+          const int d = lane + 64 * i < a.hd ? lane + 64 * i : 0;
+          uint8_t c[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) c[u] = v[u][d];
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            acc[i] = fmaf(wj[u], (seen >> (j + u)) & 1 ? code1<CT>(c[u]) : 0.0f, acc[i]);
+        }
       }
     }
     if (a.splits > 1) {
