@@ -294,7 +294,7 @@ def kv_rows_q8_selection(op, dtype, code, T, R, nk, hd, block, aligned):
     team = 1                                                # a wavefront
     if vec:
         vecs = min(_cdiv(T, R), block) * (hd // v)
-        team = 0 if vecs < 128 else 1 if vecs <= 512 else 2
+        team = 0 if vecs <= 128 else 1 if vecs <= 512 else 2
         key[3] |= team << 16
     if team == 0:                                           # 16 lanes; heads one after the other
         groups = _cdiv(parts, 4)

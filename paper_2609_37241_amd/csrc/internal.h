@@ -222,9 +222,9 @@ AttnPlan attn_q8_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t 
 // 19.6 and 19.7, 768 28.5 and 27.2, 2048 109 and 101).
 inline bool q8_join_four(int64_t T, int32_t nq) { return T * nq < 512; }
 // Lanes of a team that quantises a block's rows of a head, `vecs` vectors: 0: 16, 1: 64, 2: 256
-// (8192 rows of 8 + 8 heads of 128, teams of 16 / 64 / 256, us: 64 vectors 16.7 / 27.1 / 89.7,
-// 128 19.0 / 18.0 / 48, 256 20.5 / 14.7 / 28.1, 512 35.7 / 14.3 / 18.4, 1024 67 / 18.7 / 14.9).
-inline uint32_t q8_write_team(int64_t vecs) { return vecs < 128 ? 0 : vecs <= 512 ? 1 : 2; }
+// (8192 rows of 8 + 8 heads of 128, teams of 16 / 64 / 256, us: 64 vectors 15.5 / 29.3 / 96.7,
+// 128 15.1 / 18.7 / 51.9, 256 20.2 / 14.4 / 29.7, 512 35.1 / 14.0 / 18.9, 1024 67 / 18.6 / 14.7).
+inline uint32_t q8_write_team(int64_t vecs) { return vecs <= 128 ? 0 : vecs <= 512 ? 1 : 2; }
 // Heads that a team of 16 lanes takes one after the other.
 uint32_t q8_write_inner(int64_t units, int32_t nk);
 uint32_t q8_write_grid(int64_t units, int32_t nk, uint32_t team, uint32_t inner);

@@ -92,8 +92,8 @@ __device__ inline void store_codes(char *p, const CodesOf<N> &c) {
 // it reads twice. A block belongs to one team alone: no atomics, the same bits every
 // time. Bound by memory where there are many rows (8192 of 8 + 8 heads of 128, a scale for 16
 // tokens: 14.4 us in e4m3, 7 TB/s, with the rows in the last-level cache; int8, whose exact quotient
-// takes more work, 16.2), by a chain of four loads (starts, table, scale and rows, codes of a
-// block that goes on) for single tokens (8 requests 6.3 us, a launch alone 2.4).
+// takes more work, 15.3), by a chain of four loads (starts, table and rows, scale, codes of a
+// block that goes on) for single tokens (8 requests 6.2 us, KVW_VEC 2.4).
 // Blocks are numbered through the requests without knowing their lengths on the
 // host: n tokens touch at most floor((n - 2) / B) + 2 blocks, and at most n, so those of r
 // start at floor(q_start[r] / B) + 2 r, or (a.by_row, the fewer) at q_start[r].
@@ -134,8 +134,6 @@ __global__ __launch_bounds__(256, L == 16 ? 4 : 5) void k_q8_write(Q8RowsArgs a)
     const int32_t old = from - int32_t(begin), row0 = from - base + rq.q0;
     const int32_t items_new = (to - from) * a.per;   // work-items
     const uint32_t slot = uint32_t(begin) - col * uint32_t(a.page);
-    const bool there = uint32_t(id) < uint32_t(a.n_pages);
-    if (!there) continue;
     for (uint32_t in = 0; in < inner; ++in) {
       uint32_t part = part0 + in * TW;
       if (part >= parts) break;
@@ -175,6 +173,7 @@ __global__ __launch_bounds__(256, L == 16 ? 4 : 5) void k_q8_write(Q8RowsArgs a)
         if (L * k >= items_new) continue;   // (for all lanes)
         if (active && tid + L * k < items_new) f[k] = load(tid + L * k);
       }
+      if (uint32_t(id) >= uint32_t(a.n_pages)) break;   // (only here: the rows' loads need no page)
       const PagedView &view = is_v ? a.cv : a.ck;
       char *c = static_cast<char *>(view.p) + id * view.ps + int64_t(slot) * view.ss +
                 int64_t(h) * view.hs;

@@ -316,8 +316,8 @@ AttnPlan attn_plan(uint32_t dtype, int64_t T, int32_t R, int32_t nq, int32_t nk,
 
 // ---- the paged KV cache in 8 bits ----
 // As many as leave four wavefronts a SIMD unit, at most all (1 / 2 / 4, us: 8192 rows of 8 + 8 heads
-// of 128, a scale for four tokens 18.3 / 16.7 / 20.8, for each 37.3 / 31.6 / 28.4; 400 single rows
-// 7.0 / 8.3 / 11.8).
+// of 128, a scale for four tokens 16.9 / 15.5 / 19.7, for each 35.3 / 29.4 / 26.4; 400 single rows
+// 6.9 / 8.1 / 11.8).
 uint32_t q8_write_inner(int64_t units, int32_t nk) {
   const int64_t groups = cdiv(2 * int64_t(nk), 4), x = units * groups / (16 * kUnits);
   return uint32_t(x < 1 ? 1 : x < groups ? x : groups);
