@@ -76,7 +76,8 @@ __device__ inline void bf16_parts(float x, float y, uint32_t *p) {
 }
 
 // 8 neighbouring elements of a query (zeros where `inside` is false) in N parts, with `flip`
-// negated. An infinity has no rest.
+// negated. An infinity has no rest; a NaN whose first part is an infinity (its upper mantissa
+// bits are zero) is one in its rest.
 template <int DT, int N>
 __device__ inline void load_query(const char *p, bool inside, uint32_t flip, u32x4 *q) {
   if constexpr (DT == kBF16) {
@@ -97,8 +98,8 @@ __device__ inline void load_query(const char *p, bool inside, uint32_t flip, u32
       bf16_parts<N>(x, y, w);
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        if (k > 0 && !(fabsf(x) < __builtin_inff())) w[k] &= 0xFFFF0000u;
-        if (k > 0 && !(fabsf(y) < __builtin_inff())) w[k] &= 0x0000FFFFu;
+        if (k > 0 && fabsf(x) == __builtin_inff()) w[k] &= 0xFFFF0000u;
+        if (k > 0 && fabsf(y) == __builtin_inff()) w[k] &= 0x0000FFFFu;
         q[k][i] = w[k];
       }
     }
