@@ -241,7 +241,7 @@ struct PagedQ8Args {
   PagedArgs a;
   ScaleView ks, vs;
   float scale;            // |scale| log2 e
-  int32_t block;
+  int32_t block;          // as the caller gave it; kernels divide by block_div alone
   FastDiv block_div;      // by block
   int32_t runs;           // PA8_ROWS: its workgroups
   int32_t step_shift;     // steps of 2^step_shift keys are what it shares out

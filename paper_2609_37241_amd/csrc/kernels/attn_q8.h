@@ -179,9 +179,11 @@ __device__ inline NanKeys nan_keys(int32_t key, bool inside, const int32_t *tabl
 // ---- PA8_ROWS -----------------------------------------------------------------------------------
 // Few rows per request (decode), as PA_ROWS: the wavefronts share out a tile's keys,
 // each with its own softmax, joined in LDS at the end. HBM-bound: K and V come in whole rows,
-// past the caches (through them 115 us for the 101 below), and pass as codes through a part of LDS that is the wavefront's own, where a lane's 16
-// codes of K are two products' operands, and the transposing read of bytes gives it 8 keys of one
-// element of V.
+// past the caches, always: through them 114 us for the 101 below, 40.8 for the 37.4 of 32 requests of 2000
+// keys, whose codes the last-level cache would hold; only where several tiles of a call read the same keys
+// are they 2-3 % faster (64 new tokens behind 3900, 16 and 4 heads, 22.2 for 22.6). They pass as
+// codes through a part of LDS that is the wavefront's own, where a lane's 16 codes of K are two
+// products' operands, and the transposing read of bytes gives it 8 keys of one element of V.
 //
 // Products of 16 rows would leave most of them empty where few query heads share a K head.
 // So a tile is 16 / HG rows of each of HG neighbouring K heads, and a step of a wavefront 64 / HG
@@ -774,8 +776,11 @@ start:
 // numbers that their codes are: converted once, on the way to LDS, not by each of the
 // four wavefronts. Two of these fetch the step's K and V scales, one a lane, which all
 // read from LDS in fours (one of each four, where neighbouring keys share it, gained 1.5 %
-// only: 2048 tokens behind 6144, 291 -> 287 us). The running maximum as in PA_TILE; bf16
-// weights are one part, rounded, float32 ones three.
+// only: 2048 tokens behind 6144, 291 -> 287 us). The running maximum as in PA_TILE. bf16
+// weights, times their V scales, are one part, rounded: that adds to the rounding of the result up to as
+// much again (0.0017 -> 0.0020 .. 0.0025 against 64 bits), and a second part, as few rows have it, would
+// take 362 us for the 288 of those tokens, 41.0 for 36.5 of the windowed mixture, 64.1 for 56.6 of the
+// prompts. float32 ones are three parts.
 // Bound, as there, by each wavefront's chain of products, exponentials and LDS reads: those 2048
 // tokens, 32 and 8 heads of 128, 826 TFLOP/s in e4m3, 799 in int8 (from bf16 pages 845); a prompt's
 // last tile alone, 1024 keys of heads of 256, takes the 57 us of four such prompts.

@@ -100,7 +100,8 @@ tri_status tri_paged_attention_quant(tri_cache *c, const tri_attention_args *p, 
                    uint64_t(a.kv.hd), uint64_t(a.nq), uint64_t(a.kv.nk));
   k.k3 = (uint64_t(plan.form) << 16) | (uint64_t(plan.splits > 1) << 24) |
          (uint64_t(plan.heads) << 25) | key_code(*q8);
-  const PagedQ8Args args{attn_args(a, plan, 1.0f, attn_outgrows(a, 1)),
+  // (no `stream`: PA8_ROWS streams always, see there; the other forms never)
+  const PagedQ8Args args{attn_args(a, plan, 1.0f, false),
                          {q8->k_scale, q8->k_ps, q8->k_bs, q8->k_hs},
                          {q8->v_scale, q8->v_ps, q8->v_bs, q8->v_hs},
                          weight_scale(a.scale), q8->block, fast_div_of(uint32_t(q8->block)),
