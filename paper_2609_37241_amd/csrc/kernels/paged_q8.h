@@ -94,10 +94,20 @@ __device__ inline uint32_t to_codes4(const float *x, const Rounder &r) {
   }
 }
 
+// A float32 from which any rounding to fewer bits, ties included, goes as from q itself: cut off, its last
+// place 1 where that leaves something.
+__device__ inline float to_odd(double q) {
+  const float f = float(q);
+  uint32_t b = __float_as_uint(f);
+  if (double(f) != q) b = (b - uint32_t(fabs(double(f)) > fabs(q))) | 1u;
+  return __uint_as_float(b);
+}
+
 // Codes of scale `was` as codes of `now` > was: the nearest to c was / now. A float32 product
 // with the quotient is off by 2^-15 at most, so it tells which whole number is nearest, but within
 // 2^-12 of the middle of two; e4m3's powers of two have exact products. Else 64 bits: c was is
-// exact in them, and a quotient of 31 by 24 bits is a tie or more than 2^-56 of it off.
+// exact in them, and a quotient of 31 by 24 bits is a tie or more than 2^-56 of it off (e4m3's `now`
+// is a power of two: the quotient is exact).
 template <int CT>
 __device__ inline uint32_t recode4(uint32_t c, float was, float now) {
   float f[4], y[4];
@@ -117,7 +127,7 @@ __device__ inline uint32_t recode4(uint32_t c, float was, float now) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const double q = double(f[i]) * double(was) / double(now);
-      y[i] = CT == kInt8 ? float(rint(q)) : float(q);
+      y[i] = CT == kInt8 ? float(rint(q)) : to_odd(q);
     }
   }
   if constexpr (CT == kInt8) {

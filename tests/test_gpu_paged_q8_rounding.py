@@ -56,3 +56,44 @@ def test_codes_of_a_scale_divided_once(cache, hd):  # noqa: F811
     codes = np.rint(rows.astype(np.float64) / s[:, None])
     assert (p["kc"].cpu().numpy().reshape(T, hd) == codes).all()
     assert P.CODE_MAX[P.INT8] == np.abs(codes).max()
+
+
+def beside_ties():
+    """(code, scale): e4m3 values and float32 scales below 1 whose product is not in the middle of two
+    codes, but the float32 nearest to it is, and the even one of the two is the farther."""
+    codes = np.arange(1, 127, dtype=np.uint8)
+    v = torch.from_numpy(codes).view(torch.float8_e4m3fn).double().numpy()
+    middles = (v[:-1] + v[1:]) / 2
+    found = []
+    for c in v:
+        for m in middles[(middles < c) & (middles > 0.3 * c)]:
+            near = np.float32(m / c)
+            for s in (np.nextafter(near, np.float32(0)), near, np.nextafter(near, np.float32(1))):
+                z = c * np.float64(s)
+                if z != m and np.float32(z) == np.float32(m) and s < 1:
+                    if P.nearest_code(z, P.E4M3) != P.nearest_code(m, P.E4M3):
+                        found.append((c, s))
+    return found
+
+
+@pytest.mark.parametrize("hd", [64, 30])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_held_codes_of_scales_that_are_no_powers_of_two(cache, dtype, hd):  # noqa: F811
+    """A block that goes on and whose scale grows to 1: held codes become the nearest to c s, also
+    in a cache filled elsewhere, whose e4m3 scales are any numbers."""
+    found = beside_ties()
+    assert len(found) > 200
+    n, page = len(found), 4
+    p = {c: code_tensor((n, page, 1, hd), "e4m3", "slot") for c in ("kc", "vc")}
+    p.update({s: scale_tensor((n, 1, 1), "slot") for s in ("ks", "vs")})
+    held = torch.tensor([c for c, _ in found], dtype=torch.float32, device=DEV).view(n, 1, 1, 1).expand(n, 3, 1, hd)
+    scales = torch.from_numpy(np.array([s for _, s in found], dtype=np.float32)).to(DEV).view(n, 1, 1)
+    for c, s, sign in (("kc", "ks", 1), ("vc", "vs", -1)):
+        p[c][:, :3] = (sign * held).to(p[c].dtype)
+        p[s].copy_(scales)
+    x = torch.full((n, 1, hd), 448.0, dtype=DT[dtype], device=DEV)
+    p.update(k=x, v=x, table=i32([[r] for r in range(n)]), kv_len=i32([4] * n), q_start=i32(list(range(n + 1))))
+    want = written(p, "e4m3")
+    assert (want[2] == 1).all()
+    write(cache, p)
+    same(p, want)
