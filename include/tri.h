@@ -668,8 +668,8 @@ int64_t tri_paged_attention_workspace(const tri_attention_args *args);
  * block 1..page, a divisor of page. nk 1..4096, hd 1..512; cols * page below 2^31. */
 tri_status tri_kv_write_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
 
-/* The tokens' values code * scale, rounded once, into rows of k and v (which the call
- * writes; they must not overlap each other or the cache). With kv_len = lengths and q_start their running
+/* The tokens' values, code * scale in float32, rounded once to the type of k and v, into their
+ * rows (which the call writes; they must not overlap each other or the cache). With kv_len = lengths and q_start their running
  * sum: all tokens. Rows before q_start[0] and from q_start[R] on are left as they were. */
 tri_status tri_kv_read_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
 

@@ -191,7 +191,9 @@ __device__ inline NanKeys nan_keys(int32_t key, bool inside, const int32_t *tabl
 // scores of its own head's rows and gives the others' weights of 0, so the products are as many
 // per byte as with one head, the exponentials 1 / HG, and what is read in a slot is HG
 // heads long (64 requests of up to 8192 keys, 32 and 8 heads of 128, one / two / four a tile: 117
-// / 111 / 101 us; all of 8192 213 / 205 / 188, 5.7 TB/s of codes; one of 131,072 68 / 62 / 62).
+// / 111 / 101 us; all of 8192 213 / 205 / 188, 5.7 TB/s of codes; one of 131,072 68 / 62 / 62). float32
+// queries, three products for one, over the ragged 64: 111 us (int8), 119 (e4m3, spills 17 registers a lane);
+// 32 of them with 16 and 8 heads of 256 110, and 132 where e4m3 spills 70 (bf16, 98).
 // A NaN code of V would meet other heads' weights of 0: a unit whose sums hold one where
 // the weights are finite is done again with such codes cleared.
 //
@@ -780,7 +782,8 @@ start:
 // weights, times their V scales, are one part, rounded: that adds to the rounding of the result up to as
 // much again (0.0017 -> 0.0020 .. 0.0025 against 64 bits), and a second part, as few rows have it, would
 // take 362 us for the 288 of those tokens, 41.0 for 36.5 of the windowed mixture, 64.1 for 56.6 of the
-// prompts. float32 ones are three parts.
+// prompts. float32 ones are three parts, as are queries: those 2048 tokens 729 us, 330 TFLOP/s (990 of
+// products in bf16); 1024 behind 3072, 16 and 8 heads of 256, whose registers spill, 268 (bf16 119).
 // Bound, as there, by each wavefront's chain of products, exponentials and LDS reads: those 2048
 // tokens, 32 and 8 heads of 128, 826 TFLOP/s in e4m3, 799 in int8 (from bf16 pages 845); a prompt's
 // last tile alone, 1024 keys of heads of 256, takes the 57 us of four such prompts.
