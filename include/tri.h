@@ -663,14 +663,15 @@ int64_t tri_paged_attention_workspace(const tri_attention_args *args);
  * TRI_E4M3 2^-4 of the value, or half of 2^-9 scales near zero. The pages that a
  * call writes to must be distinct (of two tokens with one slot either may remain, and the
  * block's scale may fit neither). k and v are only read, and must not overlap the cache
- * or the scales.
+ * or the scales. Codes and scales of K must not overlap those of V (INVALID where both begin at one
+ * address); read and attended over they may.
  *
  * block 1..page, a divisor of page. nk 1..4096, hd 1..512; cols * page below 2^31. */
 tri_status tri_kv_write_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
 
 /* The tokens' values, code * scale in float32, rounded once to the type of k and v, into their
- * rows (which the call writes; they must not overlap each other or the cache). With kv_len = lengths and q_start their running
- * sum: all tokens. Rows before q_start[0] and from q_start[R] on are left as they were. */
+ * rows, which the call writes: they must not overlap the cache or each other (INVALID where both begin
+ * at one address). With kv_len = lengths and q_start their running sum: all tokens. Rows before q_start[0] and from q_start[R] on are left as they were. */
 tri_status tri_kv_read_quant(tri_cache *cache, const tri_kv_rows_args *args, void *stream);
 
 /* tri_paged_attention over codes: args->kv holds their addresses and strides, args->dtype is

@@ -37,6 +37,10 @@ tri_status rows_q8(tri_cache *c, uint32_t op, const tri_kv_rows_args *p, void *s
       (addr(a.kv_len) | addr(a.q_start)) % 4 || a.k_ts < w || a.v_ts < w ||
       !extent_ok(a.T, a.k_ts, w, es) || !extent_ok(a.T, a.v_ts, w, es))
     return finish_early(c, op, TRI_E_INVALID);
+  const bool write = op == TRI_OP_KV_WRITE_Q8;
+  // what is written for K and for V at one place: codes or scales that fit neither
+  if (write ? a.kv.k == a.kv.v || a.q8.k_scale == a.q8.v_scale : a.k == a.v)
+    return finish_early(c, op, TRI_E_INVALID);
   // rows in 16-byte vectors, their codes in 4 or 8 bytes
   const uint64_t rows = addr(a.k) | addr(a.v) | (a.T > 1 ? uint64_t(a.k_ts | a.v_ts) * es : 0);
   const bool aligned = !(rows & 15u) && !(kv_bits(a.kv, 1) & (16 / es - 1));
@@ -49,7 +53,6 @@ tri_status rows_q8(tri_cache *c, uint32_t op, const tri_kv_rows_args *p, void *s
   const int64_t by_block = a.T / q.block + 2 * int64_t(a.R);
   const bool by_row = a.T <= by_block;
   const int64_t units = by_row ? a.T : by_block;
-  const bool write = op == TRI_OP_KV_WRITE_Q8;
   // the rows that a block gets, were the requests equal
   const int64_t rows_each = (a.T + a.R - 1) / a.R < q.block ? (a.T + a.R - 1) / a.R : q.block;
   const uint32_t team = write && vec ? q8_write_team(rows_each * per) : 1;
