@@ -779,8 +779,9 @@ start:
 // four wavefronts. Two of these fetch the step's K and V scales, one a lane, which all
 // read from LDS in fours (one of each four, where neighbouring keys share it, gained 1.5 %
 // only: 2048 tokens behind 6144, 291 -> 287 us). The running maximum as in PA_TILE. bf16
-// weights, times their V scales, are one part, rounded: that adds to the rounding of the result up to as
-// much again (0.0017 -> 0.0020 .. 0.0025 against 64 bits), and a second part, as few rows have it, would
+// weights, times their V scales, are one part, rounded: that adds to the rounding of the result about as
+// much again (0.0017 -> 0.0020 .. 0.0025 against 64 bits; in int8, where one key has nearly all of most rows'
+// weight and its rounding is every element's, up to 0.0030), and a second part, as few rows have it, would
 // take 362 us for the 288 of those tokens, 41.0 for 36.5 of the windowed mixture, 64.1 for 56.6 of the
 // prompts. float32 ones are three parts, as are queries: those 2048 tokens 729 us, 330 TFLOP/s (990 of
 // products in bf16); 1024 behind 3072, 16 and 8 heads of 256, whose registers spill, 268 (bf16 119).
